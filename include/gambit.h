@@ -200,6 +200,86 @@ gambit_status gambit_decode_attn_layer(gambit_pool* pool, int32_t layer, int32_t
                                        const void* q, const void* k_new, const void* v_new, int32_t new_dtype,
                                        void* out, int32_t out_dtype, float sm_scale, void* stream);
 
+/*
+ * Packed tokens: prompts and drafts.  The calls below take tokens of several
+ * traces packed one trace after another, in list order: trace i's n_i tokens
+ * (n_i >= 0; a trace of none is left alone), then trace i + 1's.  They work
+ * on one layer and change neither lengths nor tables, so that a model can go
+ * through its layers:
+ *     gambit_kv_alloc(traces, n_i)                    once: room for the tokens
+ *     per layer l:  gambit_kv_write_layer(l, ...)     the layer's K and V
+ *                   gambit_prompt_attn(l, ...)        the layer's attention
+ * and, to verify drafted tokens,
+ *     per layer l:  gambit_tree_attn(l, ...)          drafts stay outside the pool
+ *     gambit_kv_alloc(traces, accepted)
+ *     per layer l:  gambit_kv_write_layer(l, ..., rows of the accepted drafts)
+ * Calls that list the same while the pool does not change (the layers of a
+ * step) share one plan, made by the first.  Device buffers are 16-byte
+ * aligned and contiguous; inputs and outputs do not overlap.  At most
+ * GAMBIT_MAX_PACKED tokens a call (fewer for a pool that cannot hold as many:
+ * 16 max_traces max_blocks_per_trace positions, or 64 nodes a slot).  A
+ * slot that holds a ghost cannot be listed.  Not while a decode step is open,
+ * not on a stream that is being captured (GAMBIT_ERR_UNSUPPORTED: the plan is
+ * uploaded by the call), and with the pool's device current.
+ */
+#define GAMBIT_MAX_PACKED 262144
+#define GAMBIT_MAX_NODES 64
+
+/* Write the K and V of packed tokens into layer `layer`: trace i's tokens go
+ * to its positions pos0[i] .. pos0[i] + n_tokens[i] - 1, which it holds
+ * (gambit_kv_alloc) in blocks of its own (else GAMBIT_ERR_SHARED_WRITE).
+ *   trace_ids, pos0, n_tokens  host [n]
+ *   k, v      device [n_rows][Hkv][head_dim] bf16
+ *   rows      host [total tokens]: the row of k and v that each packed token
+ *             takes (any order, rows may repeat or be left out); NULL: row i
+ *             for token i, n_rows = total tokens
+ * A bf16 pool stores the values.  An fp8 pool quantises them as gambit_decode_
+ * attn_layer does (nearest E4M3FN value of x / s, ties to the even code,
+ * saturating; NaN stays NaN).  A block whose first position is written takes
+ * its scales from the call: for K and for V the largest magnitude written into
+ * the block, over its tokens and KV heads (infinities as the largest finite
+ * value), / 448, and at least 2^-20, or at least fp8_append_scale when the
+ * write ends inside the block (later tokens are quantised with that scale).
+ * Values of the block's other positions are lost.  Other blocks keep their
+ * scales. */
+gambit_status gambit_kv_write_layer(gambit_pool* pool, int32_t layer, int32_t n, const int32_t* trace_ids,
+                                    const int32_t* pos0, const int32_t* n_tokens, const int32_t* rows,
+                                    int32_t n_rows, const void* k, const void* v, void* stream);
+
+/* Causal attention of prompt tokens over the cache: the last n_tokens[i]
+ * positions of trace i, whose K and V are in layer `layer`'s cache, attend to
+ * every position of the trace up to their own.  For the token at position t
+ * and query head h, with G = h / (Hq / Hkv),
+ *     out[token][h] = softmax(q[token][h] . K[0..t, G]^T * sm_scale) V[0..t, G]
+ * K and V past a token's own position do not reach its output, whatever they
+ * hold.  Blocks that several listed traces share before their tokens are read
+ * once for all of them when the traces have few tokens (up to 128 / (Hq / Hkv)
+ * each).
+ *   trace_ids, n_tokens  host [n]
+ *   q         device [total][Hq][head_dim] bf16
+ *   out       device [total][Hq][head_dim], bf16 or fp32 (out_dtype)
+ * With bf16 output the weights are rounded to bf16 before they meet V (half a
+ * step of 2^-7 of each), with fp32 output to 16 bits; sums are fp32. */
+gambit_status gambit_prompt_attn(gambit_pool* pool, int32_t layer, int32_t n, const int32_t* trace_ids,
+                                 const int32_t* n_tokens, const void* q, void* out, int32_t out_dtype,
+                                 float sm_scale, void* stream);
+
+/* Attention of a tree of drafted tokens of each trace: node j of trace i
+ * attends to all of the trace's cached positions (none is allowed), to its
+ * ancestors in the tree and to itself.
+ *   trace_ids, n_nodes  host [n]; n_nodes[i] <= GAMBIT_MAX_NODES
+ *   parents   host [total]: node j's parent within its tree, < j; -1: the
+ *             node follows the trace's last cached token
+ *   q         device [total][Hq][head_dim] bf16
+ *   k_new, v_new  device [total][Hkv][head_dim] bf16, the drafts' K and V
+ *             (used as they are, by fp8 pools too)
+ *   out       device [total][Hq][head_dim], bf16 or fp32 (out_dtype)
+ * Drafts that are not a node's ancestors do not reach its output, whatever
+ * they hold.  Shared blocks and precision as for gambit_prompt_attn. */
+gambit_status gambit_tree_attn(gambit_pool* pool, int32_t layer, int32_t n, const int32_t* trace_ids,
+                               const int32_t* n_nodes, const int32_t* parents, const void* q, const void* k_new,
+                               const void* v_new, void* out, int32_t out_dtype, float sm_scale, void* stream);
+
 /* A thought boundary (Alg. 1 Tournament; Eqs. 2-3; Sec. 4.1):
  *   score[i] = 1 / (1 + exp(-(h[i] . w + b)))   (linear sigmoid probe, the
  *              head form of Eq. 6 applied to the boundary hidden state)

@@ -17,7 +17,8 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libgambit.so")
 SOURCES = ["gambit_pool.cpp", "blocktable.hip", "decode_attn.hip", "probe_topk.hip", "mlp_scorer.hip",
-           "seq_scorer.cpp", "seqscorer.hip", "membench.hip"]
+           "seq_scorer.cpp", "seqscorer.hip", "membench.hip", "rows_attn.cpp", "rows_attn.hip",
+           "rows_write.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-mcode-object-version=5",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
@@ -28,7 +29,10 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-mcode
 # every such max first quiets its operands (one extra instruction each); no
 # NaN ever reaches a max there (cache slots past a chunk's end are replaced
 # by a select before any max), so that source is built without IEEE mode.
-EXTRA = {"decode_attn.hip": ["-fno-honor-nans", "-mno-amdgpu-ieee"]}
+# So is the packed rows' attention, where a NaN score that a row sees is passed
+# over by the max and then makes the row's weights NaN.
+EXTRA = {"decode_attn.hip": ["-fno-honor-nans", "-mno-amdgpu-ieee"],
+         "rows_attn.hip": ["-fno-honor-nans", "-mno-amdgpu-ieee"]}
 
 
 def build(verbose: bool = False) -> str:

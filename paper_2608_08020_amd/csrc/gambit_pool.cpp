@@ -24,18 +24,15 @@
 
 #include "../../include/gambit.h"
 #include "kernels.h"
+#include "pool.h"
 
+using namespace gambit::host;
 using gambit::AttnUnit;
 
 namespace {
 
-constexpr size_t kAlign = 256;
-constexpr int kDefaultSplits = 64;
-constexpr int kMaxLayers = 1024;
 constexpr int kDefaultChunkBlocks = 64;  // blocks per attention chunk before balancing
-
-size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
-int cdiv(int a, int b) { return (a + b - 1) / b; }
+constexpr size_t kPackedPartRows = 131072;  // partial rows of a packed call: two rounds of 512 workgroups of 128
 
 // Per-token times of one attention unit on MI355X (microseconds), by kind and
 // cache dtype: narrow units per wave, cooperative items per workgroup.  fp8:
@@ -56,13 +53,6 @@ constexpr double kUsCoop64_8 = 0.037, kUsCoop128_8 = 0.051;  // fp8, 33-64 and 6
 constexpr double kStartNarrow16 = 0.09, kStartCoop64_16 = 0.05, kStartCoop128_16 = 0.064;
 // Chunk caps as fractions of the estimated launch length.
 constexpr double kCapNarrow = 1.0, kCapCoop = 0.5;
-
-// Workspace carve-up.  All offsets are kAlign-aligned.
-struct Layout {
-  size_t list, ids, req_trace, req_ntok, pairs, free_list, nk, ticket, queues, err, scales, freebits,
-      alloc_list, units, members, part_ml, part_acc, sbar, nscore, gen, ghost, tourn, total;
-  int kmax, max_units, max_members, nwords;
-};
 
 bool layout_of(const gambit_pool_desc* d, Layout* L) {
   if (!d) return false;
@@ -102,101 +92,32 @@ bool layout_of(const gambit_pool_desc* d, Layout* L) {
   L->alloc_list = take(4 * (size_t)d->num_blocks);
   L->units = take(sizeof(AttnUnit) * (size_t)L->max_units);
   L->members = take(4 * ((size_t)L->max_members + gambit::kMemberPad));
-  L->part_ml = take(8 * (size_t)T * d->num_q_heads * kmax);
-  L->part_acc = take(4 * (size_t)T * d->num_q_heads * kmax * gambit::kHeadDim);
+  // decode steps write up to kmax partials a trace; the packed rows of a
+  // prompt or tree call as many as two rounds of workgroups
+  L->max_parts = (int)std::min<size_t>(std::max<size_t>((size_t)T * kmax, kPackedPartRows / d->num_q_heads + 1), 1 << 30);
+  L->part_ml = take(8 * (size_t)L->max_parts * d->num_q_heads);
+  L->part_acc = take(4 * (size_t)L->max_parts * d->num_q_heads * gambit::kHeadDim);
   L->sbar = take(4 * (size_t)T);
   L->nscore = take(4 * (size_t)T);
   L->gen = take(4 * (size_t)T);
   L->ghost = take(4 * (size_t)T);
   L->tourn = take(4 * ((size_t)gambit::kTournHeader + 3 * (size_t)T));
+  const size_t held = (size_t)T * d->max_blocks_per_trace * 16;
+  L->max_packed = (int)std::min<size_t>(GAMBIT_MAX_PACKED, std::max<size_t>(held, (size_t)T * gambit::kMaxNodes));
+  L->max_items = L->max_packed / (gambit::kRowsTile / g) + 2 * T + L->max_parts;
+  L->rows_plan_bytes = align_up(sizeof(gambit::RowItem) * (size_t)L->max_items) + align_up(8 * (size_t)L->max_packed) +
+                       3 * align_up(4 * (size_t)L->max_packed) + align_up(4 * (size_t)L->max_parts);
+  L->write_plan_bytes = align_up(sizeof(gambit::WriteItem) * ((size_t)L->max_packed / 16 + 2 * (size_t)T)) +
+                        align_up(4 * (size_t)L->max_packed);
+  L->rows_plan = take(L->rows_plan_bytes);
+  L->write_plan = take(L->write_plan_bytes);
   L->total = o;
   return true;
 }
 
 }  // namespace
 
-struct gambit_pool {
-  gambit_pool_desc d{};
-  Layout L{};
-  gambit::DevPool dev{};
-  uint8_t* ws = nullptr;
-  int g = 1;
-  int n_cu = 256;  // compute units of the pool's device (two attention workgroups each)
-  float append_scale = 1.f / 64.f;
-
-  // host mirror
-  std::vector<std::vector<int32_t>> table;
-  std::vector<int32_t> seq_len, refcount;
-  // tournament bookkeeping (Alg. 1): scored thoughts, tokens generated since
-  // creation, ghost flag; the scores themselves live on the device only
-  std::vector<int32_t> nscore, gen;
-  std::vector<char> ghost;
-  std::vector<uint64_t> freebits;  // bit set = free
-  int32_t nfree = 0;
-  size_t hint = 0;                 // no free bit below word `hint`
-
-  // pinned staging for host-to-device copies, reused after an event fence
-  int32_t* stage = nullptr;
-  size_t stage_ints = 0;
-  hipEvent_t stage_ev = nullptr;
-  uint8_t* plan_stage = nullptr;
-  size_t plan_stage_bytes = 0;
-  hipEvent_t plan_ev = nullptr;
-
-  // attention plan
-  bool plan_valid = false;
-  std::vector<int32_t> plan_list;
-  int xcd_off[9] = {0};
-  int plan_steps = 0;              // decode steps taken with the plan
-  size_t plan_partials = 0;        // partials of one head that a launch with the plan writes
-  int grid = 0;
-  int n_units = 0;
-  bool queues_dirty = false;       // an attention launch was not followed by its merge
-  int max_splits_used = 0;
-  int step_next = 0;               // the layer the open decode step expects next (0: none open)
-  gambit::AttnLaunch step{};       // the open step's launch arguments
-  std::vector<int32_t> cnt, first;  // per-block planner scratch, zero / -1 between calls
-  gambit_stats stats{};            // of plan_list, kept current by decode steps
-  std::vector<int32_t> plan_kinds;  // per list position: GAMBIT_UNIT_* bits of the units covering it
-
-  // attention-kernel event timing
-  std::vector<hipEvent_t> prof_ev;
-  int prof_used = 0;
-  bool prof_on = false;
-
-  std::string last_error;
-};
-
 namespace {
-
-gambit_status fail(gambit_pool* p, gambit_status s, const char* fmt, ...) {
-  if (p) {
-    char buf[512];
-    va_list ap;
-    va_start(ap, fmt);
-    vsnprintf(buf, sizeof buf, fmt, ap);
-    va_end(ap);
-    p->last_error = buf;
-  }
-  return s;
-}
-
-gambit_status hip_fail(gambit_pool* p, hipError_t e, const char* where) {
-  return fail(p, GAMBIT_ERR_DEVICE, "%s: %s", where, hipGetErrorString(e));
-}
-
-#define HIP_TRY(p, expr, where)                 \
-  do {                                          \
-    const hipError_t e_ = (expr);               \
-    if (e_ != hipSuccess) return hip_fail(p, e_, where); \
-  } while (0)
-
-inline hipStream_t S(void* s) { return static_cast<hipStream_t>(s); }
-
-template <class T>
-T* ws_ptr(gambit_pool* p, size_t off) {
-  return reinterpret_cast<T*>(p->ws + off);
-}
 
 // Runs f(0) .. f(n - 1) on up to 8 host threads (the calling one included),
 // in chunks of 16 indices; serially for small n or if no thread can start.
@@ -278,6 +199,7 @@ void mirror_add_refs(gambit_pool* p, const int32_t* row, int n, int delta) {
 }
 
 void mirror_grow(gambit_pool* p, int t, int ntok) {
+  ++p->epoch;
   const int L = p->seq_len[t];
   for (int j = cdiv(L, 16); j < cdiv(L + ntok, 16); ++j) {
     const int b = take_lowest(p);
@@ -315,6 +237,7 @@ void mirror_fork_many(gambit_pool* p, const int32_t* parents, const int32_t* chi
 }
 
 void mirror_release_rows(gambit_pool* p, int t) {
+  ++p->epoch;
   mirror_add_refs(p, p->table[t].data(), (int)p->table[t].size(), -1);
   p->table[t].clear();
   p->seq_len[t] = 0;
@@ -347,21 +270,6 @@ gambit_status upload_ints(gambit_pool* p, int32_t* dst, const int32_t* src, size
   std::memcpy(p->stage + stage_off, src, n * 4);
   HIP_TRY(p, hipMemcpyAsync(dst, p->stage + stage_off, n * 4, hipMemcpyHostToDevice, s), "upload");
   HIP_TRY(p, hipEventRecord(p->stage_ev, s), "staging fence");
-  return GAMBIT_OK;
-}
-
-gambit_status check_ids(gambit_pool* p, int32_t n, const int32_t* ids, const char* what,
-                        std::vector<char>* seen_out = nullptr) {
-  if (n < 0 || n > p->d.max_traces) return fail(p, GAMBIT_ERR_INVALID, "%s count %d out of range", what, n);
-  if (n > 0 && !ids) return fail(p, GAMBIT_ERR_INVALID, "%s list is NULL", what);
-  std::vector<char> seen(p->d.max_traces, 0);
-  for (int i = 0; i < n; ++i) {
-    const int t = ids[i];
-    if (t < 0 || t >= p->d.max_traces) return fail(p, GAMBIT_ERR_INVALID, "%s id %d out of range", what, t);
-    if (seen[t]) return fail(p, GAMBIT_ERR_INVALID, "duplicate %s id %d", what, t);
-    seen[t] = 1;
-  }
-  if (seen_out) seen_out->swap(seen);
   return GAMBIT_OK;
 }
 
@@ -754,16 +662,6 @@ void invalidate_plan(gambit_pool* p) { p->plan_valid = false; }
 }  // namespace
 
 // =============================================================================
-namespace {
-
-// Calls that change or check the pool wait for an open decode step to end.
-gambit_status step_open(gambit_pool* p) {
-  return fail(p, GAMBIT_ERR_INVALID, "a decode step is open: layer %d of %d is next", p->step_next,
-              p->dev.num_layers);
-}
-
-}  // namespace
-
 extern "C" {
 
 const char* gambit_status_str(gambit_status s) {
@@ -846,17 +744,24 @@ gambit_status gambit_pool_create(const gambit_pool_desc* desc, void* stream, gam
                         4 * (size_t)L.max_members + 4 * kAlign;
   hipError_t e = hipHostMalloc(reinterpret_cast<void**>(&p->stage), p->stage_ints * 4, hipHostMallocDefault);
   if (e == hipSuccess) e = hipHostMalloc(reinterpret_cast<void**>(&p->plan_stage), p->plan_stage_bytes, hipHostMallocDefault);
+  if (e == hipSuccess)
+    e = hipHostMalloc(reinterpret_cast<void**>(&p->packed_stage), L.rows_plan_bytes + L.write_plan_bytes, hipHostMallocDefault);
+  if (e == hipSuccess) e = hipEventCreateWithFlags(&p->rows_ev, hipEventDisableTiming);
+  if (e == hipSuccess) e = hipEventCreateWithFlags(&p->write_ev, hipEventDisableTiming);
   if (e == hipSuccess) e = hipEventCreateWithFlags(&p->stage_ev, hipEventDisableTiming);
   if (e == hipSuccess) e = hipEventCreateWithFlags(&p->plan_ev, hipEventDisableTiming);
 
   if (e == hipSuccess) {
     int dev = 0, ncu = 0;
     e = hipGetDevice(&dev);
+    p->device = dev;
     if (e == hipSuccess) e = hipDeviceGetAttribute(&ncu, hipDeviceAttributeMultiprocessorCount, dev);
     if (e == hipSuccess && ncu > 0) p->n_cu = ncu;
   }
   if (e == hipSuccess) e = hipEventRecord(p->stage_ev, S(stream));
   if (e == hipSuccess) e = hipEventRecord(p->plan_ev, S(stream));
+  if (e == hipSuccess) e = hipEventRecord(p->rows_ev, S(stream));
+  if (e == hipSuccess) e = hipEventRecord(p->write_ev, S(stream));
   if (e == hipSuccess) e = hipMemsetAsync(p->ws + L.ticket, 0, 64, S(stream));
   if (e == hipSuccess) e = hipMemsetAsync(p->ws + L.queues, 0, 64, S(stream));
   if (e == hipSuccess) e = gambit::launch_pool_init(D, S(stream));
@@ -872,11 +777,16 @@ gambit_status gambit_pool_destroy(gambit_pool* p) {
   if (!p) return GAMBIT_ERR_INVALID;
   if (p->stage_ev) (void)hipEventSynchronize(p->stage_ev);
   if (p->plan_ev) (void)hipEventSynchronize(p->plan_ev);
+  if (p->rows_ev) (void)hipEventSynchronize(p->rows_ev);
+  if (p->write_ev) (void)hipEventSynchronize(p->write_ev);
   if (p->stage) (void)hipHostFree(p->stage);
+  if (p->packed_stage) (void)hipHostFree(p->packed_stage);
   if (p->plan_stage) (void)hipHostFree(p->plan_stage);
   for (hipEvent_t e : p->prof_ev) (void)hipEventDestroy(e);
   if (p->stage_ev) (void)hipEventDestroy(p->stage_ev);
   if (p->plan_ev) (void)hipEventDestroy(p->plan_ev);
+  if (p->rows_ev) (void)hipEventDestroy(p->rows_ev);
+  if (p->write_ev) (void)hipEventDestroy(p->write_ev);
 
   delete p;
   return GAMBIT_OK;

@@ -27,6 +27,7 @@ CODE_NAMES = {ERR_INVALID: "INVALID", ERR_OUT_OF_BLOCKS: "OUT_OF_BLOCKS",
               ERR_SHARED_WRITE: "SHARED_WRITE", ERR_UNSUPPORTED: "UNSUPPORTED",
               ERR_DEVICE: "DEVICE", ERR_WORKSPACE: "WORKSPACE"}
 MAX_RANK = 4096
+MAX_PACKED, MAX_NODES = 262144, 64
 
 
 class GambitError(RuntimeError):
@@ -89,7 +90,8 @@ EXPORTS = ["gambit_workspace_size", "gambit_pool_create", "gambit_pool_destroy",
            "gambit_mlp_workspace_size", "gambit_mlp_score", "gambit_scorer_workspace_size", "gambit_scorer_create",
            "gambit_scorer_destroy", "gambit_scorer_step", "gambit_scorer_fork", "gambit_scorer_free",
            "gambit_scorer_steps", "gambit_scorer_check", "gambit_scorer_last_error", "gambit_stream_read",
-           "gambit_plan_kinds", "gambit_mlp_score_static"]
+           "gambit_plan_kinds", "gambit_mlp_score_static", "gambit_kv_write_layer", "gambit_prompt_attn",
+           "gambit_tree_attn"]
 
 
 def lib() -> ctypes.CDLL:
@@ -138,6 +140,9 @@ def lib() -> ctypes.CDLL:
         "gambit_scorer_last_error": (ctypes.c_char_p, [vp]),
         "gambit_stream_read": (i32, [vp, ctypes.c_size_t, i32, i32, vp, vp]),
         "gambit_plan_kinds": (i32, [vp, i32, vp, vp]),
+        "gambit_kv_write_layer": (i32, [vp, i32, i32, vp, vp, vp, vp, i32, vp, vp, vp]),
+        "gambit_prompt_attn": (i32, [vp, i32, i32, vp, vp, vp, vp, i32, f32, vp]),
+        "gambit_tree_attn": (i32, [vp, i32, i32, vp, vp, vp, vp, vp, vp, vp, i32, f32, vp]),
         "gambit_mlp_score_static": (i32, [i32, vp, ctypes.POINTER(Mlp), vp, vp, i32, vp, vp]),
     }
     for name, (res, args) in sig.items():
@@ -420,6 +425,72 @@ class Pool:
         _spec(q, torch.bfloat16, (n, self.Hq, self.D), "q")
         self._check(lib().gambit_decode_attn_layer(self._h, layer, n, _ptr(ids), _dev(q), _dev(k_new), _dev(v_new),
                                                    nd, _dev(out), od, sm, _stream(stream)), "decode_attn_layer")
+        return out
+
+    def _packed(self, ids, counts, what: str):
+        """Host lists of a packed call and its number of tokens."""
+        ids, counts = _host_i32(ids), _host_i32(counts)
+        if counts.shape != ids.shape:
+            raise ValueError(f"{what}: expected one per trace")
+        if counts.size and int(counts.min()) < 0:
+            raise ValueError(f"{what}: negative")
+        return ids, counts, int(counts.sum(dtype=np.int64))
+
+    def kv_write_layer(self, layer: int, ids, pos0, n_tokens, k: torch.Tensor, v: torch.Tensor, rows=None,
+                       stream=None):
+        """gambit_kv_write_layer: packed tokens' K and V (bf16 [n_rows][Hkv][D]) into one layer at positions
+        pos0[i] .. of each trace; rows (host): the row of k and v each token takes."""
+        ids, nt, total = self._packed(ids, n_tokens, "n_tokens")
+        p0 = _host_i32(pos0)
+        if p0.shape != ids.shape:
+            raise ValueError("pos0: expected one per trace")
+        if rows is not None:
+            rows = _host_i32(rows)
+            if rows.shape != (total,):
+                raise ValueError(f"rows: expected {total}, got {rows.shape}")
+            if k.dim() != 3:
+                raise ValueError("k: expected [n_rows][Hkv][D]")
+        n_rows = total if rows is None else k.shape[0]
+        _spec(k, torch.bfloat16, (n_rows, self.Hkv, self.D), "k")
+        _spec(v, torch.bfloat16, (n_rows, self.Hkv, self.D), "v")
+        self._check(lib().gambit_kv_write_layer(self._h, layer, ids.size, _ptr(ids), _ptr(p0), _ptr(nt),
+                                                None if rows is None else _ptr(rows), n_rows, _dev(k), _dev(v),
+                                                _stream(stream)), "kv_write_layer")
+
+    def _attn_out(self, total: int, q: torch.Tensor, out, out_dtype):
+        """The output of a packed attention call and its code."""
+        shape = (total, self.Hq, self.D)
+        _spec(q, torch.bfloat16, shape, "q")
+        if out is None:
+            out = torch.empty(shape, dtype=out_dtype, device=q.device)
+        _spec(out, (torch.float32, torch.bfloat16), shape, "out")
+        return out, OUT_F32 if out.dtype == torch.float32 else OUT_BF16
+
+    def prompt_attn(self, layer: int, ids, n_tokens, q: torch.Tensor, out: torch.Tensor | None = None,
+                    out_dtype=torch.bfloat16, sm_scale=None, stream=None) -> torch.Tensor:
+        """gambit_prompt_attn: causal attention of each trace's last n_tokens[i] positions over layer `layer`'s
+        cache; q and out [total][Hq][D], packed in list order."""
+        ids, nt, total = self._packed(ids, n_tokens, "n_tokens")
+        out, od = self._attn_out(total, q, out, out_dtype)
+        sm = float(self.D ** -0.5 if sm_scale is None else sm_scale)
+        self._check(lib().gambit_prompt_attn(self._h, layer, ids.size, _ptr(ids), _ptr(nt), _dev(q), _dev(out), od, sm,
+                                             _stream(stream)), "prompt_attn")
+        return out
+
+    def tree_attn(self, layer: int, ids, n_nodes, parents, q: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor,
+                  out: torch.Tensor | None = None, out_dtype=torch.bfloat16, sm_scale=None, stream=None) -> torch.Tensor:
+        """gambit_tree_attn: each trace's tree of drafted tokens (parents: index within the tree, -1 a root) over
+        layer `layer`'s cache and the nodes' ancestors; q, out [total][Hq][D], k_new, v_new [total][Hkv][D]."""
+        ids, nn, total = self._packed(ids, n_nodes, "n_nodes")
+        up = _host_i32(parents)
+        if up.shape != (total,):
+            raise ValueError(f"parents: expected {total}, got {up.shape}")
+        out, od = self._attn_out(total, q, out, out_dtype)
+        _spec(k_new, torch.bfloat16, (total, self.Hkv, self.D), "k_new")
+        _spec(v_new, torch.bfloat16, (total, self.Hkv, self.D), "v_new")
+        sm = float(self.D ** -0.5 if sm_scale is None else sm_scale)
+        self._check(lib().gambit_tree_attn(self._h, layer, ids.size, _ptr(ids), _ptr(nn), _ptr(up), _dev(q),
+                                           _dev(k_new), _dev(v_new), _dev(out), od, sm, _stream(stream)), "tree_attn")
         return out
 
     def score_prune_branch(self, ids, h: torch.Tensor, w: torch.Tensor, b: float, keep: int,

@@ -1,0 +1,499 @@
+"""Packed tokens on the GPU: layer writes, prompt attention, draft trees.
+
+Attention is compared with the definition in float64 on the same inputs.  Of
+an output sum_u p_u v_u / sum_u p_u, with S = sum_u p_u |v_u| (p normalised),
+the kernels' errors are at most, relative to S and to |out|:
+  * the weights' rounding before they meet V: 2^-8 (bf16 output, half a step
+    of bf16), 2^-16 (fp32 output: a bf16 value and the bf16 remainder);
+  * a score's error d (in its natural-exponent units) makes a weight exp(d)
+    of itself: 128 fp32 additions of products, 2^-23 of sum |q k| each, and
+    the roundings of the exponent, 2^-23 of twice the largest |score|;
+  * fp32 sums over L positions: (L + 16) 2^-23, once over V, once over l;
+and the bf16 output's own rounding is 2^-8 of |out|.
+"""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle.attention import decode_attention
+from paper_2608_08020_amd.gambit import GambitError, Pool
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+D = 128
+
+
+def _k_phys(t):
+    return (t & 3) | ((t >> 1) & 4) | ((t << 1) & 8)
+
+
+class Kept:
+    """A pool, and the K and V of every trace in token order as float64 values."""
+
+    def __init__(self, Hq, Hkv, T=8, maxb=80, fp8=False, layers=1, nb=None, seed=0, splits=0):
+        self.gen = torch.Generator(device=DEV).manual_seed(seed)
+        self.Hq, self.Hkv, self.fp8, self.layers = Hq, Hkv, fp8, layers
+        self.pool = Pool(num_blocks=nb or T * maxb, num_q_heads=Hq, num_kv_heads=Hkv, max_traces=T,
+                         max_blocks_per_trace=maxb, kv_dtype="fp8_e4m3" if fp8 else "bf16", num_layers=layers,
+                         max_splits=splits)
+        # what no token was written to is NaN
+        self.pool.k_cache.view(torch.uint8).fill_(0x7F if fp8 else 0xFF)
+        self.pool.v_cache.view(torch.uint8).fill_(0x7F if fp8 else 0xFF)
+        self.K, self.V = {}, {}
+
+    def normal(self, *shape):
+        return torch.randn(shape, generator=self.gen, device=DEV).to(torch.bfloat16)
+
+    def cache(self, layer):
+        p = self.pool
+        if self.layers == 1:
+            return p.k_cache, p.v_cache, p.kv_scale
+        return p.k_cache[layer], p.v_cache[layer], None if p.kv_scale is None else p.kv_scale[layer]
+
+    def tokens(self, t, layer, lo, hi):
+        """Positions [lo, hi) of a trace as the cache holds them, from the documented layout, [n][Hkv][D] float64."""
+        kc, vc, sc = self.cache(layer)
+        pos = np.arange(lo, hi)
+        blk = self.pool.block_table[t].cpu().numpy()[pos // 16]
+        C = 16 if self.fp8 else 8
+        d = torch.arange(D, device=DEV)
+        b = torch.from_numpy(blk.astype(np.int64)).to(DEV)
+        row = torch.from_numpy(_k_phys(pos % 16)).to(DEV)
+        tok = torch.from_numpy(pos % 16).to(DEV)
+        h = torch.arange(self.Hkv, device=DEV)
+        nb = kc.shape[0]
+        ki = (torch.div(d, C, rounding_mode="floor") * 16 + row[:, None]) * C + d % C
+        vi = d * 16 + tok[:, None]
+        k = kc.view(nb, self.Hkv, 16 * D)[b[:, None, None], h[:, None], ki[:, None]]
+        v = vc.view(nb, self.Hkv, 16 * D)[b[:, None, None], h[:, None], vi[:, None]]
+        if self.fp8:
+            k, v = (x.view(torch.float8_e4m3fn).double() * sc[b, i].double().view(-1, 1, 1) for i, x in enumerate((k, v)))
+        return k.double(), v.double()
+
+    def extend(self, ids, counts, layer=0, k=None, v=None):
+        """Room for the tokens, and their K and V in one layer."""
+        N = sum(counts)
+        k = self.normal(N, self.Hkv, D) if k is None else k
+        v = self.normal(N, self.Hkv, D) if v is None else v
+        at = [self.pool.seq_len_of(t) for t in ids]
+        self.pool.kv_alloc(ids, counts)
+        self.pool.kv_write_layer(layer, ids, at, counts, k, v)
+        base = 0
+        for t, a, m in zip(ids, at, counts):
+            if self.fp8:  # what the codes stand for
+                kk, vv = self.tokens(t, layer, a, a + m)
+            else:
+                kk, vv = k[base:base + m].double(), v[base:base + m].double()
+            e = torch.zeros(0, self.Hkv, D, dtype=torch.float64, device=DEV)
+            self.K[t] = torch.cat([self.K.get(t, e), kk])
+            self.V[t] = torch.cat([self.V.get(t, e), vv])
+            base += m
+
+    def fork(self, parents, children):
+        self.pool.kv_fork(parents, children)
+        for p, c in zip(parents, children):
+            self.K[c], self.V[c] = self.K[p].clone(), self.V[p].clone()
+
+
+def _reference(q, K, V, sees, scale):
+    """q [m][Hq][D], K, V [L][Hkv][D] float64, sees [m][L]: the output and the bound's S, and the scores' size."""
+    g = q.shape[1] // K.shape[1]
+    out, S = torch.zeros_like(q), torch.zeros_like(q)
+    big = dot = 0.0
+    for h in range(q.shape[1]):
+        k, v = K[:, h // g], V[:, h // g]
+        z = (q[:, h] @ k.T) * scale
+        big = max(big, float(z[sees].abs().max()))
+        dot = max(dot, abs(scale) * float((q[:, h].abs() @ k.abs().T)[sees].max()))
+        p = torch.softmax(z.masked_fill(~sees, -math.inf), -1)
+        out[:, h], S[:, h] = p @ v, p @ v.abs()
+    return out, S, big, dot
+
+
+def _check(got, q, K, V, sees, scale=D ** -0.5):
+    ref, S, big, dot = _reference(q.double(), K, V, sees, scale)
+    d = 128 * 2.0 ** -23 * dot + 2.0 ** -23 * 2 * big
+    rel = 2 * math.expm1(d) + 2 * (K.shape[0] + 16) * 2.0 ** -23
+    if got.dtype == torch.float32:
+        tol = (rel + 2.0 ** -16) * (S + ref.abs())
+    else:
+        tol = (rel + 2.0 ** -8) * (S + ref.abs()) + 2.0 ** -8 * ref.abs()
+    err = (got.double() - ref).abs()
+    assert torch.isfinite(got.double()).all()
+    assert (err <= tol + 1e-30).all(), (float(err.max()), float((err / tol).max()))
+
+
+def _causal(L, m):
+    return torch.arange(L, device=DEV) <= (L - m + torch.arange(m, device=DEV))[:, None]
+
+
+def _kin(up):
+    m = len(up)
+    kin = torch.zeros(m, m, dtype=torch.bool)
+    for j in range(m):
+        if up[j] >= 0:
+            kin[j] = kin[up[j]]
+        kin[j, j] = True
+    return kin.to(DEV)
+
+
+def check_prompt(S, ids, counts, out_dtype, layer=0, **kw):
+    q = S.normal(sum(counts), S.Hq, D)
+    out = S.pool.prompt_attn(layer, ids, counts, q, out_dtype=out_dtype, **kw)
+    base = 0
+    for t, m in zip(ids, counts):
+        if m:
+            L = S.K[t].shape[0]
+            _check(out[base:base + m], q[base:base + m], S.K[t], S.V[t], _causal(L, m), kw.get("sm_scale", D ** -0.5))
+        base += m
+    return q, out
+
+
+def check_tree(S, ids, ups, out_dtype, layer=0, kn=None, vn=None, **kw):
+    counts = [len(u) for u in ups]
+    N = sum(counts)
+    q = S.normal(N, S.Hq, D)
+    kn = S.normal(N, S.Hkv, D) if kn is None else kn
+    vn = S.normal(N, S.Hkv, D) if vn is None else vn
+    flat = [x for u in ups for x in u]
+    out = S.pool.tree_attn(layer, ids, counts, flat, q, kn, vn, out_dtype=out_dtype, **kw)
+    base = 0
+    e = torch.zeros(0, S.Hkv, D, dtype=torch.float64, device=DEV)
+    for t, m, up in zip(ids, counts, ups):
+        if m:
+            K, V = S.K.get(t, e), S.V.get(t, e)
+            sees = torch.cat([torch.ones(m, K.shape[0], dtype=torch.bool, device=DEV), _kin(up)], 1)
+            s = slice(base, base + m)
+            _check(out[s], q[s], torch.cat([K, kn[s].double()]), torch.cat([V, vn[s].double()]), sees,
+                   kw.get("sm_scale", D ** -0.5))
+        base += m
+    return q, kn, vn, out
+
+
+def _random_tree(rng, m):
+    return [int(rng.integers(-1, j)) if rng.random() < 0.5 else max(-1, j - int(rng.integers(1, 4))) for j in range(m)]
+
+
+HEADS = [(8, 2), (4, 4), (16, 1), (24, 3), (64, 8), (6, 3)]
+OUT = [torch.float32, torch.bfloat16]
+
+
+# ------------------------------------------------------------------ writes --
+@pytest.mark.parametrize("Hkv", [1, 3, 8])
+@pytest.mark.parametrize("layers", [1, 3])
+def test_write_bf16_lands_where_the_layout_says(Hkv, layers):
+    S = Kept(Hkv, Hkv, T=6, maxb=9, layers=layers)
+    S.pool.k_cache.zero_(), S.pool.v_cache.zero_()
+    ids, pos0, n = [4, 0, 2, 5], [0, 7, 33, 16], [1, 50, 0, 64]
+    S.pool.kv_alloc(ids, [a + m + 3 for a, m in zip(pos0, n)])
+    k, v = S.normal(sum(n), Hkv, D), S.normal(sum(n), Hkv, D)
+    layer = layers - 1
+    S.pool.kv_write_layer(layer, ids, pos0, n, k, v)
+    base = 0
+    for t, a, m in zip(ids, pos0, n):
+        kk, vv = S.tokens(t, layer, a, a + m)
+        assert torch.equal(kk, k[base:base + m].double()) and torch.equal(vv, v[base:base + m].double())
+        base += m
+    # nothing else was written, in this layer or another
+    assert int((S.pool.k_cache != 0).sum()) == int((k != 0).sum())
+    assert int((S.pool.v_cache != 0).sum()) == int((v != 0).sum())
+    S.pool.pool_check()
+
+
+def test_write_takes_rows_in_any_order():
+    S = Kept(4, 2, T=4, maxb=6)
+    k, v = S.normal(9, 2, D), S.normal(9, 2, D)
+    rows = [8, 3, 3, 3, 0, 5, 8, 1]
+    S.pool.kv_alloc([1, 3], [20, 5])
+    S.pool.kv_write_layer(0, [3, 1], [2, 14], [3, 5], k, v, rows=rows)
+    for t, a, r in ((3, 2, rows[:3]), (1, 14, rows[3:])):
+        kk, vv = S.tokens(t, 0, a, a + len(r))
+        assert torch.equal(kk, k[r].double()) and torch.equal(vv, v[r].double())
+
+
+def _codes(x, s):
+    """Nearest E4M3FN codes of x / s (float32 quotient)."""
+    return (x.float() / s).clamp(-448, 448).to(torch.float8_e4m3fn).view(torch.uint8)
+
+
+@pytest.mark.parametrize("Hkv", [1, 2, 8, 12])
+def test_write_fp8_scales_and_codes(Hkv):
+    S = Kept(Hkv, Hkv, T=4, maxb=8, fp8=True, layers=2)
+    ids, pos0, n = [2, 0, 3], [0, 21, 5], [40, 45, 6]
+    S.pool.kv_alloc(ids, [a + m + 2 for a, m in zip(pos0, n)])
+    old = 0.03125
+    S.pool.kv_scale.fill_(old)
+    N = sum(n)
+    k, v = S.normal(N, Hkv, D), S.normal(N, Hkv, D)
+    k[3] *= 1000.0            # a block of large values
+    v[17:32] *= 2.0 ** -30    # with token 16 below: a filled block of tiny ones
+    v[16] = 0.0
+    k[n[0] + 1, 0, 5] = 1e4   # beyond 448 of a scale that the block keeps
+    k[n[0] + 2, 0, 6] = math.nan
+    S.pool.kv_write_layer(1, ids, pos0, n, k, v)
+    table = S.pool.block_table.cpu().numpy()
+    kc, vc, sc = S.cache(1)
+    base = 0
+    for t, a, m in zip(ids, pos0, n):
+        for j in range(a // 16, (a + m - 1) // 16 + 1):
+            lo, hi = max(a, 16 * j), min(a + m, 16 * j + 16)
+            b = int(table[t, j])
+            for i, (x, cache) in enumerate(((k, kc), (v, vc))):
+                x = x[base + lo - a:base + hi - a]
+                if lo == 16 * j:
+                    most = x.float().abs().nan_to_num(0.0).max() / torch.tensor(448.0, device=DEV)
+                    want = torch.maximum(most, torch.tensor(2.0 ** -20 if hi - lo == 16 else 2.0 ** -6, device=DEV))
+                else:
+                    want = torch.tensor(old, device=DEV)
+                assert torch.equal(sc[b, i], want), (t, j, i)
+                code = cache[b].reshape(Hkv, -1)
+                r = np.arange(lo - 16 * j, hi - 16 * j)
+                d = np.arange(D)
+                idx = ((d // 16) * 16 + _k_phys(r)[:, None]) * 16 + d % 16 if i == 0 else d * 16 + r[:, None]
+                got = code[:, torch.from_numpy(idx).to(DEV)].permute(1, 0, 2)
+                w = _codes(x, want)
+                nan = torch.isnan(x.float())
+                assert torch.equal(got[~nan], w[~nan]) and ((got[nan] & 0x7F) == 0x7F).all(), (t, j, i)
+        base += m
+    # the other layer, and the slots between, keep what they had
+    assert (S.pool.k_cache[0] == 0x7F).all() and (S.pool.kv_scale[0] == old).all()
+    assert int((kc != 0x7F).sum()) <= N * Hkv * D
+
+
+# ------------------------------------------------------------------ prompts --
+@pytest.mark.parametrize("out_dtype", OUT)
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("heads", HEADS)
+def test_prompts_of_different_lengths(heads, fp8, out_dtype):
+    S = Kept(*heads, fp8=fp8, T=8, maxb=40)
+    ids, counts = [5, 0, 3, 7, 1], [1, 64, 130, 0, 257]
+    S.extend(ids, counts)
+    check_prompt(S, ids, counts, out_dtype)
+    S.extend(ids, [16, 1, 0, 3, 65])                   # behind what is cached
+    check_prompt(S, ids[::-1], [65, 3, 0, 1, 16], out_dtype)
+    check_prompt(S, [3], [1], out_dtype)               # single tokens
+    S.pool.pool_check()
+
+
+@pytest.mark.parametrize("out_dtype", OUT)
+@pytest.mark.parametrize("fp8", [False, True])
+def test_few_tokens_behind_shared_prefixes(fp8, out_dtype):
+    S = Kept(8, 2, fp8=fp8, T=16, maxb=300)
+    S.extend([0, 1], [1003, 640])
+    S.fork([0, 0, 0, 1, 1], [2, 3, 4, 5, 6])
+    S.extend([2, 5, 6], [70, 16, 5])
+    S.fork([2, 5], [7, 8])
+    ids = [8, 0, 2, 3, 5, 7, 1, 6]
+    counts = [3, 1, 8, 0, 20, 2, 32, 33]               # the last: more rows than one tile
+    S.extend(ids, counts)
+    check_prompt(S, ids, counts, out_dtype)
+    check_prompt(S, [0, 2, 7], [5, 40, 9], out_dtype)  # tokens that other traces hold too
+    check_prompt(S, [3, 4], [17, 1003], out_dtype)
+
+
+def test_a_long_context_is_split_and_joined():
+    S = Kept(32, 8, T=4, maxb=1300)
+    S.extend([2], [20011])
+    S.extend([2], [5])
+    q, out = check_prompt(S, [2], [5], torch.float32)
+    again = S.pool.prompt_attn(0, [2], [5], q, out_dtype=torch.float32)
+    assert torch.equal(out, again)                     # one order of sums
+    check_prompt(S, [2], [700], torch.bfloat16)
+
+
+@pytest.mark.parametrize("splits", [0, 1])
+def test_partial_slots_of_a_small_pool_suffice(splits):
+    S = Kept(64, 8, T=2, maxb=400, splits=splits)
+    S.extend([0], [6000])
+    S.fork([0], [1])
+    check_prompt(S, [1, 0], [16, 9], torch.float32)
+    check_tree(S, [0, 1], [_random_tree(np.random.default_rng(1), 64)] * 2, torch.float32)
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.05, 0.5])
+def test_softmax_scales(scale):
+    S = Kept(8, 2, T=4, maxb=20)
+    S.extend([1], [150])
+    check_prompt(S, [1], [150], torch.float32, sm_scale=scale)
+    check_tree(S, [1], [[-1, 0, 0]], torch.float32, sm_scale=scale)
+
+
+@pytest.mark.parametrize("bad", [math.inf, -math.inf, math.nan])
+@pytest.mark.parametrize("out_dtype", OUT)
+def test_later_tokens_do_not_reach_earlier_ones_whatever_they_hold(bad, out_dtype):
+    S = Kept(8, 2, T=4, maxb=20)
+    n, at = 180, 77
+    k, v = S.normal(n, 2, D), S.normal(n, 2, D)
+    S.extend([2], [n], k=k, v=v)
+    q, _ = check_prompt(S, [2], [n], out_dtype)
+    k[at:at + 3, 1, 17] = bad
+    v[at, 0, 3] = bad
+    v[at + 2, 1, 100] = bad
+    S.pool.kv_write_layer(0, [2], [0], [n], k, v)
+    out = S.pool.prompt_attn(0, [2], [n], q, out_dtype=out_dtype)
+    _check(out[:at], q[:at], S.K[2][:at], S.V[2][:at], _causal(at, at))
+    # KV head 0 (query heads 0-3): V of one element of one token is not finite
+    assert not torch.isfinite(out[at:, :4, 3].double()).any()
+    keep = torch.arange(D, device=DEV) != 3
+    assert torch.isfinite(out[:, :4][..., keep].double()).all()
+    # KV head 1: scores of +-inf or NaN from there on, where a row's weight is NaN or zero
+    assert torch.isfinite(out[:at, 4:].double()).all()
+
+
+# -------------------------------------------------------------------- trees --
+@pytest.mark.parametrize("out_dtype", OUT)
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("heads", HEADS)
+def test_trees_over_contexts_of_different_lengths(heads, fp8, out_dtype):
+    rng = np.random.default_rng(3)
+    S = Kept(*heads, fp8=fp8, T=10, maxb=60)
+    ids, ctx = [1, 4, 0, 7, 8, 2, 5], [1, 15, 16, 17, 640, 64, 333]
+    S.extend(ids, ctx)
+    ups = [_random_tree(rng, m) for m in (64, 1, 7, 33, 16, 0, 5)]
+    check_tree(S, ids + [9], ups + [[-1, -1, 0, 2]], out_dtype)      # the last over no cached position
+    check_tree(S, [8], [list(range(-1, 63))], out_dtype)             # a chain
+    check_tree(S, [8, 4], [[-1] * 64, [-1]], out_dtype)              # a star; a single token
+    S.pool.pool_check()
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+def test_trees_behind_shared_prefixes(fp8):
+    rng = np.random.default_rng(4)
+    S = Kept(32, 8, fp8=fp8, T=24, maxb=300)
+    S.extend([0, 1], [2501, 640])
+    S.fork([0] * 7 + [1] * 3, list(range(2, 12)))
+    S.extend([2, 3, 9], [100, 16, 3])
+    S.fork([2, 3, 9], [12, 13, 14])
+    ids = [int(x) for x in rng.permutation(15)]
+    check_tree(S, ids, [_random_tree(rng, int(rng.integers(0, 20))) for _ in ids], torch.float32)
+    check_tree(S, ids[:5], [_random_tree(rng, 8) for _ in ids[:5]], torch.bfloat16)
+
+
+@pytest.mark.parametrize("bad", [math.inf, math.nan])
+@pytest.mark.parametrize("out_dtype", OUT)
+def test_other_branches_do_not_reach_a_node_whatever_they_hold(bad, out_dtype):
+    S = Kept(8, 2, T=4, maxb=20)
+    S.extend([3], [50])
+    up = [-1, 0, 0, 1, 2, 3, -1]                      # node 2 and its child 4 are spoilt
+    q, kn, vn, _ = check_tree(S, [3], [up], out_dtype)
+    kn[2], vn[2] = bad, bad
+    vn[4, 1, 9] = bad
+    out = S.pool.tree_attn(0, [3], [7], up, q, kn, vn, out_dtype=out_dtype)
+    fine = [0, 1, 3, 5, 6]
+    # sums over a spoilt block go token by token, so not the same bits
+    _check(out[fine], q[fine], torch.cat([S.K[3], kn[fine].double()]), torch.cat([S.V[3], vn[fine].double()]),
+           torch.cat([torch.ones(5, 50, dtype=torch.bool, device=DEV), _kin([-1, 0, 1, 2, -1])], 1))
+    assert not torch.isfinite(out[2].double()).any()
+
+
+# ------------------------------------------------------------- as they are used --
+@pytest.mark.parametrize("fp8", [False, True])
+def test_a_serving_step(fp8):
+    """Prompts layer by layer, branches, drafted trees, the accepted path written back, then decode steps; the
+    attention of a chain of drafts is that of the same tokens once they are in the cache (bf16 pools)."""
+    L, Hq, Hkv = 2, 16, 4
+    S = Kept(Hq, Hkv, T=8, maxb=30, fp8=fp8, layers=L, seed=9)
+    per = []
+    ids, n = [0, 1], [75, 131]
+    S.pool.kv_alloc(ids, n)
+    for layer in range(L):
+        k, v = S.normal(sum(n), Hkv, D), S.normal(sum(n), Hkv, D)
+        S.pool.kv_write_layer(layer, ids, [0, 0], n, k, v)
+        S.K, S.V = {}, {}
+        for t, m in zip(ids, n):
+            S.K[t], S.V[t] = S.tokens(t, layer, 0, m)
+        check_prompt(S, ids, n, torch.float32, layer=layer)
+        per.append((dict(S.K), dict(S.V)))
+    S.pool.kv_fork([0, 1, 0], [2, 3, 4])
+    for K, V in per:
+        for a, b in ((0, 2), (1, 3), (0, 4)):
+            K[b], V[b] = K[a].clone(), V[a].clone()
+    pop, ups = [0, 1, 2, 3, 4], [[-1, 0, 1, 1], [-1, 0, 0, 2], [-1], [-1, -1], [-1, 0, 1, 2, 3]]
+    path = [[0, 1, 3], [0, 2], [0], [], [0, 1, 2, 3, 4]]
+    counts, took = [len(u) for u in ups], [len(x) for x in path]
+    base = np.cumsum([0] + counts)
+    rows = [int(b) + j for b, x in zip(base, path) for j in x]
+    at = [S.pool.seq_len_of(t) for t in pop]
+    drafts = []
+    for layer in range(L):
+        S.K, S.V = per[layer]
+        drafts.append(check_tree(S, pop, ups, torch.float32, layer=layer))
+    S.pool.kv_alloc(pop, took)
+    for layer in range(L):
+        q, kn, vn, out = drafts[layer]
+        S.pool.kv_write_layer(layer, pop, at, took, kn, vn, rows=rows)
+        S.K, S.V = per[layer]
+        for t, a, m in zip(pop, at, took):
+            kk, vv = S.tokens(t, layer, a, a + m)
+            S.K[t], S.V[t] = torch.cat([S.K[t], kk]), torch.cat([S.V[t], vv])
+        again = S.pool.prompt_attn(layer, pop, took, q[rows].contiguous(), out_dtype=torch.float32)
+        if not fp8:
+            assert (again - out[rows]).abs().max() <= 2.0 ** -14  # the same sums in another order
+    # a decode step of the framework over what is there now
+    qd = [S.normal(5, Hq, D) for _ in range(L)]
+    kd, vd = ([S.normal(5, Hkv, D) for _ in range(L)] for _ in range(2))
+    for layer in range(L):
+        out = S.pool.decode_attn_layer(layer, pop, qd[layer], kd[layer], vd[layer], new_dtype="bf16", out_dtype=torch.float32)
+        if not fp8:
+            K, V = per[layer]
+            for i, t in enumerate(pop):
+                ref = decode_attention(qd[layer][i].double().cpu().numpy(),
+                                       torch.cat([K[t], kd[layer][i:i + 1].double()]).cpu().numpy(),
+                                       torch.cat([V[t], vd[layer][i:i + 1].double()]).cpu().numpy(), D ** -0.5)
+                err = np.abs(out[i].cpu().numpy() - ref)
+                assert (err <= 1e-3 + 2e-3 * np.abs(ref)).all()
+    S.pool.pool_check()
+
+
+def test_another_stream_and_two_calls_at_once():
+    S = Kept(32, 8, T=6, maxb=100)
+    S.extend([0, 1], [900, 333])
+    q, want = check_prompt(S, [0, 1], [900, 333], torch.bfloat16)
+    other = Kept(32, 8, T=6, maxb=100, seed=1)
+    other.extend([3], [1000])
+    q2, want2 = check_prompt(other, [3], [1000], torch.bfloat16)
+    torch.cuda.synchronize()
+    s1, s2 = torch.cuda.Stream(), torch.cuda.Stream()
+    outs = []
+    for _ in range(3):  # two pools, each on a stream of its own
+        outs.append((S.pool.prompt_attn(0, [0, 1], [900, 333], q, stream=s1),
+                     other.pool.prompt_attn(0, [3], [1000], q2, stream=s2)))
+        outs.append((S.pool.prompt_attn(0, [0, 1], [900, 333], q, stream=s1, out=torch.empty_like(want)), outs[-1][1]))
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, want) and torch.equal(b, want2) for a, b in outs)
+
+
+def test_a_captured_stream_is_refused():
+    S = Kept(8, 2, T=2, maxb=8)
+    S.extend([0], [40])
+    q, out = check_prompt(S, [0], [40], torch.bfloat16)
+    g = torch.cuda.CUDAGraph()
+    x = torch.zeros(4, device=DEV)
+    with torch.cuda.graph(g):
+        x += 1
+        with pytest.raises(GambitError, match="captured"):
+            S.pool.prompt_attn(0, [0], [40], q, out=out)
+        with pytest.raises(GambitError, match="captured"):
+            S.pool.tree_attn(0, [0], [1], [-1], q[:1], q[:1, :2].contiguous(), q[:1, :2].contiguous(), out=out[:1])
+        with pytest.raises(GambitError, match="captured"):
+            S.pool.kv_write_layer(0, [0], [0], [1], q[:1, :2].contiguous(), q[:1, :2].contiguous())
+    g.replay()
+    torch.cuda.synchronize()
+    assert float(x[0]) == 1.0
+    check_prompt(S, [0], [40], torch.bfloat16)
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+def test_caches_past_four_gigabytes(fp8):
+    """Blocks whose byte offsets pass 32 bits: a trace holds the pool's first blocks, another its last."""
+    per = 16 * D * 8 * (1 if fp8 else 2)               # bytes of a block
+    nb = (1 << 32) // per + 40
+    S = Kept(16, 8, T=2, maxb=nb, nb=nb, fp8=fp8, splits=1)
+    S.pool.kv_alloc([0], [16 * (nb - 20)])
+    S.K[0] = S.V[0] = None
+    S.extend([1], [300])
+    assert int(S.pool.block_table[1, 0]) == nb - 20
+    check_prompt(S, [1], [300], torch.float32)
+    check_tree(S, [1], [[-1, 0]], torch.float32)
