@@ -17,7 +17,7 @@
 //
 // P is one bf16 operand when the output is bf16 (its rounding, 2^-8 of a
 // term, is of the output's own size and averages over the terms; the sum l is
-// taken over the rounded values) and hi + lo bf16 parts (16 bits) when the
+// taken over the rounded values) and three bf16 planes (24 bits) when the
 // output is fp32.
 //
 // A range that is split, or shared by several traces, leaves unnormalised
@@ -39,8 +39,6 @@ typedef int32_t i32x16 __attribute__((ext_vector_type(16)));
 #define GAMBIT_CONST __attribute__((address_space(4)))
 
 constexpr int kThreads = 256;
-constexpr int kVOff = kKeyTile * kHeadDim * 2;  // V behind K in a stage
-constexpr int kStage = 2 * kVOff;
 constexpr float kLazy = 8.f;  // a row's reference moves when a score exceeds it by 2^kLazy
 
 __device__ inline uint32_t pack_bf16x2(float a, float b) {
@@ -59,6 +57,32 @@ __device__ inline float ld_const(const float* p) {
 // need no quieting first); a NaN operand is passed over.
 __device__ inline float max3(float a, float b, float c) { return fmaxf(fmaxf(a, b), c); }
 
+// Four direct loads of 1 KiB each, 16 bytes a lane: from base + off + 1024 k
+// (base uniform, off the lane's) into LDS at l + 1024 k + 16 x lane.  An
+// instruction's offset counts for both sides.
+__device__ inline void dma16x4(const uint8_t* base, uint32_t off, uint8_t* l) {
+  uint32_t save;
+  const uintptr_t b = reinterpret_cast<uintptr_t>(base);
+  const uint64_t sb = (uint64_t)__builtin_amdgcn_readfirstlane((uint32_t)(b >> 32)) << 32 |
+                      (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)b);
+  asm volatile(
+      "s_mov_b32 %0, m0\n\ts_mov_b32 m0, %3\n\ts_nop 0\n\t"
+      "global_load_lds_dwordx4 %1, %2\n\t"
+      "global_load_lds_dwordx4 %1, %2 offset:1024\n\t"
+      "global_load_lds_dwordx4 %1, %2 offset:2048\n\t"
+      "global_load_lds_dwordx4 %1, %2 offset:3072\n\ts_nop 0\n\t"
+      "s_mov_b32 m0, %0"
+      : "=&s"(save)
+      : "v"(off), "s"(sb), "s"(__builtin_amdgcn_readfirstlane(lds_addr(l)))
+      : "memory");
+}
+
+// Every load and LDS access of the wave has ended.
+__device__ inline void wait_all() {
+  __builtin_amdgcn_s_waitcnt(0x0070);  // vmcnt 0, lgkmcnt 0
+  asm volatile("" ::: "memory");
+}
+
 __device__ inline float other_half(float x) { return __shfl_xor(x, 32); }
 
 // fp8 E4M3 -> bf16, eight codes (exact).
@@ -71,17 +95,28 @@ __device__ inline uint4 widen8(uint32_t w0, uint32_t w1) {
                     __builtin_bit_cast(uint32_t, c), __builtin_bit_cast(uint32_t, d));
 }
 
-// Keep the first nv of eight bf16 values.
-__device__ inline uint4 keep_first(uint4 x, int nv) {
-  x.x &= nv >= 2 ? 0xffffffffu : (nv == 1 ? 0xffffu : 0u);
-  x.y &= nv >= 4 ? 0xffffffffu : (nv == 3 ? 0xffffu : 0u);
-  x.z &= nv >= 6 ? 0xffffffffu : (nv == 5 ? 0xffffu : 0u);
-  x.w &= nv >= 8 ? 0xffffffffu : (nv == 7 ? 0xffffu : 0u);
-  return x;
-}
+// The helpers below work on pairs of bf16 and on single bits without
+// comparisons: a comparison's result takes two scalar registers, and a tile's
+// worth of them pushed the loop's own out of theirs.
 
-__device__ inline bool not_finite2(uint32_t x) {
-  return (x & 0x7f80u) == 0x7f80u || (x & 0x7f800000u) == 0x7f800000u;
+// Bit b of x as a mask, all ones or none.
+__device__ inline uint32_t bit_mask(uint32_t x, int b) { return (uint32_t)((int32_t)(x << (31 - b)) >> 31); }
+__device__ inline float select(uint32_t mask, float a, float b) {
+  return __uint_as_float((__float_as_uint(a) & mask) | (__float_as_uint(b) & ~mask));
+}
+// 0x8000 in each half that is not finite.
+__device__ inline uint32_t not_finite2(uint32_t x) { return ((x & 0x7f807f80u) + 0x00800080u) & 0x80008000u; }
+// 0x8000 flags -> 0xffff masks.
+__device__ inline uint32_t widen_flags(uint32_t f) { return (f << 1) - (f >> 15); }
+// Ones (bf16) in each half that is of the kind (0: +inf, 1: -inf, 2: NaN).
+__device__ inline uint32_t ones_of(uint32_t x, int kind) {
+  const uint32_t z = x ^ (kind ? 0xff80ff80u : 0x7f807f80u);
+  const uint32_t inf = ~(((z & 0x7fff7fffu) + 0x7fff7fffu) | z), nan = (x & 0x7fff7fffu) + 0x007f007fu;
+  return (((kind == 2 ? nan : inf) & 0x80008000u) >> 15) * 0x3f80u;
+}
+template <class F>
+__device__ inline uint4 each(uint4 x, F&& f) {
+  return make_uint4(f(x.x), f(x.y), f(x.z), f(x.w));
 }
 
 // The running state of a wave's 32 rows.  Lane (half h, row n): acc[db][r] is
@@ -91,63 +126,70 @@ struct Rows {
   f32x16 acc[4];
 };
 
-// One stage in LDS:
-//  K: [32-token half th][operand kb][d half][block of the two][row] 16 bytes
-//  V: [block][32 d][token half][d % 32] 16 bytes
-// so lane l's operand is at 16 l of each 1 KiB.
-struct KeyScales {
-  float k[4], v[4];  // of the tile's blocks (fp8)
+// Raw scores of a key tile: s[th][r] of lane (h, n) is row n's score of token
+// 32 th + 16 (r / 8) + 8 h + r % 8.
+struct Scores {
+  f32x16 s[2];
 };
 
-// One key tile for the wave's rows.  MASKED: bit t of `vis` says whether the
-// lane's row sees token t of the tile; tokens from nvalid on hold no values.
-template <bool FP8, bool HILO, bool MASKED>
-__device__ inline void key_tile(const uint8_t* stage, int lane, const bf16x8 (&q)[8], float c, const KeyScales& sc,
-                                uint64_t vis, int nvalid, Rows& st) {
-  const int h = lane >> 5;
-  const uint8_t* base = stage + lane * 16;
-  f32x16 s[2];
+// fp8: the scales of a tile's four blocks.
+struct KeyScales {
+  float k[4], v[4];
+};
+
+// The operands in LDS, the lane's 16 bytes.  K is the cache's own image of each
+// block ([d chunk][row]), every second block 128 bytes further, so that the
+// two blocks of a read use different banks; V is [block][32 d][token half][d].
+constexpr int kKBlock = kBlock * kHeadDim * 2;
+__host__ __device__ constexpr int k_block_at(int b) { return b * kKBlock + (b & 1) * 128 + (b >> 1) * 256; }
+__device__ inline int k_lane(int lane) {
+  return k_block_at((lane >> 4) & 1) + (lane >> 5) * 256 + (lane & 15) * 16;
+}
+__device__ inline bf16x8 k_operand(const uint8_t* k, int th, int kb) {
+  return *reinterpret_cast<const bf16x8*>(k + k_block_at(2 * th) + kb * 512);
+}
+__device__ inline bf16x8 v_operand(const uint8_t* v, int b, int db) {
+  return *reinterpret_cast<const bf16x8*>(v + (b * 4 + db) * 1024);
+}
+
+// S^T of the tile whose K is at `k`.
+__device__ inline void qk(const uint8_t* k, const bf16x8 (&q)[8], Scores& x) {
 #pragma unroll
-  for (int th = 0; th < 2; ++th) {
-    s[th] = f32x16{};
+  for (int th = 0; th < 2; ++th) x.s[th] = f32x16{};
 #pragma unroll
-    for (int kb = 0; kb < 8; ++kb)
-      s[th] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-          *reinterpret_cast<const bf16x8*>(base + (th * 8 + kb) * 1024), q[kb], s[th], 0, 0, 0);
+  for (int kb = 0; kb < 8; ++kb)
+#pragma unroll
+    for (int th = 0; th < 2; ++th)
+      x.s[th] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_operand(k, th, kb), q[kb], x.s[th], 0, 0, 0);
+}
+
+// Block b's factor of the raw scores (log2 units).
+template <bool FP8>
+__device__ inline float factor(float c, const KeyScales& sc, int b) {
+  return FP8 ? fmaxf(c * sc.k[b], 1e-37f) : c;
+}
+
+// The lane's largest score of the tile, scaled.
+template <bool FP8>
+__device__ inline float tile_max(const Scores& x, float c, const KeyScales& sc) {
+  float mb[4];
+#pragma unroll
+  for (int b = 0; b < 4; ++b) {
+    const f32x16& s = x.s[b / 2];
+    const int o = 8 * (b % 2);
+    mb[b] = max3(max3(max3(s[o], s[o + 1], s[o + 2]), s[o + 3], s[o + 4]), s[o + 5], s[o + 6]);
+    mb[b] = fmaxf(mb[b], s[o + 7]);
+    if constexpr (FP8) mb[b] *= factor<FP8>(c, sc, b);
   }
-  if constexpr (MASKED) {
-    const uint32_t v0 = (uint32_t)vis >> (8 * h), v1 = (uint32_t)(vis >> 32) >> (8 * h);
-#pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      const uint32_t bit = 1u << (16 * (r / 8) + r % 8);
-      s[0][r] = (v0 & bit) ? s[0][r] : -INFINITY;
-      s[1][r] = (v1 & bit) ? s[1][r] : -INFINITY;
-    }
-  }
-  float cb[4];
-#pragma unroll
-  for (int b = 0; b < 4; ++b) cb[b] = FP8 ? fmaxf(c * sc.k[b], 1e-37f) : c;
-  float mx;
-  if constexpr (FP8) {
-    float mb[4];
-#pragma unroll
-    for (int b = 0; b < 4; ++b) {
-      const f32x16& x = s[b / 2];
-      const int o = 8 * (b % 2);
-      mb[b] = max3(max3(x[o], x[o + 1], x[o + 2]), max3(x[o + 3], x[o + 4], x[o + 5]), x[o + 6]);
-      mb[b] = max3(mb[b], x[o + 7], x[o + 7]) * cb[b];
-    }
-    mx = max3(max3(mb[0], mb[1], mb[2]), mb[3], mb[3]);
-  } else {
-    mx = max3(s[0][0], s[0][1], s[1][0]);
-#pragma unroll
-    for (int r = 2; r < 16; r += 2) mx = max3(mx, s[0][r], s[0][r + 1]);
-#pragma unroll
-    for (int r = 1; r < 15; r += 2) mx = max3(mx, s[1][r], s[1][r + 1]);
-    mx = max3(mx, s[1][15], s[1][15]) * c;
-  }
+  const float mx = fmaxf(max3(mb[0], mb[1], mb[2]), mb[3]);
+  return FP8 ? mx : mx * c;
+}
+
+// Moves a row's reference when a score exceeds it by more than 2^kLazy; until
+// then the weights stay <= 2^kLazy and nothing is rescaled.
+__device__ inline void rescale(float mx, Rows& st) {
   if (__builtin_amdgcn_ballot_w64(mx > st.m + kLazy)) {
-    mx = max3(mx, other_half(mx), mx);
+    mx = fmaxf(mx, other_half(mx));
     const float m_new = mx > st.m + kLazy ? mx : st.m;
     const float alpha = m_new == st.m ? 1.f : __builtin_amdgcn_exp2f(st.m - m_new);
     st.l *= alpha;
@@ -155,111 +197,180 @@ __device__ inline void key_tile(const uint8_t* stage, int lane, const bf16x8 (&q
     for (int db = 0; db < 4; ++db) st.acc[db] *= alpha;
     st.m = m_new;
   }
-  const float nm = st.m == -INFINITY ? 0.f : -st.m;
-  uint4 ph[4], pl[4];
-  float l0 = 0.f, l1 = 0.f;
+}
+
+__device__ inline float reference(const Rows& st) { return st.m == -INFINITY ? 0.f : -st.m; }
+
+// Weights of tokens 2 j and 2 j + 1 of the lane's eight of block b as part of
+// the B operand of P.V: one bf16 plane, or (WIDE) three whose sum is the weight
+// to fp32's precision; their sum goes to l.
+template <bool FP8, bool WIDE>
+__device__ inline void weigh_pair(const Scores& x, int b, int j, float cb, float nm, float vs, float& l,
+                                  uint32_t (&p)[WIDE ? 3 : 1][4]) {
+  float u = __builtin_amdgcn_exp2f(fmaf(x.s[b / 2][8 * (b % 2) + 2 * j], cb, nm));
+  float v = __builtin_amdgcn_exp2f(fmaf(x.s[b / 2][8 * (b % 2) + 2 * j + 1], cb, nm));
+  if constexpr (FP8 || WIDE) l += u + v;
+  if constexpr (FP8) u *= vs, v *= vs;
+  p[0][j] = pack_bf16x2(u, v);
+  if constexpr (WIDE) {
 #pragma unroll
-  for (int b = 0; b < 4; ++b) {
-    uint32_t hw[4], lw[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      float x = __builtin_amdgcn_exp2f(fmaf(s[b / 2][8 * (b % 2) + 2 * j], cb[b], nm));
-      float y = __builtin_amdgcn_exp2f(fmaf(s[b / 2][8 * (b % 2) + 2 * j + 1], cb[b], nm));
-      if constexpr (FP8 || HILO) {
-        l0 += x;
-        l1 += y;
-      }
-      if constexpr (FP8) {
-        x *= sc.v[b];
-        y *= sc.v[b];
-      }
-      hw[j] = pack_bf16x2(x, y);
-      if constexpr (HILO)
-        lw[j] = pack_bf16x2(x - __uint_as_float(hw[j] << 16), y - __uint_as_float(hw[j] & 0xffff0000u));
-      if constexpr (!FP8 && !HILO)
-        l0 = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, hw[j]), bf16x2{(__bf16)1.f, (__bf16)1.f}, l0,
-                                             false);
+    for (int k = 1; k < 3; ++k) {  // the remainders are exact
+      u -= __uint_as_float(p[k - 1][j] << 16);
+      v -= __uint_as_float(p[k - 1][j] & 0xffff0000u);
+      p[k][j] = pack_bf16x2(u, v);
     }
-    ph[b] = make_uint4(hw[0], hw[1], hw[2], hw[3]);
-    if constexpr (HILO) pl[b] = make_uint4(lw[0], lw[1], lw[2], lw[3]);
   }
-  st.l += l0 + l1;
-  if constexpr (!MASKED) {
+  if constexpr (!FP8 && !WIDE)
+    l = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, p[0][j]), bf16x2{(__bf16)1.f, (__bf16)1.f}, l, false);
+}
+
+__device__ inline bf16x8 operand(const uint32_t (&p)[4]) {
+  return __builtin_bit_cast(bf16x8, make_uint4(p[0], p[1], p[2], p[3]));
+}
+
+// A tile that every row of the wave sees whole (scores x), and with it the
+// scores y of the next tile.  A wave issues in order and a matrix product
+// holds up only what needs its result, so the order is written out: between
+// two products the vector units make two tokens' weights (while Q.K of the
+// next tile runs) or a part of the next tile's maximum (while P.V runs), and
+// an operand is read from LDS kAhead products before it is used.
+template <bool FP8>
+__device__ inline void plain_tile(const uint8_t* v, const uint8_t* k_next, const bf16x8 (&q)[8], float c,
+                                  const KeyScales& sc, const KeyScales& sc_next, const Scores& x, Scores& y, float& mx,
+                                  Rows& st) {
+  constexpr int kAhead = 6;
+  const float nm = reference(st);
+  float cb[4], l[2] = {0.f, 0.f}, mb[4];
 #pragma unroll
-    for (int b = 0; b < 4; ++b)
+  for (int b = 0; b < 4; ++b) cb[b] = factor<FP8>(c, sc, b);
+  uint32_t p[4][1][4];
+  bf16x8 ring[kAhead];
+  auto load = [&](int n) { return n < 16 ? k_operand(k_next, n % 2, n / 2) : v_operand(v, (n - 16) / 4, n % 4); };
 #pragma unroll
-      for (int db = 0; db < 4; ++db) {
-        const bf16x8 v = *reinterpret_cast<const bf16x8*>(base + kVOff + (b * 4 + db) * 1024);
-        st.acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, __builtin_bit_cast(bf16x8, ph[b]), st.acc[db], 0, 0, 0);
-        if constexpr (HILO)
-          st.acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, __builtin_bit_cast(bf16x8, pl[b]), st.acc[db], 0, 0, 0);
+  for (int n = 0; n < kAhead; ++n) ring[n] = load(n);
+  __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+  for (int n = 0; n < 32; ++n) {
+    if (n < 16) {
+      y.s[n % 2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ring[n % kAhead], q[n / 2], n < 2 ? f32x16{} : y.s[n % 2], 0, 0, 0);
+      weigh_pair<FP8, false>(x, n / 4, n % 4, cb[n / 4], nm, sc.v[n / 4], l[n % 2], p[n / 4]);
+    } else {
+      const int m = n - 16;
+      st.acc[m % 4] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ring[n % kAhead], operand(p[m / 4][0]), st.acc[m % 4], 0, 0, 0);
+      if (m >= 4 && m < 12) {  // y's four blocks, four scores a time
+        const int b = (m - 4) / 2, o = 8 * (b % 2) + 4 * (m % 2);
+        const f32x16& s = y.s[b / 2];
+        mb[b] = m % 2 == 0 ? fmaxf(max3(s[o], s[o + 1], s[o + 2]), s[o + 3]) : max3(max3(mb[b], s[o], s[o + 1]), s[o + 2], s[o + 3]);
       }
-  } else {
-    // A value that some rows see may be infinite or NaN where other rows have
-    // P = 0, which the product would turn into NaN: such a block is added
-    // row by row, from the tokens that the row sees.
-#pragma unroll 1
-    for (int b = 0; b < 4; ++b) {
-      uint4 v[4];
-      bool bad = false;
-      const int nv = nvalid - 16 * b - 8 * h;
+    }
+    if (n + kAhead < 32) ring[n % kAhead] = load(n + kAhead);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  st.l += l[0] + l[1];
+  if constexpr (FP8) {
 #pragma unroll
-      for (int db = 0; db < 4; ++db) {
-        v[db] = keep_first(*reinterpret_cast<const uint4*>(base + kVOff + (b * 4 + db) * 1024), nv);
-        bad |= not_finite2(v[db].x) || not_finite2(v[db].y) || not_finite2(v[db].z) || not_finite2(v[db].w);
-      }
-      if (!__builtin_amdgcn_ballot_w64(bad)) {
+    for (int b = 0; b < 4; ++b) mb[b] *= factor<FP8>(c, sc_next, b);
+  }
+  mx = fmaxf(max3(mb[0], mb[1], mb[2]), mb[3]);
+  if constexpr (!FP8) mx *= c;
+}
+
+// Adds the values of one kind (0: +inf, 1: -inf, 2: NaN) in a block's V to the
+// rows that have a weight for them: the product of the weights with ones where
+// the values are.
+__device__ inline void add_not_finite(const uint4 (&v)[4], bf16x8 p, int kind, Rows& st) {
+  const uint32_t what = kind == 2 ? 0x7fc00000u : kind ? 0xff800000u : 0x7f800000u;
 #pragma unroll
-        for (int db = 0; db < 4; ++db) {
-          const bf16x8 x = __builtin_bit_cast(bf16x8, v[db]);
-          st.acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, __builtin_bit_cast(bf16x8, ph[0]), st.acc[db], 0, 0, 0);
-          if constexpr (HILO)
-            st.acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, __builtin_bit_cast(bf16x8, pl[0]), st.acc[db], 0, 0, 0);
-        }
-      } else {
-        uint4 w = ph[0], wl = HILO ? pl[0] : make_uint4(0, 0, 0, 0);
-#pragma unroll 1
-        for (int e = 0; e < 8; ++e) {
-          float p = __uint_as_float(w.x << 16);
-          if constexpr (HILO) p += __uint_as_float(wl.x << 16);
-          const float po = other_half(p);
-#pragma unroll 1
-          for (int t = 0; t < 2; ++t) {  // the token of the lane's own half, then the other half's
-            const int tok = 16 * b + 8 * (t ? 1 - h : h) + e;
-            const float pt = t ? po : p;
-            const bool sees = tok < nvalid && ((vis >> tok) & 1);
-            const uint8_t* col = stage + kVOff + b * 4096 + ((tok >> 3) & 1) * 512 + 2 * e;
+  for (int db = 0; db < 4; ++db) {
+    const uint4 a = each(v[db], [&](uint32_t x) { return ones_of(x, kind); });
+    const f32x16 n = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), p, f32x16{}, 0, 0, 0);
 #pragma unroll
-            for (int db = 0; db < 4; ++db)
-#pragma unroll
-              for (int r = 0; r < 16; ++r) {
-                const uint32_t x = *reinterpret_cast<const uint16_t*>(col + db * 1024 + (8 * (r / 4) + 4 * h + r % 4) * 16);
-                const float add = pt * __uint_as_float(x << 16);
-                st.acc[db][r] += sees ? add : 0.f;
-              }
-          }
-          w = make_uint4(w.x >> 16 | w.y << 16, w.y >> 16 | w.z << 16, w.z >> 16 | w.w << 16, w.w >> 16);
-          if constexpr (HILO)
-            wl = make_uint4(wl.x >> 16 | wl.y << 16, wl.y >> 16 | wl.z << 16, wl.z >> 16 | wl.w << 16, wl.w >> 16);
-        }
-      }
-      ph[0] = ph[1], ph[1] = ph[2], ph[2] = ph[3];
-      if constexpr (HILO) pl[0] = pl[1], pl[1] = pl[2], pl[2] = pl[3];
+    for (int r = 0; r < 16; ++r) {
+      uint32_t add = what & (uint32_t)(-__float_as_int(n[r]) >> 31);  // where the weights' sum is not zero
+      asm("" : "+v"(add));  // the source's arithmetic is compiled as if NaN did not occur
+      st.acc[db][r] += __uint_as_float(add);
     }
   }
 }
 
-// The drafts of a trace as a stage: tokens in rows there, so V is turned on
-// the way.  Tokens past the tree are zeros.
-__device__ inline void stage_drafts(const RowsLaunch& A, const RowItem& U, int Hkv, int kvh, int t, uint8_t* stage) {
+// Scores of tokens that the lane's row does not see (bits of `vis`) become -inf.
+__device__ inline void mask_scores(uint64_t vis, int lane, Scores& x) {
+  const uint32_t v0 = (uint32_t)vis >> (8 * (lane >> 5)), v1 = (uint32_t)(vis >> 32) >> (8 * (lane >> 5));
+#pragma unroll
+  for (int r = 0; r < 16; ++r) {
+    const int bit = 16 * (r / 8) + r % 8;
+    x.s[0][r] = select(bit_mask(v0, bit), x.s[0][r], -INFINITY);
+    x.s[1][r] = select(bit_mask(v1, bit), x.s[1][r], -INFINITY);
+  }
+}
+
+// A tile without one behind it (WIDE: any): the weights of a block are made
+// between the products of the block before.
+template <bool FP8, bool WIDE>
+__device__ inline void last_tile(const uint8_t* v, float c, const KeyScales& sc, const Scores& x, Rows& st) {
+  constexpr int kAhead = 6, kPlanes = WIDE ? 3 : 1;
+  const float nm = reference(st);
+  float l = 0.f;
+  uint32_t p[2][kPlanes][4];
+  bf16x8 ring[kAhead];
+#pragma unroll
+  for (int n = 0; n < kAhead; ++n) ring[n] = v_operand(v, n / 4, n % 4);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) weigh_pair<FP8, WIDE>(x, 0, j, factor<FP8>(c, sc, 0), nm, sc.v[0], l, p[0]);
+  __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+  for (int n = 0; n < 16; ++n) {
+    const int b = n / 4;
+#pragma unroll
+    for (int k = kPlanes - 1; k >= 0; --k)
+      st.acc[n % 4] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ring[n % kAhead], operand(p[b % 2][k]), st.acc[n % 4], 0, 0, 0);
+    if (b < 3) weigh_pair<FP8, WIDE>(x, b + 1, n % 4, factor<FP8>(c, sc, b + 1), nm, sc.v[b + 1], l, p[(b + 1) % 2]);
+    if (n + kAhead < 16) ring[n % kAhead] = v_operand(v, (n + kAhead) / 4, (n + kAhead) % 4);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  st.l += l;
+}
+
+// The same for a tile whose V holds infinities or NaN that not every row sees:
+// where a row's weight is zero the product would make them NaN, so they are
+// zeros in the product and go to the rows with a weight for them beside it.
+template <bool FP8, bool WIDE>
+__device__ inline void slow_tile(const uint8_t* vt, float c, const KeyScales& sc, const Scores& x, Rows& st) {
+  const float nm = reference(st);
+#pragma unroll
+  for (int b = 0; b < 4; ++b) {
+    uint32_t p[WIDE ? 3 : 1][4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) weigh_pair<FP8, WIDE>(x, b, j, factor<FP8>(c, sc, b), nm, sc.v[b], st.l, p);
+    uint4 v[4];
+#pragma unroll
+    for (int db = 0; db < 4; ++db) v[db] = __builtin_bit_cast(uint4, v_operand(vt, b, db));
+#pragma unroll 1
+    for (int kind = 0; kind < 3; ++kind) add_not_finite(v, operand(p[0]), kind, st);
+#pragma unroll
+    for (int db = 0; db < 4; ++db) {
+      v[db] = each(v[db], [](uint32_t y) { return y & ~widen_flags(not_finite2(y)); });
+#pragma unroll
+      for (int k = WIDE ? 2 : 0; k >= 0; --k)
+        st.acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v[db]), operand(p[k]), st.acc[db], 0, 0, 0);
+    }
+    __builtin_amdgcn_sched_barrier(0);  // one block's operands at a time
+  }
+}
+
+// The drafts of a trace as a key tile in LDS: tokens in rows there, so V is
+// turned on the way.  Tokens past the tree are zeros.  Returns whether the
+// thread's part of V holds infinities or NaN.
+__device__ inline uint32_t stage_drafts(const RowsLaunch& A, const RowItem& U, int Hkv, int kvh, int t, uint8_t* kst,
+                                        uint8_t* vst) {
+  uint32_t bad = 0;
 #pragma unroll
   for (int x = 0; x < 4; ++x) {
     const int u = t + x * kThreads, j = u >> 4, ch = u & 15;
     uint4 k = make_uint4(0, 0, 0, 0);
     if (j < U.ndraft)
       k = *reinterpret_cast<const uint4*>(A.k_new + ((size_t)(U.draft + j) * Hkv + kvh) * kHeadDim + 8 * ch);
-    *reinterpret_cast<uint4*>(stage + ((j >> 5) * 8 + (ch >> 1)) * 1024 + (ch & 1) * 512 + ((j >> 4) & 1) * 256 +
-                              k_phys(j & 15) * 16) = k;
+    *reinterpret_cast<uint4*>(kst + k_block_at(j >> 4) + ch * 256 + k_phys(j & 15) * 16) = k;
   }
 #pragma unroll
   for (int x = 0; x < 4; ++x) {
@@ -269,17 +380,23 @@ __device__ inline void stage_drafts(const RowsLaunch& A, const RowItem& U, int H
     for (int e = 0; e < 8; ++e)
       if (j0 + e < U.ndraft)
         w[e / 2] |= (uint32_t)A.v_new[((size_t)(U.draft + j0 + e) * Hkv + kvh) * kHeadDim + d] << (16 * (e % 2));
-    *reinterpret_cast<uint4*>(stage + kVOff + (j0 >> 4) * 4096 + (d >> 5) * 1024 + ((j0 >> 3) & 1) * 512 + (d & 31) * 16) =
+    *reinterpret_cast<uint4*>(vst + (j0 >> 4) * 4096 + (d >> 5) * 1024 + ((j0 >> 3) & 1) * 512 + (d & 31) * 16) =
         make_uint4(w[0], w[1], w[2], w[3]);
+    bad |= not_finite2(w[0]) | not_finite2(w[1]) | not_finite2(w[2]) | not_finite2(w[3]);
   }
+  return bad;
 }
 
-template <bool FP8, bool HILO, bool DRAFT>
+constexpr int kKTile = k_block_at(4), kVTile = kKeyTile * kHeadDim * 2;  // of a key tile in LDS
+
+template <bool FP8, bool WIDE, bool DRAFT>
 __global__ __launch_bounds__(kThreads, 2) void rows_attn_kernel(DevPool P, RowsLaunch A) {
-  __shared__ __attribute__((aligned(1024))) uint8_t lds[2 * kStage];
-  const int kvh = blockIdx.x % P.Hkv;
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[2 * kKTile + 2 * kVTile];
+  __shared__ uint32_t bad_s[2][4];  // by tile and wave: its block's V is not all finite
+  // the quotient in a scalar register, so that what it leads to is read by scalar loads
+  const int item = __builtin_amdgcn_readfirstlane(blockIdx.x / P.Hkv), kvh = blockIdx.x - item * P.Hkv;
   const RowItem U = __builtin_bit_cast(
-      RowItem, *reinterpret_cast<const GAMBIT_CONST i32x16*>(reinterpret_cast<uintptr_t>(A.items + blockIdx.x / P.Hkv)));
+      RowItem, *reinterpret_cast<const GAMBIT_CONST i32x16*>(reinterpret_cast<uintptr_t>(A.items + item)));
   const int t = threadIdx.x, lane = t & 63, w = __builtin_amdgcn_readfirstlane(t >> 6);
   const int h = lane >> 5, gs = A.gshift;
   const int nrows = U.ntok << gs, row = 32 * w + (lane & 31);
@@ -288,6 +405,87 @@ __global__ __launch_bounds__(kThreads, 2) void rows_attn_kernel(DevPool P, RowsL
   if (here) tok = U.listed ? A.list[U.tok + (row >> gs)] : U.tok + (row >> gs);
   const int head = (kvh << gs) + (row & ((1 << gs) - 1));
 
+  // positions the lane's row sees, and the fewest and most that a row of the wave does
+  const int t0 = kBlock * U.jb0;
+  auto limit = [&](int r) { return U.pos0 == kNoLimit ? U.end : min(U.end, U.pos0 + (r >> gs) + 1); };
+  const int lim = limit(min(row, nrows - 1));
+  const bool active = 32 * w < nrows;
+  const int lim_lo = limit(32 * w), lim_hi = limit(min(32 * w + 31, nrows - 1));
+  const int ntiles = U.end > t0 ? (U.end - t0 + kKeyTile - 1) / kKeyTile : 0;
+  // tiles of which the wave sees something
+  const int nt = active && lim_hi > t0 ? (lim_hi - t0 + kKeyTile - 1) / kKeyTile : 0;
+  const int jlast = (U.end - 1) / kBlock;
+  const int32_t* brow = P.table + (size_t)U.trace * P.max_blocks;
+  const size_t tile_bytes = (size_t)kBlock * kHeadDim * (FP8 ? 1 : 2);
+
+  // Wave w moves block w of a tile.  Its id is asked for a tile ahead of its
+  // bytes (fp8: all four ids, whose scales every wave needs).
+  auto id_of = [&](int i, int b) { return ld_const(brow + min(U.jb0 + 4 * i + b, jlast)); };
+  bool bad_id = false;
+  auto checked = [&](int id) {
+    const bool in = (unsigned)id < (unsigned)P.num_blocks;
+    bad_id |= !in;
+    return in ? id : 0;
+  };
+  auto block_at = [&](const uint8_t* cache, int id) { return cache + ((size_t)id * P.Hkv + kvh) * tile_bytes; };
+  auto kbuf = [&](int i) { return lds + (i & 1) * kKTile; };
+  auto vbuf = [&](int i) { return lds + 2 * kKTile + (i & 1) * kVTile; };
+  uint4 raw_k[2], raw_v[2];  // fp8: the codes on their way
+  auto ask_k = [&](int id, int i) {
+    const uint8_t* src = block_at(P.k_cache, id);
+    if constexpr (FP8) {
+      raw_k[0] = *reinterpret_cast<const uint4*>(src + lane * 16);
+      raw_k[1] = *reinterpret_cast<const uint4*>(src + lane * 16 + 1024);
+    } else {
+      dma16x4(src, lane * 16, kbuf(i) + k_block_at(w));
+    }
+  };
+  auto ask_v = [&](int id, int i) {
+    const uint8_t* src = block_at(P.v_cache, id);
+    if constexpr (FP8) {
+      raw_v[0] = *reinterpret_cast<const uint4*>(src + lane * 16);
+      raw_v[1] = *reinterpret_cast<const uint4*>(src + lane * 16 + 1024);
+    } else {
+      dma16x4(src, (2 * (lane & 31) + h) * 16, vbuf(i) + w * kKBlock);
+    }
+  };
+  auto widen_k = [&](int i) {  // 16 d of a row -> two chunks of 8
+#pragma unroll
+    for (int y = 0; y < 2; ++y) {
+      uint8_t* k = kbuf(i) + k_block_at(w) + (2 * (4 * y + (lane >> 4)) * kBlock + (lane & 15)) * 16;
+      *reinterpret_cast<uint4*>(k) = widen8(raw_k[y].x, raw_k[y].y);
+      *reinterpret_cast<uint4*>(k + kBlock * 16) = widen8(raw_k[y].z, raw_k[y].w);
+    }
+  };
+  auto widen_v = [&](int i) {  // 16 tokens of a d -> two halves
+#pragma unroll
+    for (int y = 0; y < 2; ++y) {
+      uint8_t* v = vbuf(i) + w * kKBlock + (2 * y + h) * 1024 + (lane & 31) * 16;
+      *reinterpret_cast<uint4*>(v) = widen8(raw_v[y].x, raw_v[y].y);
+      *reinterpret_cast<uint4*>(v + 512) = widen8(raw_v[y].z, raw_v[y].w);
+    }
+  };
+  auto scales = [&](int i) {
+    KeyScales s;
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+      s.k[b] = s.v[b] = 1.f;
+      if constexpr (FP8) {
+        const size_t id = checked(id_of(i, b));
+        s.k[b] = ld_const(P.kv_scale + 2 * id);
+        s.v[b] = ld_const(P.kv_scale + 2 * id + 1);
+      }
+    }
+    return s;
+  };
+
+  // the first loads: tile 0's K, then the queries, tile 0's V and tile 1's K
+  int id0 = 0, id1 = 0, id2 = 0;  // wave's blocks of tiles i, i + 1, i + 2 (past the end: the last block, unused)
+  if (ntiles > 0) {
+    id0 = checked(id_of(0, w));
+    id1 = checked(id_of(1, w));
+    ask_k(id0, 0);
+  }
   // the wave's queries, row n of lane (n, h): d = 16 kb + 8 h ..
   bf16x8 q[8];
 #pragma unroll
@@ -303,125 +501,144 @@ __global__ __launch_bounds__(kThreads, 2) void rows_attn_kernel(DevPool P, RowsL
   st.l = 0.f;
 #pragma unroll
   for (int db = 0; db < 4; ++db) st.acc[db] = f32x16{};
-
-  // positions the lane's row sees, and the fewest and most that a row of the wave does
-  const int t0 = kBlock * U.jb0;
-  auto limit = [&](int r) { return U.pos0 == kNoLimit ? U.end : min(U.end, U.pos0 + (r >> gs) + 1); };
-  const int lim = limit(min(row, nrows - 1));
-  const bool active = 32 * w < nrows;
-  const int lim_lo = limit(32 * w), lim_hi = limit(min(32 * w + 31, nrows - 1));
-  const int ntiles = U.end > t0 ? (U.end - t0 + kKeyTile - 1) / kKeyTile : 0;
-  const int jlast = (U.end - 1) / kBlock;
-  const int32_t* brow = P.table + (size_t)U.trace * P.max_blocks;
-  const size_t tile_bytes = (size_t)kBlock * kHeadDim * (FP8 ? 1 : 2);
-
-  int ids[4];        // blocks of the next tile to fetch
-  KeyScales sc_next, sc;
-  uint4 raw[4];      // fp8: the next tile on its way
-  auto fetch_ids = [&](int i) {
-#pragma unroll
-    for (int b = 0; b < 4; ++b) ids[b] = ld_const(brow + min(U.jb0 + 4 * i + b, jlast));
-  };
-  auto id_of = [&](int b) { return b == 0 ? ids[0] : b == 1 ? ids[1] : b == 2 ? ids[2] : ids[3]; };  // b uniform
-  auto tile_at = [&](const uint8_t* cache, int id) { return cache + ((size_t)id * P.Hkv + kvh) * tile_bytes; };
-  auto check_ids = [&]() {
-#pragma unroll
-    for (int b = 0; b < 4; ++b)
-      if ((unsigned)ids[b] >= (unsigned)P.num_blocks) {
-        if (t == 0) atomicOr(P.err, kErrBadBlock);
-        ids[b] = 0;
-      }
-  };
-  // asks for tile i (ids): bf16 straight into the stage, fp8 into registers
-  auto fetch = [&](uint8_t* stage) {
-    check_ids();
-    if constexpr (!FP8) {
-      const int th = w >> 1, kb0 = 4 * (w & 1);
-      const uint8_t* k = tile_at(P.k_cache, (lane & 16) ? id_of(2 * th + 1) : id_of(2 * th)) +
-                         ((2 * kb0 + h) * kBlock + (lane & 15)) * 16;
-      const uint8_t* v = tile_at(P.v_cache, id_of(w)) + (2 * (lane & 31) + h) * 16;
-#pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        dma16(k + x * 512, stage + (th * 8 + kb0 + x) * 1024);
-        dma16(v + x * 1024, stage + kVOff + (w * 4 + x) * 1024);
-      }
-    } else {
-      const int b = w >> 1, u = (t & 127) * 16;
-      raw[0] = *reinterpret_cast<const uint4*>(tile_at(P.k_cache, id_of(b)) + u);
-      raw[1] = *reinterpret_cast<const uint4*>(tile_at(P.k_cache, id_of(b + 2)) + u);
-      raw[2] = *reinterpret_cast<const uint4*>(tile_at(P.v_cache, id_of(b)) + u);
-      raw[3] = *reinterpret_cast<const uint4*>(tile_at(P.v_cache, id_of(b + 2)) + u);
-#pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        sc_next.k[x] = ld_const(P.kv_scale + 2 * ids[x]);
-        sc_next.v[x] = ld_const(P.kv_scale + 2 * ids[x] + 1);
-      }
-    }
-  };
-  // fp8: the fetched tile widened into the stage
-  auto settle = [&](uint8_t* stage) {
-    if constexpr (FP8) {
-      const int b = w >> 1, x = t & 127;
-#pragma unroll
-      for (int y = 0; y < 2; ++y) {  // blocks b and b + 2
-        uint8_t* k = stage + (y * 8 + (x >> 4)) * 1024 + b * 256 + (x & 15) * 16;
-        *reinterpret_cast<uint4*>(k) = widen8(raw[y].x, raw[y].y);
-        *reinterpret_cast<uint4*>(k + 512) = widen8(raw[y].z, raw[y].w);
-        uint8_t* v = stage + kVOff + (b + 2 * y) * 4096 + (x >> 5) * 1024 + (x & 31) * 16;
-        *reinterpret_cast<uint4*>(v) = widen8(raw[2 + y].x, raw[2 + y].y);
-        *reinterpret_cast<uint4*>(v + 512) = widen8(raw[2 + y].z, raw[2 + y].w);
-      }
-      sc = sc_next;
-    }
-  };
-
+  Scores x, y;
+  float mx = -INFINITY;
+  KeyScales sc{}, sc1{};
   if (ntiles > 0) {
-    fetch_ids(0);
-    fetch(lds);
-    if (ntiles > 1) fetch_ids(1);
-    settle(lds);
+    if constexpr (FP8) widen_k(0);
+    wait_all();
+    barrier_no_fence();
+    ask_v(id0, 0);
+    if (ntiles > 1) ask_k(id1, 1);
+    id2 = id_of(2, w);
+    sc = scales(0);
+    sc1 = scales(1);
+    if (nt > 0) {
+      qk(kbuf(0) + k_lane(lane), q, x);
+      mx = tile_max<FP8>(x, A.c, sc);
+    }
+    if constexpr (FP8) {
+      widen_v(0);
+      if (ntiles > 1) widen_k(1);
+    }
+  }
+  // A tile that ends the range, or that not every row of the workgroup sees
+  // whole: its tokens past the end hold anything, and become zeros in V (their
+  // weights are zero); bad_s says whether the others hold infinities or NaN.
+  const int lim_wg = limit(0);
+  auto clean_v = [&](int i) {
+    uint8_t* v = vbuf(i) + w * kKBlock + lane * 16;
+    const int n = min(max(U.end - (t0 + kKeyTile * i + kBlock * w + 8 * h), 0), 8);
+    const uint32_t there = (1u << n) - 1;
+    const uint4 keep = make_uint4((bit_mask(there, 0) & 0xffffu) | (bit_mask(there, 1) & 0xffff0000u),
+                                  (bit_mask(there, 2) & 0xffffu) | (bit_mask(there, 3) & 0xffff0000u),
+                                  (bit_mask(there, 4) & 0xffffu) | (bit_mask(there, 5) & 0xffff0000u),
+                                  (bit_mask(there, 6) & 0xffffu) | (bit_mask(there, 7) & 0xffff0000u));
+    uint32_t bad = 0;
+#pragma unroll
+    for (int db = 0; db < 4; ++db) {
+      uint4* at = reinterpret_cast<uint4*>(v + db * 1024);
+      const uint4 x = *at, y = make_uint4(x.x & keep.x, x.y & keep.y, x.z & keep.z, x.w & keep.w);
+      bad |= not_finite2(y.x) | not_finite2(y.y) | not_finite2(y.z) | not_finite2(y.w);
+      *at = y;
+    }
+    const uint64_t any = __builtin_amdgcn_ballot_w64(bad != 0);
+    if (lane == 0) bad_s[i & 1][w] = any != 0;
+  };
+  auto is_bad = [&](int i) {
+    return __builtin_amdgcn_readfirstlane(bad_s[i & 1][0] | bad_s[i & 1][1] | bad_s[i & 1][2] | bad_s[i & 1][3]) != 0;
+  };
+  // Start of tile i: its V and the K of tile i + 1 are there in every wave, and
+  // no wave reads its K or the V of tile i - 1 any more; the next ones are asked for.
+  auto begin = [&](int i) {
+    wait_all();
+    barrier_no_fence();
+    id2 = checked(id2);
+    if (i + 2 < ntiles) ask_k(id2, i);
+    if (i + 1 < ntiles) ask_v(id1, i + 1);
+    id1 = id2;
+    id2 = id_of(i + 3, w);
+  };
+  auto end = [&](int i) {
+    if constexpr (FP8) {
+      if (i + 2 < ntiles) widen_k(i);
+      if (i + 1 < ntiles) widen_v(i + 1);
+    }
+    sc = sc1;
+    sc1 = scales(i + 2);
+  };
+  auto plain = [&](int i, const Scores& a, Scores& b) {
+    rescale(mx, st);
+    plain_tile<FP8>(vbuf(i) + lane * 16, kbuf(i + 1) + k_lane(lane), q, A.c, sc, sc1, a, b, mx, st);
+  };
+  int i = 0;
+  if constexpr (!WIDE) {
+    // tiles that every row of the workgroup sees whole, before the wave's last
+    const int np = min(lim_wg > t0 ? (lim_wg - t0) / kKeyTile : 0, nt - 1);
+#pragma unroll 1
+    for (; i + 1 < np; i += 2) {
+      begin(i);
+      plain(i, x, y);
+      end(i);
+      begin(i + 1);
+      plain(i + 1, y, x);
+      end(i + 1);
+    }
   }
 #pragma unroll 1
-  for (int i = 0; i < ntiles; ++i) {
-    uint8_t* stage = lds + (i & 1) * kStage;
-    // the tile is there in every wave, and no wave reads the other stage any more
-    if constexpr (FP8)
-      __syncthreads();
-    else {
-      __builtin_amdgcn_s_waitcnt(0x0070);  // vmcnt 0, lgkmcnt 0
-      barrier_no_fence();
-    }
-    const KeyScales now = sc;
-    if (i + 1 < ntiles) {
-      fetch(lds + ((i + 1) & 1) * kStage);
-      if (i + 2 < ntiles) fetch_ids(i + 2);
-    }
+  for (; i < ntiles; ++i) {
     const int tb = t0 + kKeyTile * i;
-    if (active && tb < lim_hi) {
-      if (tb + kKeyTile <= lim_lo) {
-        key_tile<FP8, HILO, false>(stage, lane, q, A.c, now, 0, kKeyTile, st);
+    const bool check = tb + kKeyTile > lim_wg;  // uniform over the workgroup
+    if (check) {
+      wait_all();
+      clean_v(i);
+    }
+    begin(i);
+    if (i < nt) {
+      if (tb + kKeyTile > lim_lo) {
+        mask_scores(lim - tb <= 0 ? 0 : ~0ull >> (64 - min(lim - tb, 64)), lane, x);
+        mx = tile_max<FP8>(x, A.c, sc);
+      }
+      const bool more = i + 1 < nt;
+      if (check && is_bad(i)) {
+        rescale(mx, st);
+        slow_tile<FP8, WIDE>(vbuf(i) + lane * 16, A.c, sc, x, st);
+      } else if (!WIDE && more) {
+        if constexpr (!WIDE) plain(i, x, y);
+        x = y;
       } else {
-        const int k = min(max(lim - tb, 0), kKeyTile);
-        const uint64_t vis = k >= 64 ? ~0ull : (1ull << k) - 1;
-        key_tile<FP8, HILO, true>(stage, lane, q, A.c, now, vis, U.end - tb, st);
+        rescale(mx, st);
+        last_tile<FP8, WIDE>(vbuf(i) + lane * 16, A.c, sc, x, st);
+      }
+      if (more && (WIDE || (check && is_bad(i)))) {
+        qk(kbuf(i + 1) + k_lane(lane), q, x);
+        mx = tile_max<FP8>(x, A.c, sc1);
       }
     }
-    if (i + 1 < ntiles) settle(lds + ((i + 1) & 1) * kStage);
+    end(i);
   }
   if constexpr (DRAFT) {
     if (U.draft >= 0) {  // uniform
       __syncthreads();   // the last tile is read
-      stage_drafts(A, U, P.Hkv, kvh, t, lds);
+      const uint32_t bad = stage_drafts(A, U, P.Hkv, kvh, t, kbuf(0), vbuf(0));
+      const uint64_t any = __builtin_amdgcn_ballot_w64(bad != 0);
+      if (lane == 0) bad_s[0][w] = any != 0;
       __syncthreads();
       if (active) {
         KeyScales one;
 #pragma unroll
         for (int b = 0; b < 4; ++b) one.k[b] = one.v[b] = 1.f;
-        const uint64_t vis = here ? A.anc[tok] : 1;
-        key_tile<FP8, HILO, true>(lds, lane, q, A.c, one, vis, kKeyTile, st);
+        qk(kbuf(0) + k_lane(lane), q, x);
+        mask_scores(here ? A.anc[tok] : 1, lane, x);
+        rescale(tile_max<FP8>(x, A.c, one), st);
+        if (is_bad(0))
+          slow_tile<FP8, WIDE>(vbuf(0) + lane * 16, A.c, one, x, st);
+        else
+          last_tile<FP8, WIDE>(vbuf(0) + lane * 16, A.c, one, x, st);
       }
     }
   }
+  if (bad_id && lane == 0) atomicOr(P.err, kErrBadBlock);
   const float l = st.l + other_half(st.l);
   if (!here) return;
   if (U.kidx < 0) {
@@ -434,7 +651,7 @@ __global__ __launch_bounds__(kThreads, 2) void rows_attn_kernel(DevPool P, RowsL
         const f32x4 x = {st.acc[db][4 * j] * inv, st.acc[db][4 * j + 1] * inv, st.acc[db][4 * j + 2] * inv,
                          st.acc[db][4 * j + 3] * inv};
         const size_t at = o + 32 * db + 8 * j;
-        if constexpr (HILO)
+        if constexpr (WIDE)
           *reinterpret_cast<f32x4*>(static_cast<float*>(A.out) + at) = x;
         else
           *reinterpret_cast<uint2*>(static_cast<uint16_t*>(A.out) + at) =
@@ -484,24 +701,24 @@ __global__ __launch_bounds__(256) void rows_merge_kernel(RowsLaunch A, int32_t H
         make_uint2(pack_bf16x2(o[0] * inv, o[1] * inv), pack_bf16x2(o[2] * inv, o[3] * inv));
 }
 
-template <bool FP8, bool HILO>
+template <bool FP8, bool WIDE>
 void launch_items(const DevPool& P, const RowsLaunch& L, hipStream_t s) {
   const dim3 grid((unsigned)L.n_items * P.Hkv);
   if (L.anc)
-    hipLaunchKernelGGL((rows_attn_kernel<FP8, HILO, true>), grid, dim3(kThreads), 0, s, P, L);
+    hipLaunchKernelGGL((rows_attn_kernel<FP8, WIDE, true>), grid, dim3(kThreads), 0, s, P, L);
   else
-    hipLaunchKernelGGL((rows_attn_kernel<FP8, HILO, false>), grid, dim3(kThreads), 0, s, P, L);
+    hipLaunchKernelGGL((rows_attn_kernel<FP8, WIDE, false>), grid, dim3(kThreads), 0, s, P, L);
 }
 
 }  // namespace
 
 hipError_t launch_rows_attention(const DevPool& P, const RowsLaunch& L, hipStream_t s) {
   if (L.n_items <= 0) return hipSuccess;
-  const bool fp8 = P.esize == 1, hilo = L.out_f32;
-  if (fp8 && hilo) launch_items<true, true>(P, L, s);
-  if (fp8 && !hilo) launch_items<true, false>(P, L, s);
-  if (!fp8 && hilo) launch_items<false, true>(P, L, s);
-  if (!fp8 && !hilo) launch_items<false, false>(P, L, s);
+  const bool fp8 = P.esize == 1, wide = L.out_f32;
+  if (fp8 && wide) launch_items<true, true>(P, L, s);
+  if (fp8 && !wide) launch_items<true, false>(P, L, s);
+  if (!fp8 && wide) launch_items<false, true>(P, L, s);
+  if (!fp8 && !wide) launch_items<false, false>(P, L, s);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || L.n_merge == 0) return e;
   hipLaunchKernelGGL(rows_merge_kernel, dim3(((unsigned)L.n_merge * P.Hq + 7) / 8), dim3(256), 0, s, L, P.Hq);
