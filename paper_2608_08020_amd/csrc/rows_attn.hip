@@ -387,6 +387,7 @@ __device__ inline uint32_t stage_drafts(const RowsLaunch& A, const RowItem& U, i
   return bad;
 }
 
+constexpr int kRowBytes = kHeadDim * 2;  // of a query
 constexpr int kKTile = k_block_at(4), kVTile = kKeyTile * kHeadDim * 2;  // of a key tile in LDS
 
 template <bool FP8, bool WIDE, bool DRAFT>
@@ -486,15 +487,24 @@ __global__ __launch_bounds__(kThreads, 2) void rows_attn_kernel(DevPool P, RowsL
     id1 = checked(id_of(1, w));
     ask_k(id0, 0);
   }
-  // the wave's queries, row n of lane (n, h): d = 16 kb + 8 h ..
+  // The wave's queries by way of LDS (V's place), so that whole rows are read:
+  // row r's 16-byte chunk c at place c ^ (r % 16).
+  uint8_t* mine = lds + 2 * kKTile + w * 32 * kRowBytes;
+  if (active) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const int r = 4 * k + (lane >> 4);
+      const int rt = __shfl(tok, r), rh = (kvh << gs) + (r & ((1 << gs) - 1));  // 32 rows: a whole number of groups
+      const size_t at = 32 * w + r < nrows ? (size_t)rt * P.Hq + rh : (size_t)__shfl(tok, 0) * P.Hq + (kvh << gs);
+      dma16(A.q + at * kHeadDim + 8 * ((lane & 15) ^ (r & 15)), mine + k * 1024);
+    }
+  }
+  wait_all();
   bf16x8 q[8];
 #pragma unroll
   for (int kb = 0; kb < 8; ++kb) {
-    uint4 x = make_uint4(0, 0, 0, 0);
-    if (here) x = *reinterpret_cast<const uint4*>(A.q + ((size_t)tok * P.Hq + head) * kHeadDim + 16 * kb + 8 * h);
-    x.x = (x.x & A.q_and) ^ A.q_xor, x.y = (x.y & A.q_and) ^ A.q_xor;
-    x.z = (x.z & A.q_and) ^ A.q_xor, x.w = (x.w & A.q_and) ^ A.q_xor;
-    q[kb] = __builtin_bit_cast(bf16x8, x);
+    uint4 x = *reinterpret_cast<const uint4*>(mine + (lane & 31) * kRowBytes + (((2 * kb + h) ^ (lane & 15)) * 16));
+    q[kb] = __builtin_bit_cast(bf16x8, each(x, [&](uint32_t y) { return (y & A.q_and) ^ A.q_xor; }));
   }
   Rows st;
   st.m = -INFINITY;
@@ -640,34 +650,48 @@ __global__ __launch_bounds__(kThreads, 2) void rows_attn_kernel(DevPool P, RowsL
   }
   if (bad_id && lane == 0) atomicOr(P.err, kErrBadBlock);
   const float l = st.l + other_half(st.l);
-  if (!here) return;
-  if (U.kidx < 0) {
-    const float inv = 1.f / l;
-    const size_t o = ((size_t)tok * P.Hq + head) * kHeadDim + 4 * h;
+  size_t at = 0;  // the row's place in the output or among the partials
+  if (here) at = (U.kidx >= 0 ? (size_t)(A.off[tok] + U.kidx) : (size_t)tok) * P.Hq + head;
+  if (U.kidx >= 0) {  // uniform
+    if (!here) return;
+    float* dst = A.part_acc + at * kHeadDim + 4 * h;
 #pragma unroll
     for (int db = 0; db < 4; ++db)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const f32x4 x = {st.acc[db][4 * j] * inv, st.acc[db][4 * j + 1] * inv, st.acc[db][4 * j + 2] * inv,
-                         st.acc[db][4 * j + 3] * inv};
-        const size_t at = o + 32 * db + 8 * j;
-        if constexpr (WIDE)
-          *reinterpret_cast<f32x4*>(static_cast<float*>(A.out) + at) = x;
-        else
-          *reinterpret_cast<uint2*>(static_cast<uint16_t*>(A.out) + at) =
-              make_uint2(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]));
-      }
+      for (int j = 0; j < 4; ++j)
+        *reinterpret_cast<f32x4*>(dst + 32 * db + 8 * j) =
+            f32x4{st.acc[db][4 * j], st.acc[db][4 * j + 1], st.acc[db][4 * j + 2], st.acc[db][4 * j + 3]};
+    if (h == 0) A.part_ml[at] = float2{st.m, l};
     return;
   }
-  const size_t part = (size_t)(A.off[tok] + U.kidx) * P.Hq + head;
-  float* dst = A.part_acc + part * kHeadDim + 4 * h;
+  // Outputs leave by way of LDS, whole rows at a time: a row's 16-byte chunk c
+  // at place c ^ (row % 16), a wave's rows in its own part.
+  const float inv = 1.f / l;
+  __syncthreads();  // no wave reads K or V any more
+  if (!active) return;
+  constexpr int kLanes = WIDE ? 32 : 16, kPer = 64 / kLanes;  // lanes a row, rows an instruction stores
+  uint8_t* rows = lds + w * 32 * 16 * kLanes;
+  const int n = lane & 31;
 #pragma unroll
   for (int db = 0; db < 4; ++db)
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-      *reinterpret_cast<f32x4*>(dst + 32 * db + 8 * j) =
-          f32x4{st.acc[db][4 * j], st.acc[db][4 * j + 1], st.acc[db][4 * j + 2], st.acc[db][4 * j + 3]};
-  if (h == 0) A.part_ml[part] = float2{st.m, l};
+    for (int j = 0; j < 4; ++j) {
+      const f32x4 v = {st.acc[db][4 * j] * inv, st.acc[db][4 * j + 1] * inv, st.acc[db][4 * j + 2] * inv,
+                       st.acc[db][4 * j + 3] * inv};
+      if constexpr (WIDE)
+        *reinterpret_cast<f32x4*>(rows + n * 512 + ((8 * db + 2 * j + h) ^ n) * 16) = v;
+      else
+        *reinterpret_cast<uint2*>(rows + n * 256 + ((4 * db + j) ^ (n & 15)) * 16 + 8 * h) =
+            make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+    }
+  wait_all();
+#pragma unroll
+  for (int k = 0; k < 32 / kPer; ++k) {
+    const int r = k * kPer + lane / kLanes, c = lane % kLanes;
+    const uint4 v = *reinterpret_cast<const uint4*>(rows + (r * kLanes + (c ^ (r % kLanes))) * 16);
+    const size_t to = (size_t)__shfl((uint32_t)(at >> 32), r) << 32 | (uint32_t)__shfl((uint32_t)at, r);
+    if (32 * w + r < nrows) reinterpret_cast<uint4*>(A.out)[to * kLanes + c] = v;
+  }
 }
 
 // out = sum_k 2^(m_k - M) acc_k / sum_k 2^(m_k - M) l_k, M the largest m_k;
