@@ -28,7 +28,8 @@ struct RowItem {
   int32_t kidx;    // partial of these rows; -1: the whole result, written to `out`
   int32_t draft;   // first packed token of the trace's tree, -1: none
   int32_t ndraft;  // its tokens
-  int32_t pad[6];
+  int32_t once;    // 1: no other item reads the range's blocks
+  int32_t pad[5];
 };
 static_assert(sizeof(RowItem) == 64, "one scalar load");
 

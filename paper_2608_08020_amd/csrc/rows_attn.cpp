@@ -113,7 +113,7 @@ struct Plan {
 // partial rows cost more than its keys.
 constexpr int kLeastChunk = 256;
 // Workgroups a call is cut into, as a multiple of those the chip runs at once.
-constexpr double kRounds = 2.0;
+constexpr double kRounds = 1.0;
 
 struct Run {
   int j0, j1;                    // blocks
@@ -220,6 +220,7 @@ bool try_plan(gambit_pool* p, const std::vector<Listed>& L, const std::vector<Ru
       it.pos0 = tree ? gambit::kNoLimit : x.ctx + a;
       it.draft = tree ? x.base : -1;
       it.ndraft = tree ? x.m : 0;
+      it.once = x.m <= tile;
       chunked(it, x.priv, end, nch, nk > 1 ? before[i] : -1);
     }
   }
@@ -240,6 +241,7 @@ bool try_plan(gambit_pool* p, const std::vector<Listed>& L, const std::vector<Ru
       it.listed = 1;
       it.pos0 = gambit::kNoLimit;
       it.draft = -1;
+      it.once = (int)toks.size() <= tile;
       chunked(it, R.j0, 16 * R.j1, run_chunks[r], run_kidx[r][0]);
     }
   }

@@ -59,22 +59,36 @@ __device__ inline float max3(float a, float b, float c) { return fmaxf(fmaxf(a, 
 
 // Four direct loads of 1 KiB each, 16 bytes a lane: from base + off + 1024 k
 // (base uniform, off the lane's) into LDS at l + 1024 k + 16 x lane.  An
-// instruction's offset counts for both sides.
-__device__ inline void dma16x4(const uint8_t* base, uint32_t off, uint8_t* l) {
+// instruction's offset counts for both sides.  `once`: nobody else reads these
+// bytes (non-temporal hint).
+__device__ inline void dma16x4(const uint8_t* base, uint32_t off, uint8_t* l, bool once) {
   uint32_t save;
   const uintptr_t b = reinterpret_cast<uintptr_t>(base);
   const uint64_t sb = (uint64_t)__builtin_amdgcn_readfirstlane((uint32_t)(b >> 32)) << 32 |
                       (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)b);
-  asm volatile(
-      "s_mov_b32 %0, m0\n\ts_mov_b32 m0, %3\n\ts_nop 0\n\t"
-      "global_load_lds_dwordx4 %1, %2\n\t"
-      "global_load_lds_dwordx4 %1, %2 offset:1024\n\t"
-      "global_load_lds_dwordx4 %1, %2 offset:2048\n\t"
-      "global_load_lds_dwordx4 %1, %2 offset:3072\n\ts_nop 0\n\t"
-      "s_mov_b32 m0, %0"
-      : "=&s"(save)
-      : "v"(off), "s"(sb), "s"(__builtin_amdgcn_readfirstlane(lds_addr(l)))
-      : "memory");
+  const uint32_t at = __builtin_amdgcn_readfirstlane(lds_addr(l));
+#define GAMBIT_DMA16X4(hint)                                     \
+  asm volatile(                                                  \
+      "s_mov_b32 %0, m0\n\ts_mov_b32 m0, %3\n\ts_nop 0\n\t"     \
+      "global_load_lds_dwordx4 %1, %2" hint "\n\t"               \
+      "global_load_lds_dwordx4 %1, %2 offset:1024" hint "\n\t"   \
+      "global_load_lds_dwordx4 %1, %2 offset:2048" hint "\n\t"   \
+      "global_load_lds_dwordx4 %1, %2 offset:3072" hint "\n\t"   \
+      "s_nop 0\n\ts_mov_b32 m0, %0"                              \
+      : "=&s"(save)                                              \
+      : "v"(off), "s"(sb), "s"(at)                               \
+      : "memory")
+  if (once)
+    GAMBIT_DMA16X4(" nt");
+  else
+    GAMBIT_DMA16X4("");
+#undef GAMBIT_DMA16X4
+}
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+__device__ inline uint4 load16(const uint8_t* p, bool once) {
+  const u32x4* x = reinterpret_cast<const u32x4*>(p);
+  return __builtin_bit_cast(uint4, once ? __builtin_nontemporal_load(x) : *x);
 }
 
 // Every load and LDS access of the wave has ended.
@@ -435,19 +449,19 @@ __global__ __launch_bounds__(kThreads, 2) void rows_attn_kernel(DevPool P, RowsL
   auto ask_k = [&](int id, int i) {
     const uint8_t* src = block_at(P.k_cache, id);
     if constexpr (FP8) {
-      raw_k[0] = *reinterpret_cast<const uint4*>(src + lane * 16);
-      raw_k[1] = *reinterpret_cast<const uint4*>(src + lane * 16 + 1024);
+      raw_k[0] = load16(src + lane * 16, U.once);
+      raw_k[1] = load16(src + lane * 16 + 1024, U.once);
     } else {
-      dma16x4(src, lane * 16, kbuf(i) + k_block_at(w));
+      dma16x4(src, lane * 16, kbuf(i) + k_block_at(w), U.once);
     }
   };
   auto ask_v = [&](int id, int i) {
     const uint8_t* src = block_at(P.v_cache, id);
     if constexpr (FP8) {
-      raw_v[0] = *reinterpret_cast<const uint4*>(src + lane * 16);
-      raw_v[1] = *reinterpret_cast<const uint4*>(src + lane * 16 + 1024);
+      raw_v[0] = load16(src + lane * 16, U.once);
+      raw_v[1] = load16(src + lane * 16 + 1024, U.once);
     } else {
-      dma16x4(src, (2 * (lane & 31) + h) * 16, vbuf(i) + w * kKBlock);
+      dma16x4(src, (2 * (lane & 31) + h) * 16, vbuf(i) + w * kKBlock, U.once);
     }
   };
   auto widen_k = [&](int i) {  // 16 d of a row -> two chunks of 8
@@ -695,26 +709,46 @@ __global__ __launch_bounds__(kThreads, 2) void rows_attn_kernel(DevPool P, RowsL
 }
 
 // out = sum_k 2^(m_k - M) acc_k / sum_k 2^(m_k - M) l_k, M the largest m_k;
-// eight rows a workgroup, 32 lanes of four d a row.  A partial without a seen
-// position has m = -inf and counts for nothing.
+// eight rows a workgroup, a half-wave a row, four d a lane.  Each lane takes the
+// factors of every 32nd partial, four partials' rows are asked for at a time.
+// A partial without a seen position has m = -inf and counts for nothing.
 __global__ __launch_bounds__(256) void rows_merge_kernel(RowsLaunch A, int32_t Hq) {
   const int r = blockIdx.x * 8 + (threadIdx.x >> 5), x = threadIdx.x & 31;
   if (r >= A.n_merge * Hq) return;
   const int tok = A.merge[r / Hq], head = r % Hq;
   const int n = A.nk[tok];
   const size_t p0 = (size_t)A.off[tok] * Hq + head;
-  float M = -INFINITY;
-  for (int k = 0; k < n; ++k) M = fmaxf(M, A.part_ml[p0 + (size_t)k * Hq].x);
+  float M = -INFINITY, l = 0.f;
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
-  float l = 0.f;
-  for (int k = 0; k < n; ++k) {
-    const size_t p = p0 + (size_t)k * Hq;
-    const float2 ml = A.part_ml[p];
-    const f32x4 a = *reinterpret_cast<const f32x4*>(A.part_acc + p * kHeadDim + 4 * x);
+  for (int k0 = 0; k0 < n; k0 += 32) {
+    const float2 ml = k0 + x < n ? A.part_ml[p0 + (size_t)(k0 + x) * Hq] : float2{-INFINITY, 0.f};
+    float most = fmaxf(M, ml.x);
+#pragma unroll
+    for (int s = 16; s; s >>= 1) most = fmaxf(most, __shfl_xor(most, s));
+    if (most != M) {  // uniform over the half-wave
+      const float f = M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(M - most);
+      l *= f;
+      o *= f;
+      M = most;
+    }
     const float f = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - M);
-    l = fmaf(f, ml.y, l);
-    if (f != 0.f)
-      for (int e = 0; e < 4; ++e) o[e] = fmaf(f, a[e], o[e]);
+    float sum = f * ml.y;
+#pragma unroll
+    for (int s = 16; s; s >>= 1) sum += __shfl_xor(sum, s);
+    l += sum;
+    const int m = min(32, n - k0);
+    for (int k = 0; k < m; k += 4) {
+      f32x4 a[4];
+#pragma unroll
+      for (int y = 0; y < 4; ++y)
+        a[y] = *reinterpret_cast<const f32x4*>(A.part_acc + (p0 + (size_t)(k0 + min(k + y, m - 1)) * Hq) * kHeadDim + 4 * x);
+#pragma unroll
+      for (int y = 0; y < 4; ++y) {
+        const float g = k + y < m ? __shfl(f, (threadIdx.x & 32) + k + y) : 0.f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] = g == 0.f ? o[e] : fmaf(g, a[y][e], o[e]);
+      }
+    }
   }
   const float inv = 1.f / l;
   const size_t at = ((size_t)tok * Hq + head) * kHeadDim + 4 * x;
