@@ -146,9 +146,9 @@ struct Scores {
   f32x16 s[2];
 };
 
-// fp8: the scales of a tile's four blocks.
+// fp8: the scales of a tile's four blocks; of V's also log2 and reciprocal.
 struct KeyScales {
-  float k[4], v[4];
+  float k[4], v[4], log_v[4], inv_v[4];
 };
 
 // The operands in LDS, the lane's 16 bytes.  K is the cache's own image of each
@@ -217,14 +217,18 @@ __device__ inline float reference(const Rows& st) { return st.m == -INFINITY ? 0
 
 // Weights of tokens 2 j and 2 j + 1 of the lane's eight of block b as part of
 // the B operand of P.V: one bf16 plane, or (WIDE) three whose sum is the weight
-// to fp32's precision; their sum goes to l.
+// to fp32's precision; their sum goes to l.  fp8: the operand holds the weight
+// times the block's V scale - in one plane by way of the exponent (nm includes
+// log2 of the scale), and l takes the sums as they are, to be divided.
 template <bool FP8, bool WIDE>
 __device__ inline void weigh_pair(const Scores& x, int b, int j, float cb, float nm, float vs, float& l,
                                   uint32_t (&p)[WIDE ? 3 : 1][4]) {
   float u = __builtin_amdgcn_exp2f(fmaf(x.s[b / 2][8 * (b % 2) + 2 * j], cb, nm));
   float v = __builtin_amdgcn_exp2f(fmaf(x.s[b / 2][8 * (b % 2) + 2 * j + 1], cb, nm));
-  if constexpr (FP8 || WIDE) l += u + v;
-  if constexpr (FP8) u *= vs, v *= vs;
+  if constexpr (WIDE) {
+    l += u + v;
+    if constexpr (FP8) u *= vs, v *= vs;
+  }
   p[0][j] = pack_bf16x2(u, v);
   if constexpr (WIDE) {
 #pragma unroll
@@ -233,54 +237,92 @@ __device__ inline void weigh_pair(const Scores& x, int b, int j, float cb, float
       v -= __uint_as_float(p[k - 1][j] & 0xffff0000u);
       p[k][j] = pack_bf16x2(u, v);
     }
-  }
-  if constexpr (!FP8 && !WIDE)
+  } else {
     l = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, p[0][j]), bf16x2{(__bf16)1.f, (__bf16)1.f}, l, false);
+  }
+}
+
+// What a block's exponents add to the scores, and what its sum counts for.
+template <bool FP8, bool WIDE>
+__device__ inline float shift(float nm, const KeyScales& sc, int b) {
+  return FP8 && !WIDE ? nm + sc.log_v[b] : nm;
+}
+template <bool FP8, bool WIDE>
+__device__ inline float share(float l, const KeyScales& sc, int b) {
+  return FP8 && !WIDE ? l * sc.inv_v[b] : l;
 }
 
 __device__ inline bf16x8 operand(const uint32_t (&p)[4]) {
   return __builtin_bit_cast(bf16x8, make_uint4(p[0], p[1], p[2], p[3]));
 }
 
+// Keeps what makes x where it is written (sums and maxima that are used later
+// otherwise sink to there, with their operands in registers until then).
+__device__ inline void stay(float& x) { asm volatile("" : "+v"(x)); }
+
 // A tile that every row of the wave sees whole (scores x), and with it the
 // scores y of the next tile.  A wave issues in order and a matrix product
 // holds up only what needs its result, so the order is written out: between
-// two products the vector units make two tokens' weights (while Q.K of the
-// next tile runs) or a part of the next tile's maximum (while P.V runs), and
-// an operand is read from LDS kAhead products before it is used.
+// two products the vector units take one step each of two tokens' weights -
+// the exponents of a pair, the exponentials of the pair before, the rounding of
+// the one before that, its sum - while Q.K of the next tile runs, and a part of
+// the next tile's maximum while P.V runs; nothing waits for the instruction in
+// front of it, and an operand is read from LDS kAhead products before its use.
 template <bool FP8>
 __device__ inline void plain_tile(const uint8_t* v, const uint8_t* k_next, const bf16x8 (&q)[8], float c,
                                   const KeyScales& sc, const KeyScales& sc_next, const Scores& x, Scores& y, float& mx,
                                   Rows& st) {
   constexpr int kAhead = 6;
   const float nm = reference(st);
-  float cb[4], l[2] = {0.f, 0.f}, mb[4];
+  float cb[4], nb[4], l[4] = {0.f, 0.f, 0.f, 0.f}, mb[4];
 #pragma unroll
-  for (int b = 0; b < 4; ++b) cb[b] = factor<FP8>(c, sc, b);
-  uint32_t p[4][1][4];
+  for (int b = 0; b < 4; ++b) cb[b] = factor<FP8>(c, sc, b), nb[b] = shift<FP8, false>(nm, sc, b);
+  uint32_t p[4][4];
+  float arg[2][2], e[2][2];  // by pair, every second one at the same place
   bf16x8 ring[kAhead];
   auto load = [&](int n) { return n < 16 ? k_operand(k_next, n % 2, n / 2) : v_operand(v, (n - 16) / 4, n % 4); };
+  auto args = [&](int j) {
+    const int b = j / 4, o = 8 * (b % 2) + 2 * (j % 4);
+    arg[j % 2][0] = fmaf(x.s[b / 2][o], cb[b], nb[b]);
+    arg[j % 2][1] = fmaf(x.s[b / 2][o + 1], cb[b], nb[b]);
+    stay(arg[j % 2][0]);
+    stay(arg[j % 2][1]);
+  };
 #pragma unroll
   for (int n = 0; n < kAhead; ++n) ring[n] = load(n);
+  args(0);
   __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
   for (int n = 0; n < 32; ++n) {
-    if (n < 16) {
+    if (n < 16)
       y.s[n % 2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ring[n % kAhead], q[n / 2], n < 2 ? f32x16{} : y.s[n % 2], 0, 0, 0);
-      weigh_pair<FP8, false>(x, n / 4, n % 4, cb[n / 4], nm, sc.v[n / 4], l[n % 2], p[n / 4]);
-    } else {
-      const int m = n - 16;
-      st.acc[m % 4] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ring[n % kAhead], operand(p[m / 4][0]), st.acc[m % 4], 0, 0, 0);
-      if (m >= 4 && m < 12) {  // y's four blocks, four scores a time
-        const int b = (m - 4) / 2, o = 8 * (b % 2) + 4 * (m % 2);
-        const f32x16& s = y.s[b / 2];
-        mb[b] = m % 2 == 0 ? fmaxf(max3(s[o], s[o + 1], s[o + 2]), s[o + 3]) : max3(max3(mb[b], s[o], s[o + 1]), s[o + 2], s[o + 3]);
-      }
+    else
+      st.acc[n % 4] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ring[n % kAhead], operand(p[n / 4 - 4]), st.acc[n % 4], 0, 0, 0);
+    if (n < 16) {
+      e[n % 2][0] = __builtin_amdgcn_exp2f(arg[n % 2][0]);
+      e[n % 2][1] = __builtin_amdgcn_exp2f(arg[n % 2][1]);
+      stay(e[n % 2][0]);
+      stay(e[n % 2][1]);
+    }
+    if (n < 15) args(n + 1);
+    if (n >= 1 && n < 17) p[(n - 1) / 4][(n - 1) % 4] = pack_bf16x2(e[(n - 1) % 2][0], e[(n - 1) % 2][1]);
+    if (n >= 2 && n < 18) {
+      const int b = (n - 2) / 4;
+      l[b] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, p[b][(n - 2) % 4]),
+                                             bf16x2{(__bf16)1.f, (__bf16)1.f}, l[b], false);
+      stay(l[b]);
+    }
+    if (n >= 20 && n < 28) {  // y's four blocks, four scores a time
+      const int b = n % 4, o = 8 * (b % 2) + 4 * (n / 4 - 5);
+      const f32x16& s = y.s[b / 2];
+      mb[b] = n < 24 ? fmaxf(max3(s[o], s[o + 1], s[o + 2]), s[o + 3]) : max3(max3(mb[b], s[o], s[o + 1]), s[o + 2], s[o + 3]);
+      stay(mb[b]);
     }
     if (n + kAhead < 32) ring[n % kAhead] = load(n + kAhead);
     __builtin_amdgcn_sched_barrier(0);
   }
-  st.l += l[0] + l[1];
+#pragma unroll
+  for (int b = 0; b < 4; ++b) st.l += share<FP8, false>(l[b], sc, b);
   if constexpr (FP8) {
 #pragma unroll
     for (int b = 0; b < 4; ++b) mb[b] *= factor<FP8>(c, sc_next, b);
@@ -324,13 +366,13 @@ template <bool FP8, bool WIDE>
 __device__ inline void last_tile(const uint8_t* v, float c, const KeyScales& sc, const Scores& x, Rows& st) {
   constexpr int kAhead = 6, kPlanes = WIDE ? 3 : 1;
   const float nm = reference(st);
-  float l = 0.f;
+  float l[4] = {0.f, 0.f, 0.f, 0.f};
   uint32_t p[2][kPlanes][4];
   bf16x8 ring[kAhead];
 #pragma unroll
   for (int n = 0; n < kAhead; ++n) ring[n] = v_operand(v, n / 4, n % 4);
 #pragma unroll
-  for (int j = 0; j < 4; ++j) weigh_pair<FP8, WIDE>(x, 0, j, factor<FP8>(c, sc, 0), nm, sc.v[0], l, p[0]);
+  for (int j = 0; j < 4; ++j) weigh_pair<FP8, WIDE>(x, 0, j, factor<FP8>(c, sc, 0), shift<FP8, WIDE>(nm, sc, 0), sc.v[0], l[0], p[0]);
   __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
   for (int n = 0; n < 16; ++n) {
@@ -338,11 +380,16 @@ __device__ inline void last_tile(const uint8_t* v, float c, const KeyScales& sc,
 #pragma unroll
     for (int k = kPlanes - 1; k >= 0; --k)
       st.acc[n % 4] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ring[n % kAhead], operand(p[b % 2][k]), st.acc[n % 4], 0, 0, 0);
-    if (b < 3) weigh_pair<FP8, WIDE>(x, b + 1, n % 4, factor<FP8>(c, sc, b + 1), nm, sc.v[b + 1], l, p[(b + 1) % 2]);
+    if (b < 3) {
+      weigh_pair<FP8, WIDE>(x, b + 1, n % 4, factor<FP8>(c, sc, b + 1), shift<FP8, WIDE>(nm, sc, b + 1), sc.v[b + 1], l[b + 1],
+                            p[(b + 1) % 2]);
+      stay(l[b + 1]);
+    }
     if (n + kAhead < 16) ring[n % kAhead] = v_operand(v, (n + kAhead) / 4, (n + kAhead) % 4);
     __builtin_amdgcn_sched_barrier(0);
   }
-  st.l += l;
+#pragma unroll
+  for (int b = 0; b < 4; ++b) st.l += share<FP8, WIDE>(l[b], sc, b);
 }
 
 // The same for a tile whose V holds infinities or NaN that not every row sees:
@@ -354,8 +401,10 @@ __device__ inline void slow_tile(const uint8_t* vt, float c, const KeyScales& sc
 #pragma unroll
   for (int b = 0; b < 4; ++b) {
     uint32_t p[WIDE ? 3 : 1][4];
+    float l = 0.f;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) weigh_pair<FP8, WIDE>(x, b, j, factor<FP8>(c, sc, b), nm, sc.v[b], st.l, p);
+    for (int j = 0; j < 4; ++j) weigh_pair<FP8, WIDE>(x, b, j, factor<FP8>(c, sc, b), shift<FP8, WIDE>(nm, sc, b), sc.v[b], l, p);
+    st.l += share<FP8, WIDE>(l, sc, b);
     uint4 v[4];
 #pragma unroll
     for (int db = 0; db < 4; ++db) v[db] = __builtin_bit_cast(uint4, v_operand(vt, b, db));
@@ -407,6 +456,7 @@ constexpr int kKTile = k_block_at(4), kVTile = kKeyTile * kHeadDim * 2;  // of a
 template <bool FP8, bool WIDE, bool DRAFT>
 __global__ __launch_bounds__(kThreads, 2) void rows_attn_kernel(DevPool P, RowsLaunch A) {
   __shared__ __attribute__((aligned(1024))) uint8_t lds[2 * kKTile + 2 * kVTile];
+  __shared__ __attribute__((aligned(16))) float scale_s[3][4][4];
   __shared__ uint32_t bad_s[2][4];  // by tile and wave: its block's V is not all finite
   // the quotient in a scalar register, so that what it leads to is read by scalar loads
   const int item = __builtin_amdgcn_readfirstlane(blockIdx.x / P.Hkv), kvh = blockIdx.x - item * P.Hkv;
@@ -433,8 +483,7 @@ __global__ __launch_bounds__(kThreads, 2) void rows_attn_kernel(DevPool P, RowsL
   const int32_t* brow = P.table + (size_t)U.trace * P.max_blocks;
   const size_t tile_bytes = (size_t)kBlock * kHeadDim * (FP8 ? 1 : 2);
 
-  // Wave w moves block w of a tile.  Its id is asked for a tile ahead of its
-  // bytes (fp8: all four ids, whose scales every wave needs).
+  // Wave w moves block w of a tile.  Its id is asked for a tile ahead of its bytes.
   auto id_of = [&](int i, int b) { return ld_const(brow + min(U.jb0 + 4 * i + b, jlast)); };
   bool bad_id = false;
   auto checked = [&](int id) {
@@ -445,12 +494,14 @@ __global__ __launch_bounds__(kThreads, 2) void rows_attn_kernel(DevPool P, RowsL
   auto block_at = [&](const uint8_t* cache, int id) { return cache + ((size_t)id * P.Hkv + kvh) * tile_bytes; };
   auto kbuf = [&](int i) { return lds + (i & 1) * kKTile; };
   auto vbuf = [&](int i) { return lds + 2 * kKTile + (i & 1) * kVTile; };
-  uint4 raw_k[2], raw_v[2];  // fp8: the codes on their way
+  uint4 raw_k[2], raw_v[2];  // fp8: the codes on their way,
+  float raw_scale = 0.f;     // and the block's K scale (lane 0) and V scale (lanes 1 to 3)
   auto ask_k = [&](int id, int i) {
     const uint8_t* src = block_at(P.k_cache, id);
     if constexpr (FP8) {
       raw_k[0] = load16(src + lane * 16, U.once);
       raw_k[1] = load16(src + lane * 16 + 1024, U.once);
+      if (lane < 4) raw_scale = P.kv_scale[2 * (size_t)id + min(lane, 1)];
     } else {
       dma16x4(src, lane * 16, kbuf(i) + k_block_at(w), U.once);
     }
@@ -465,6 +516,10 @@ __global__ __launch_bounds__(kThreads, 2) void rows_attn_kernel(DevPool P, RowsL
     }
   };
   auto widen_k = [&](int i) {  // 16 d of a row -> two chunks of 8
+    if (lane < 4) {  // lane 0: K's; lanes 1 to 3: V's, its log2, its reciprocal
+      const float x = lane ? fmaxf(raw_scale, 0x1p-100f) : raw_scale;
+      scale_s[i % 3][lane][w] = lane == 2 ? __builtin_amdgcn_logf(x) : lane == 3 ? 1.f / x : x;
+    }
 #pragma unroll
     for (int y = 0; y < 2; ++y) {
       uint8_t* k = kbuf(i) + k_block_at(w) + (2 * (4 * y + (lane >> 4)) * kBlock + (lane & 15)) * 16;
@@ -480,16 +535,16 @@ __global__ __launch_bounds__(kThreads, 2) void rows_attn_kernel(DevPool P, RowsL
       *reinterpret_cast<uint4*>(v + 512) = widen8(raw_v[y].z, raw_v[y].w);
     }
   };
+  // fp8: the scales of a tile's blocks, put into LDS by the wave that moves the
+  // block when it settles the tile's K, two tiles ahead (so three places).
   auto scales = [&](int i) {
     KeyScales s;
 #pragma unroll
     for (int b = 0; b < 4; ++b) {
-      s.k[b] = s.v[b] = 1.f;
-      if constexpr (FP8) {
-        const size_t id = checked(id_of(i, b));
-        s.k[b] = ld_const(P.kv_scale + 2 * id);
-        s.v[b] = ld_const(P.kv_scale + 2 * id + 1);
-      }
+      s.k[b] = FP8 ? scale_s[i % 3][0][b] : 1.f;
+      s.v[b] = FP8 ? scale_s[i % 3][1][b] : 1.f;
+      s.log_v[b] = FP8 ? scale_s[i % 3][2][b] : 0.f;
+      s.inv_v[b] = FP8 ? scale_s[i % 3][3][b] : 1.f;
     }
     return s;
   };
@@ -527,7 +582,6 @@ __global__ __launch_bounds__(kThreads, 2) void rows_attn_kernel(DevPool P, RowsL
   for (int db = 0; db < 4; ++db) st.acc[db] = f32x16{};
   Scores x, y;
   float mx = -INFINITY;
-  KeyScales sc{}, sc1{};
   if (ntiles > 0) {
     if constexpr (FP8) widen_k(0);
     wait_all();
@@ -535,11 +589,9 @@ __global__ __launch_bounds__(kThreads, 2) void rows_attn_kernel(DevPool P, RowsL
     ask_v(id0, 0);
     if (ntiles > 1) ask_k(id1, 1);
     id2 = id_of(2, w);
-    sc = scales(0);
-    sc1 = scales(1);
     if (nt > 0) {
       qk(kbuf(0) + k_lane(lane), q, x);
-      mx = tile_max<FP8>(x, A.c, sc);
+      mx = tile_max<FP8>(x, A.c, scales(0));
     }
     if constexpr (FP8) {
       widen_v(0);
@@ -578,22 +630,20 @@ __global__ __launch_bounds__(kThreads, 2) void rows_attn_kernel(DevPool P, RowsL
     wait_all();
     barrier_no_fence();
     id2 = checked(id2);
-    if (i + 2 < ntiles) ask_k(id2, i);
+    if (i + 2 < ntiles) ask_k(id2, i + 2);
     if (i + 1 < ntiles) ask_v(id1, i + 1);
     id1 = id2;
     id2 = id_of(i + 3, w);
   };
   auto end = [&](int i) {
     if constexpr (FP8) {
-      if (i + 2 < ntiles) widen_k(i);
+      if (i + 2 < ntiles) widen_k(i + 2);
       if (i + 1 < ntiles) widen_v(i + 1);
     }
-    sc = sc1;
-    sc1 = scales(i + 2);
   };
   auto plain = [&](int i, const Scores& a, Scores& b) {
     rescale(mx, st);
-    plain_tile<FP8>(vbuf(i) + lane * 16, kbuf(i + 1) + k_lane(lane), q, A.c, sc, sc1, a, b, mx, st);
+    plain_tile<FP8>(vbuf(i) + lane * 16, kbuf(i + 1) + k_lane(lane), q, A.c, scales(i), scales(i + 1), a, b, mx, st);
   };
   int i = 0;
   if constexpr (!WIDE) {
@@ -621,22 +671,22 @@ __global__ __launch_bounds__(kThreads, 2) void rows_attn_kernel(DevPool P, RowsL
     if (i < nt) {
       if (tb + kKeyTile > lim_lo) {
         mask_scores(lim - tb <= 0 ? 0 : ~0ull >> (64 - min(lim - tb, 64)), lane, x);
-        mx = tile_max<FP8>(x, A.c, sc);
+        mx = tile_max<FP8>(x, A.c, scales(i));
       }
       const bool more = i + 1 < nt;
       if (check && is_bad(i)) {
         rescale(mx, st);
-        slow_tile<FP8, WIDE>(vbuf(i) + lane * 16, A.c, sc, x, st);
+        slow_tile<FP8, WIDE>(vbuf(i) + lane * 16, A.c, scales(i), x, st);
       } else if (!WIDE && more) {
         if constexpr (!WIDE) plain(i, x, y);
         x = y;
       } else {
         rescale(mx, st);
-        last_tile<FP8, WIDE>(vbuf(i) + lane * 16, A.c, sc, x, st);
+        last_tile<FP8, WIDE>(vbuf(i) + lane * 16, A.c, scales(i), x, st);
       }
       if (more && (WIDE || (check && is_bad(i)))) {
         qk(kbuf(i + 1) + k_lane(lane), q, x);
-        mx = tile_max<FP8>(x, A.c, sc1);
+        mx = tile_max<FP8>(x, A.c, scales(i + 1));
       }
     }
     end(i);
@@ -651,7 +701,7 @@ __global__ __launch_bounds__(kThreads, 2) void rows_attn_kernel(DevPool P, RowsL
       if (active) {
         KeyScales one;
 #pragma unroll
-        for (int b = 0; b < 4; ++b) one.k[b] = one.v[b] = 1.f;
+        for (int b = 0; b < 4; ++b) one.k[b] = one.v[b] = one.inv_v[b] = 1.f, one.log_v[b] = 0.f;
         qk(kbuf(0) + k_lane(lane), q, x);
         mask_scores(here ? A.anc[tok] : 1, lane, x);
         rescale(tile_max<FP8>(x, A.c, one), st);
