@@ -157,16 +157,19 @@ def workspace_size(desc: PoolDesc) -> int:
 
 
 def _stream(stream=None):
-    s = torch.cuda.current_stream() if stream is None else stream
-    return ctypes.c_void_p(s.cuda_stream)
+    if stream is None:  # the raw handle: a small call is otherwise a tenth stream objects
+        return ctypes.c_void_p(torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()))
+    return ctypes.c_void_p(stream.cuda_stream)
 
 
 def _host_i32(x) -> np.ndarray:
+    if type(x) is np.ndarray and x.dtype == np.int32 and x.ndim == 1 and x.flags.c_contiguous:
+        return x
     return np.ascontiguousarray(np.asarray(x, dtype=np.int32))
 
 
 def _ptr(a: np.ndarray):
-    return a.ctypes.data_as(ctypes.c_void_p)
+    return a.__array_interface__["data"][0]
 
 
 def _spec(t: torch.Tensor, dtype=None, shape=None, what: str = "tensor"):
@@ -432,9 +435,8 @@ class Pool:
         ids, counts = _host_i32(ids), _host_i32(counts)
         if counts.shape != ids.shape:
             raise ValueError(f"{what}: expected one per trace")
-        if counts.size and int(counts.min()) < 0:
-            raise ValueError(f"{what}: negative")
-        return ids, counts, int(counts.sum(dtype=np.int64))
+        # (a negative count is refused by the library, before anything is read)
+        return ids, counts, sum(counts.tolist()) if counts.size <= 64 else int(counts.sum(dtype=np.int64))
 
     def kv_write_layer(self, layer: int, ids, pos0, n_tokens, k: torch.Tensor, v: torch.Tensor, rows=None,
                        stream=None):
