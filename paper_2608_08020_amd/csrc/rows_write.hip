@@ -14,21 +14,35 @@ namespace {
 
 constexpr int kRow = kHeadDim * 2;  // bytes of a token's head in the caller's K or V
 
-// Nearest E4M3FN code of y (ties to even; beyond 448 saturating; NaN stays).
-__device__ inline uint32_t fp8_code(float y) {
-  const uint32_t u = __float_as_uint(y), sign = (u >> 24) & 0x80u, m = u & 0x7FFFFFFFu;
-  const float a = __uint_as_float(m);
-  uint32_t c;
-  if (m > 0x7F800000u)
-    c = 0x7Fu;
-  else if (a >= 448.f)
-    c = 0x7Eu;
-  else if (a < 0.015625f)  // subnormal: steps of 2^-9
-    c = (uint32_t)__builtin_rintf(a * 512.f);
-  else
-    c = ((m + 0x7FFFFu + ((m >> 20) & 1u)) >> 20) - (120u << 3);
-  return sign | c;
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+// x / s rounded to fp32, r = 1 / s rounded: a product with the reciprocal and
+// one correction by the exact remainder is the rounded quotient (Markstein's
+// theorem).  Quotients beyond E4M3FN's range saturate whatever their last bits,
+// and so small ones that the remainder underflows have code zero.
+__device__ inline float quotient(float x, float s, float r) {
+  const float q = x * r, e = fmaf(-q, s, x);
+  return fabsf(q) < 512.f ? fmaf(e, r, q) : q;
 }
+
+// Nearest E4M3FN codes of four quotients (ties to even; beyond 448 saturating;
+// NaN stays), one byte each.
+__device__ inline uint32_t fp8_codes(float a, float b, float c, float d) {
+  const float y[4] = {a, b, c, d};
+  float z[4];
+  uint32_t nan = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    z[i] = __builtin_amdgcn_fmed3f(y[i], -448.f, 448.f);
+    nan |= y[i] != y[i] ? 0xffu << (8 * i) : 0u;
+  }
+  int w = __builtin_amdgcn_cvt_pk_fp8_f32(z[0], z[1], 0, false);
+  w = __builtin_amdgcn_cvt_pk_fp8_f32(z[2], z[3], w, true);
+  return ((uint32_t)w & ~nan) | (0x7f7f7f7fu & nan);
+}
+
+__device__ inline float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ inline float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
 
 __device__ inline size_t source_row(const WriteLaunch& L, int tok) { return L.rows ? L.rows[tok] : tok; }
 
@@ -69,23 +83,46 @@ __global__ __launch_bounds__(256) void rows_write_bf16_kernel(DevPool P, WriteLa
   }
 }
 
-// blockIdx.y: 0 K, 1 V.  Heads go eight at a time through registers: their
-// tokens are read once where a block has at most eight heads, twice otherwise.
+// blockIdx.y: 0 K, 1 V.  Two heads of the block a pass, a half of the workgroup
+// each, four passes in registers (so a block of at most eight heads is read
+// once, a larger one twice: magnitudes, then codes).  K: a thread takes 16 d of
+// a row, one 16-byte chunk of the tile, in the tile's order, so its stores need
+// no turning.  V: four tokens by four d, turned in LDS.
 __global__ __launch_bounds__(256) void rows_write_fp8_kernel(DevPool P, WriteLaunch L) {
-  constexpr int kHeads = 8, kTile = kBlock * kHeadDim;
+  constexpr int kPasses = 4, kHeads = 2 * kPasses, kTile = kBlock * kHeadDim;
   __shared__ __attribute__((aligned(16))) uint8_t lds[kHeads * kTile];
   __shared__ uint32_t most_s[4];
-  const int t = threadIdx.x, which = blockIdx.y;
+  const int t = threadIdx.x, half = t >> 7, u = t & 127;
+  const bool is_v = blockIdx.y != 0;
   const WriteItem U = L.items[blockIdx.x];
-  const int r0 = U.r0, r1 = U.r1, row = t >> 4, c = t & 15;
-  const uint16_t* src = (which ? L.v : L.k) + source_row(L, U.src + min(max(row, r0), r1 - 1) - r0) * P.Hkv * kHeadDim + 8 * c;
-  uint4 x[kHeads];
+  const int r0 = U.r0, r1 = U.r1;
+  // the thread's rows: K one, V four; rows outside the write re-read one inside it (never stored)
+  const int krow = k_phys(u & 15), c = u >> 4;   // K: 16-byte chunk c of row krow
+  const int tg = u >> 5, dg = u & 31;            // V: tokens 4 tg .., d 4 dg ..
+  size_t src[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int row = is_v ? 4 * tg + i : krow;
+    src[i] = source_row(L, U.src + min(max(row, r0), r1 - 1) - r0) * P.Hkv * kHeadDim + (is_v ? 4 * dg : 16 * c);
+  }
+  uint4 x[kPasses][2];  // K: 16 values of a row; V: 4 values of 4 rows
   auto load = [&](int h0) {
 #pragma unroll
-    for (int i = 0; i < kHeads; ++i)
-      x[i] = *reinterpret_cast<const uint4*>(src + (size_t)min(h0 + i, P.Hkv - 1) * kHeadDim);
+    for (int i = 0; i < kPasses; ++i) {
+      const size_t h = (size_t)min(h0 + 2 * i + half, P.Hkv - 1) * kHeadDim;
+      if (is_v) {
+        u32x2 y[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) y[j] = *reinterpret_cast<const u32x2*>(L.v + src[j] + h);
+        x[i][0] = make_uint4(y[0].x, y[0].y, y[1].x, y[1].y);
+        x[i][1] = make_uint4(y[2].x, y[2].y, y[3].x, y[3].y);
+      } else {
+        x[i][0] = *reinterpret_cast<const uint4*>(L.k + src[0] + h);
+        x[i][1] = *reinterpret_cast<const uint4*>(L.k + src[0] + h + 8);
+      }
+    }
   };
-  float* scale_at = P.kv_scale + 2 * (size_t)U.blk + which;
+  float* scale_at = P.kv_scale + 2 * (size_t)U.blk + is_v;
   float s;
   load(0);
   if (U.floor > 0.f) {
@@ -94,8 +131,9 @@ __global__ __launch_bounds__(256) void rows_write_fp8_kernel(DevPool P, WriteLau
     for (int h0 = 0; h0 < P.Hkv; h0 += kHeads) {
       if (h0) load(h0);
 #pragma unroll
-      for (int i = 0; i < kHeads; ++i) {
-        const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+      for (int i = 0; i < 2 * kPasses; ++i) {
+        const uint4 y = x[i / 2][i % 2];
+        const uint32_t w[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const uint32_t lo = w[j] & 0x7fffu, hi = (w[j] >> 16) & 0x7fffu;
@@ -115,41 +153,41 @@ __global__ __launch_bounds__(256) void rows_write_fp8_kernel(DevPool P, WriteLau
   } else {
     s = *scale_at;
   }
-  uint8_t* cache = which ? P.v_cache : P.k_cache;
+  const float r = 1.f / s;
+  auto q = [&](float y) { return quotient(y, s, r); };
+  uint8_t* cache = (is_v ? P.v_cache : P.k_cache) + (size_t)U.blk * P.Hkv * kTile;
   for (int h0 = 0; h0 < P.Hkv; h0 += kHeads) {
     const int nh = min(kHeads, P.Hkv - h0);
     if (h0) {
-      __syncthreads();  // the tiles of the heads before are stored
+      __syncthreads();  // the heads before are stored
       load(h0);
     }
 #pragma unroll
-    for (int i = 0; i < kHeads; ++i) {
-      if (i >= nh) break;
-      const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
-      uint32_t y[8];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        y[2 * j] = fp8_code(__uint_as_float(w[j] << 16) / s);
-        y[2 * j + 1] = fp8_code(__uint_as_float(w[j] & 0xffff0000u) / s);
-      }
-      uint8_t* tile = lds + i * kTile;
-      if (which == 0) {  // elements 8 c .. 8 c + 7 of the row: half a 16-byte chunk
-        *reinterpret_cast<uint2*>(tile + ((c >> 1) * kBlock + k_phys(row)) * 16 + (c & 1) * 8) =
-            make_uint2(y[0] | y[1] << 8 | y[2] << 16 | y[3] << 24, y[4] | y[5] << 8 | y[6] << 16 | y[7] << 24);
+    for (int i = 0; i < kPasses; ++i) {
+      const int hh = 2 * i + half;
+      const uint4 a = x[i][0], b = x[i][1];
+      if (!is_v) {
+        const uint4 y = make_uint4(fp8_codes(q(bf16_lo(a.x)), q(bf16_hi(a.x)), q(bf16_lo(a.y)), q(bf16_hi(a.y))),
+                                   fp8_codes(q(bf16_lo(a.z)), q(bf16_hi(a.z)), q(bf16_lo(a.w)), q(bf16_hi(a.w))),
+                                   fp8_codes(q(bf16_lo(b.x)), q(bf16_hi(b.x)), q(bf16_lo(b.y)), q(bf16_hi(b.y))),
+                                   fp8_codes(q(bf16_lo(b.z)), q(bf16_hi(b.z)), q(bf16_lo(b.w)), q(bf16_hi(b.w))));
+        if (hh < nh && krow >= r0 && krow < r1) *reinterpret_cast<uint4*>(cache + (size_t)(h0 + hh) * kTile + u * 16) = y;
       } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) tile[(8 * c + j) * kBlock + row] = (uint8_t)y[j];
+        uint32_t* tile = reinterpret_cast<uint32_t*>(lds + hh * kTile) + tg;  // [d][tokens]
+        tile[(4 * dg + 0) * 4] = fp8_codes(q(bf16_lo(a.x)), q(bf16_lo(a.z)), q(bf16_lo(b.x)), q(bf16_lo(b.z)));
+        tile[(4 * dg + 1) * 4] = fp8_codes(q(bf16_hi(a.x)), q(bf16_hi(a.z)), q(bf16_hi(b.x)), q(bf16_hi(b.z)));
+        tile[(4 * dg + 2) * 4] = fp8_codes(q(bf16_lo(a.y)), q(bf16_lo(a.w)), q(bf16_lo(b.y)), q(bf16_lo(b.w)));
+        tile[(4 * dg + 3) * 4] = fp8_codes(q(bf16_hi(a.y)), q(bf16_hi(a.w)), q(bf16_hi(b.y)), q(bf16_hi(b.w)));
       }
     }
+    if (!is_v) continue;
     __syncthreads();
-    uint8_t* dst = cache + ((size_t)U.blk * P.Hkv + h0) * kTile;
-    for (int u = t; u < nh * (kTile / 16); u += 256) {
-      const uint4 v = *reinterpret_cast<const uint4*>(lds + u * 16);
-      const int krow = k_phys(u & 15);
-      if (which == 0 ? (krow >= r0 && krow < r1) : (r0 == 0 && r1 == kBlock)) {
-        *reinterpret_cast<uint4*>(dst + u * 16) = v;
-      } else if (which == 1) {
-        for (int e = r0; e < r1; ++e) dst[u * 16 + e] = lds[u * 16 + e];
+    for (int d = t; d < nh * kHeadDim; d += 256) {
+      uint8_t* dst = cache + (size_t)h0 * kTile + d * kBlock;
+      if (r0 == 0 && r1 == kBlock) {
+        *reinterpret_cast<uint4*>(dst) = *reinterpret_cast<const uint4*>(lds + d * kBlock);
+      } else {
+        for (int e = r0; e < r1; ++e) dst[e] = lds[d * kBlock + e];
       }
     }
   }
