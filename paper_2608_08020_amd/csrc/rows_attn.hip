@@ -621,6 +621,14 @@ __global__ __launch_bounds__(kThreads, 2) void rows_attn_kernel(DevPool P, RowsL
     const uint64_t any = __builtin_amdgcn_ballot_w64(bad != 0);
     if (lane == 0) bad_s[i & 1][w] = any != 0;
   };
+  auto settle = [&](int i) {
+    const bool check = t0 + kKeyTile * (i + 1) > lim_wg;  // uniform over the workgroup
+    if (check) {
+      wait_all();
+      clean_v(i);
+    }
+    return check;
+  };
   auto is_bad = [&](int i) {
     return __builtin_amdgcn_readfirstlane(bad_s[i & 1][0] | bad_s[i & 1][1] | bad_s[i & 1][2] | bad_s[i & 1][3]) != 0;
   };
@@ -646,6 +654,16 @@ __global__ __launch_bounds__(kThreads, 2) void rows_attn_kernel(DevPool P, RowsL
     plain_tile<FP8>(vbuf(i) + lane * 16, kbuf(i + 1) + k_lane(lane), q, A.c, scales(i), scales(i + 1), a, b, mx, st);
   };
   int i = 0;
+  if (nt == 0) {
+    // The wave's rows see nothing here: it moves its blocks for the others, in a
+    // loop in which nothing else is held in registers.
+#pragma unroll 1
+    for (; i < ntiles; ++i) {
+      settle(i);
+      begin(i);
+      end(i);
+    }
+  }
   if constexpr (!WIDE) {
     // tiles that every row of the workgroup sees whole, before the wave's last
     const int np = min(lim_wg > t0 ? (lim_wg - t0) / kKeyTile : 0, nt - 1);
@@ -662,11 +680,7 @@ __global__ __launch_bounds__(kThreads, 2) void rows_attn_kernel(DevPool P, RowsL
 #pragma unroll 1
   for (; i < ntiles; ++i) {
     const int tb = t0 + kKeyTile * i;
-    const bool check = tb + kKeyTile > lim_wg;  // uniform over the workgroup
-    if (check) {
-      wait_all();
-      clean_v(i);
-    }
+    const bool check = settle(i);
     begin(i);
     if (i < nt) {
       if (tb + kKeyTile > lim_lo) {
