@@ -146,9 +146,17 @@ struct Scores {
   f32x16 s[2];
 };
 
-// fp8: the scales of a tile's four blocks; of V's also log2 and reciprocal.
-struct KeyScales {
-  float k[4], v[4], log_v[4], inv_v[4];
+// The factors of a tile's blocks.  fp8: in LDS, [quantity][block], read where
+// they are used (a tile's worth of them would take 16 registers); bf16: the
+// softmax scale.
+struct Factors {
+  const float* s;
+  float c;
+  template <bool FP8>
+  __device__ float k(int b) const { return FP8 ? s[b] : c; }  // of the raw scores, in log2 units
+  __device__ float v(int b) const { return s[4 + b]; }        // of V, its log2 and reciprocal
+  __device__ float log_v(int b) const { return s[8 + b]; }
+  __device__ float inv_v(int b) const { return s[12 + b]; }
 };
 
 // The operands in LDS, the lane's 16 bytes.  K is the cache's own image of each
@@ -177,15 +185,9 @@ __device__ inline void qk(const uint8_t* k, const bf16x8 (&q)[8], Scores& x) {
       x.s[th] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_operand(k, th, kb), q[kb], x.s[th], 0, 0, 0);
 }
 
-// Block b's factor of the raw scores (log2 units).
-template <bool FP8>
-__device__ inline float factor(float c, const KeyScales& sc, int b) {
-  return FP8 ? fmaxf(c * sc.k[b], 1e-37f) : c;
-}
-
 // The lane's largest score of the tile, scaled.
 template <bool FP8>
-__device__ inline float tile_max(const Scores& x, float c, const KeyScales& sc) {
+__device__ inline float tile_max(const Scores& x, const Factors& f) {
   float mb[4];
 #pragma unroll
   for (int b = 0; b < 4; ++b) {
@@ -193,10 +195,10 @@ __device__ inline float tile_max(const Scores& x, float c, const KeyScales& sc) 
     const int o = 8 * (b % 2);
     mb[b] = max3(max3(max3(s[o], s[o + 1], s[o + 2]), s[o + 3], s[o + 4]), s[o + 5], s[o + 6]);
     mb[b] = fmaxf(mb[b], s[o + 7]);
-    if constexpr (FP8) mb[b] *= factor<FP8>(c, sc, b);
+    if constexpr (FP8) mb[b] *= f.k<FP8>(b);
   }
   const float mx = fmaxf(max3(mb[0], mb[1], mb[2]), mb[3]);
-  return FP8 ? mx : mx * c;
+  return FP8 ? mx : mx * f.c;
 }
 
 // Moves a row's reference when a score exceeds it by more than 2^kLazy; until
@@ -244,12 +246,12 @@ __device__ inline void weigh_pair(const Scores& x, int b, int j, float cb, float
 
 // What a block's exponents add to the scores, and what its sum counts for.
 template <bool FP8, bool WIDE>
-__device__ inline float shift(float nm, const KeyScales& sc, int b) {
-  return FP8 && !WIDE ? nm + sc.log_v[b] : nm;
+__device__ inline float shift(float nm, const Factors& f, int b) {
+  return FP8 && !WIDE ? nm + f.log_v(b) : nm;
 }
 template <bool FP8, bool WIDE>
-__device__ inline float share(float l, const KeyScales& sc, int b) {
-  return FP8 && !WIDE ? l * sc.inv_v[b] : l;
+__device__ inline float share(float l, const Factors& f, int b) {
+  return FP8 && !WIDE ? l * f.inv_v(b) : l;
 }
 
 __device__ inline bf16x8 operand(const uint32_t (&p)[4]) {
@@ -269,14 +271,11 @@ __device__ inline void stay(float& x) { asm volatile("" : "+v"(x)); }
 // the next tile's maximum while P.V runs; nothing waits for the instruction in
 // front of it, and an operand is read from LDS kAhead products before its use.
 template <bool FP8>
-__device__ inline void plain_tile(const uint8_t* v, const uint8_t* k_next, const bf16x8 (&q)[8], float c,
-                                  const KeyScales& sc, const KeyScales& sc_next, const Scores& x, Scores& y, float& mx,
-                                  Rows& st) {
+__device__ inline void plain_tile(const uint8_t* v, const uint8_t* k_next, const bf16x8 (&q)[8], const Factors& f,
+                                  const Factors& f_next, const Scores& x, Scores& y, float& mx, Rows& st) {
   constexpr int kAhead = 6;
   const float nm = reference(st);
   float cb[4], nb[4], l[4] = {0.f, 0.f, 0.f, 0.f}, mb[4];
-#pragma unroll
-  for (int b = 0; b < 4; ++b) cb[b] = factor<FP8>(c, sc, b), nb[b] = shift<FP8, false>(nm, sc, b);
   uint32_t p[4][4];
   float arg[2][2], e[2][2];  // by pair, every second one at the same place
   bf16x8 ring[kAhead];
@@ -288,6 +287,7 @@ __device__ inline void plain_tile(const uint8_t* v, const uint8_t* k_next, const
     stay(arg[j % 2][0]);
     stay(arg[j % 2][1]);
   };
+  cb[0] = f.k<FP8>(0), nb[0] = shift<FP8, false>(nm, f, 0);
 #pragma unroll
   for (int n = 0; n < kAhead; ++n) ring[n] = load(n);
   args(0);
@@ -304,6 +304,7 @@ __device__ inline void plain_tile(const uint8_t* v, const uint8_t* k_next, const
       stay(e[n % 2][0]);
       stay(e[n % 2][1]);
     }
+    if (n < 12 && n % 4 == 0) cb[n / 4 + 1] = f.k<FP8>(n / 4 + 1), nb[n / 4 + 1] = shift<FP8, false>(nm, f, n / 4 + 1);
     if (n < 15) args(n + 1);
     if (n >= 1 && n < 17) p[(n - 1) / 4][(n - 1) % 4] = pack_bf16x2(e[(n - 1) % 2][0], e[(n - 1) % 2][1]);
     if (n >= 2 && n < 18) {
@@ -312,6 +313,7 @@ __device__ inline void plain_tile(const uint8_t* v, const uint8_t* k_next, const
                                              bf16x2{(__bf16)1.f, (__bf16)1.f}, l[b], false);
       stay(l[b]);
     }
+    if (n >= 6 && n < 22 && n % 4 == 2) st.l += share<FP8, false>(l[(n - 6) / 4], f, (n - 6) / 4);
     if (n >= 20 && n < 28) {  // y's four blocks, four scores a time
       const int b = n % 4, o = 8 * (b % 2) + 4 * (n / 4 - 5);
       const f32x16& s = y.s[b / 2];
@@ -321,14 +323,12 @@ __device__ inline void plain_tile(const uint8_t* v, const uint8_t* k_next, const
     if (n + kAhead < 32) ring[n % kAhead] = load(n + kAhead);
     __builtin_amdgcn_sched_barrier(0);
   }
-#pragma unroll
-  for (int b = 0; b < 4; ++b) st.l += share<FP8, false>(l[b], sc, b);
   if constexpr (FP8) {
 #pragma unroll
-    for (int b = 0; b < 4; ++b) mb[b] *= factor<FP8>(c, sc_next, b);
+    for (int b = 0; b < 4; ++b) mb[b] *= f_next.k<FP8>(b);
   }
   mx = fmaxf(max3(mb[0], mb[1], mb[2]), mb[3]);
-  if constexpr (!FP8) mx *= c;
+  if constexpr (!FP8) mx *= f.c;
 }
 
 // Adds the values of one kind (0: +inf, 1: -inf, 2: NaN) in a block's V to the
@@ -363,7 +363,7 @@ __device__ inline void mask_scores(uint64_t vis, int lane, Scores& x) {
 // A tile without one behind it (WIDE: any): the weights of a block are made
 // between the products of the block before.
 template <bool FP8, bool WIDE>
-__device__ inline void last_tile(const uint8_t* v, float c, const KeyScales& sc, const Scores& x, Rows& st) {
+__device__ inline void last_tile(const uint8_t* v, const Factors& f, const Scores& x, Rows& st) {
   constexpr int kAhead = 6, kPlanes = WIDE ? 3 : 1;
   const float nm = reference(st);
   float l[4] = {0.f, 0.f, 0.f, 0.f};
@@ -372,7 +372,7 @@ __device__ inline void last_tile(const uint8_t* v, float c, const KeyScales& sc,
 #pragma unroll
   for (int n = 0; n < kAhead; ++n) ring[n] = v_operand(v, n / 4, n % 4);
 #pragma unroll
-  for (int j = 0; j < 4; ++j) weigh_pair<FP8, WIDE>(x, 0, j, factor<FP8>(c, sc, 0), shift<FP8, WIDE>(nm, sc, 0), sc.v[0], l[0], p[0]);
+  for (int j = 0; j < 4; ++j) weigh_pair<FP8, WIDE>(x, 0, j, f.k<FP8>(0), shift<FP8, WIDE>(nm, f, 0), FP8 ? f.v(0) : 1.f, l[0], p[0]);
   __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
   for (int n = 0; n < 16; ++n) {
@@ -381,7 +381,7 @@ __device__ inline void last_tile(const uint8_t* v, float c, const KeyScales& sc,
     for (int k = kPlanes - 1; k >= 0; --k)
       st.acc[n % 4] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ring[n % kAhead], operand(p[b % 2][k]), st.acc[n % 4], 0, 0, 0);
     if (b < 3) {
-      weigh_pair<FP8, WIDE>(x, b + 1, n % 4, factor<FP8>(c, sc, b + 1), shift<FP8, WIDE>(nm, sc, b + 1), sc.v[b + 1], l[b + 1],
+      weigh_pair<FP8, WIDE>(x, b + 1, n % 4, f.k<FP8>(b + 1), shift<FP8, WIDE>(nm, f, b + 1), FP8 ? f.v(b + 1) : 1.f, l[b + 1],
                             p[(b + 1) % 2]);
       stay(l[b + 1]);
     }
@@ -389,22 +389,23 @@ __device__ inline void last_tile(const uint8_t* v, float c, const KeyScales& sc,
     __builtin_amdgcn_sched_barrier(0);
   }
 #pragma unroll
-  for (int b = 0; b < 4; ++b) st.l += share<FP8, WIDE>(l[b], sc, b);
+  for (int b = 0; b < 4; ++b) st.l += share<FP8, WIDE>(l[b], f, b);
 }
 
 // The same for a tile whose V holds infinities or NaN that not every row sees:
 // where a row's weight is zero the product would make them NaN, so they are
 // zeros in the product and go to the rows with a weight for them beside it.
 template <bool FP8, bool WIDE>
-__device__ inline void slow_tile(const uint8_t* vt, float c, const KeyScales& sc, const Scores& x, Rows& st) {
+__device__ inline void slow_tile(const uint8_t* vt, const Factors& f, const Scores& x, Rows& st) {
   const float nm = reference(st);
 #pragma unroll
   for (int b = 0; b < 4; ++b) {
     uint32_t p[WIDE ? 3 : 1][4];
     float l = 0.f;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) weigh_pair<FP8, WIDE>(x, b, j, factor<FP8>(c, sc, b), shift<FP8, WIDE>(nm, sc, b), sc.v[b], l, p);
-    st.l += share<FP8, WIDE>(l, sc, b);
+    for (int j = 0; j < 4; ++j)
+      weigh_pair<FP8, WIDE>(x, b, j, f.k<FP8>(b), shift<FP8, WIDE>(nm, f, b), FP8 ? f.v(b) : 1.f, l, p);
+    st.l += share<FP8, WIDE>(l, f, b);
     uint4 v[4];
 #pragma unroll
     for (int db = 0; db < 4; ++db) v[db] = __builtin_bit_cast(uint4, v_operand(vt, b, db));
@@ -516,8 +517,8 @@ __global__ __launch_bounds__(kThreads, 2) void rows_attn_kernel(DevPool P, RowsL
     }
   };
   auto widen_k = [&](int i) {  // 16 d of a row -> two chunks of 8
-    if (lane < 4) {  // lane 0: K's; lanes 1 to 3: V's, its log2, its reciprocal
-      const float x = lane ? fmaxf(raw_scale, 0x1p-100f) : raw_scale;
+    if (lane < 4) {  // lane 0: K's with the softmax scale; lanes 1 to 3: V's, its log2, its reciprocal
+      const float x = lane ? fmaxf(raw_scale, 0x1p-100f) : fmaxf(A.c * raw_scale, 0x1p-120f);
       scale_s[i % 3][lane][w] = lane == 2 ? __builtin_amdgcn_logf(x) : lane == 3 ? 1.f / x : x;
     }
 #pragma unroll
@@ -537,17 +538,7 @@ __global__ __launch_bounds__(kThreads, 2) void rows_attn_kernel(DevPool P, RowsL
   };
   // fp8: the scales of a tile's blocks, put into LDS by the wave that moves the
   // block when it settles the tile's K, two tiles ahead (so three places).
-  auto scales = [&](int i) {
-    KeyScales s;
-#pragma unroll
-    for (int b = 0; b < 4; ++b) {
-      s.k[b] = FP8 ? scale_s[i % 3][0][b] : 1.f;
-      s.v[b] = FP8 ? scale_s[i % 3][1][b] : 1.f;
-      s.log_v[b] = FP8 ? scale_s[i % 3][2][b] : 0.f;
-      s.inv_v[b] = FP8 ? scale_s[i % 3][3][b] : 1.f;
-    }
-    return s;
-  };
+  auto factors = [&](int i) { return Factors{scale_s[i % 3][0], A.c}; };
 
   // the first loads: tile 0's K, then the queries, tile 0's V and tile 1's K
   int id0 = 0, id1 = 0, id2 = 0;  // wave's blocks of tiles i, i + 1, i + 2 (past the end: the last block, unused)
@@ -591,7 +582,7 @@ __global__ __launch_bounds__(kThreads, 2) void rows_attn_kernel(DevPool P, RowsL
     id2 = id_of(2, w);
     if (nt > 0) {
       qk(kbuf(0) + k_lane(lane), q, x);
-      mx = tile_max<FP8>(x, A.c, scales(0));
+      mx = tile_max<FP8>(x, factors(0));
     }
     if constexpr (FP8) {
       widen_v(0);
@@ -651,7 +642,7 @@ __global__ __launch_bounds__(kThreads, 2) void rows_attn_kernel(DevPool P, RowsL
   };
   auto plain = [&](int i, const Scores& a, Scores& b) {
     rescale(mx, st);
-    plain_tile<FP8>(vbuf(i) + lane * 16, kbuf(i + 1) + k_lane(lane), q, A.c, scales(i), scales(i + 1), a, b, mx, st);
+    plain_tile<FP8>(vbuf(i) + lane * 16, kbuf(i + 1) + k_lane(lane), q, factors(i), factors(i + 1), a, b, mx, st);
   };
   int i = 0;
   if (nt == 0) {
@@ -685,22 +676,22 @@ __global__ __launch_bounds__(kThreads, 2) void rows_attn_kernel(DevPool P, RowsL
     if (i < nt) {
       if (tb + kKeyTile > lim_lo) {
         mask_scores(lim - tb <= 0 ? 0 : ~0ull >> (64 - min(lim - tb, 64)), lane, x);
-        mx = tile_max<FP8>(x, A.c, scales(i));
+        mx = tile_max<FP8>(x, factors(i));
       }
       const bool more = i + 1 < nt;
       if (check && is_bad(i)) {
         rescale(mx, st);
-        slow_tile<FP8, WIDE>(vbuf(i) + lane * 16, A.c, scales(i), x, st);
+        slow_tile<FP8, WIDE>(vbuf(i) + lane * 16, factors(i), x, st);
       } else if (!WIDE && more) {
         if constexpr (!WIDE) plain(i, x, y);
         x = y;
       } else {
         rescale(mx, st);
-        last_tile<FP8, WIDE>(vbuf(i) + lane * 16, A.c, scales(i), x, st);
+        last_tile<FP8, WIDE>(vbuf(i) + lane * 16, factors(i), x, st);
       }
       if (more && (WIDE || (check && is_bad(i)))) {
         qk(kbuf(i + 1) + k_lane(lane), q, x);
-        mx = tile_max<FP8>(x, A.c, scales(i + 1));
+        mx = tile_max<FP8>(x, factors(i + 1));
       }
     }
     end(i);
@@ -711,18 +702,17 @@ __global__ __launch_bounds__(kThreads, 2) void rows_attn_kernel(DevPool P, RowsL
       const uint32_t bad = stage_drafts(A, U, P.Hkv, kvh, t, kbuf(0), vbuf(0));
       const uint64_t any = __builtin_amdgcn_ballot_w64(bad != 0);
       if (lane == 0) bad_s[0][w] = any != 0;
+      if (FP8 && t < 16) scale_s[0][t >> 2][t & 3] = t < 4 ? A.c : t >> 2 == 2 ? 0.f : 1.f;  // the drafts are bf16
       __syncthreads();
       if (active) {
-        KeyScales one;
-#pragma unroll
-        for (int b = 0; b < 4; ++b) one.k[b] = one.v[b] = one.inv_v[b] = 1.f, one.log_v[b] = 0.f;
+        const Factors one = factors(0);
         qk(kbuf(0) + k_lane(lane), q, x);
         mask_scores(here ? A.anc[tok] : 1, lane, x);
-        rescale(tile_max<FP8>(x, A.c, one), st);
+        rescale(tile_max<FP8>(x, one), st);
         if (is_bad(0))
-          slow_tile<FP8, WIDE>(vbuf(0) + lane * 16, A.c, one, x, st);
+          slow_tile<FP8, WIDE>(vbuf(0) + lane * 16, one, x, st);
         else
-          last_tile<FP8, WIDE>(vbuf(0) + lane * 16, A.c, one, x, st);
+          last_tile<FP8, WIDE>(vbuf(0) + lane * 16, one, x, st);
       }
     }
   }
