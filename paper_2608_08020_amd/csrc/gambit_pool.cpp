@@ -32,7 +32,7 @@ using gambit::AttnUnit;
 namespace {
 
 constexpr int kDefaultChunkBlocks = 64;  // blocks per attention chunk before balancing
-constexpr size_t kPackedPartRows = 131072;  // partial rows of a packed call: two rounds of 512 workgroups of 128
+constexpr size_t kPackedPartRows = 262144;  // partial rows of a packed call: four rounds of 512 workgroups of 128
 
 // Per-token times of one attention unit on MI355X (microseconds), by kind and
 // cache dtype: narrow units per wave, cooperative items per workgroup.  fp8:
@@ -93,7 +93,7 @@ bool layout_of(const gambit_pool_desc* d, Layout* L) {
   L->units = take(sizeof(AttnUnit) * (size_t)L->max_units);
   L->members = take(4 * ((size_t)L->max_members + gambit::kMemberPad));
   // decode steps write up to kmax partials a trace; the packed rows of a
-  // prompt or tree call as many as two rounds of workgroups
+  // prompt or tree call as many as four rounds of workgroups
   L->max_parts = (int)std::min<size_t>(std::max<size_t>((size_t)T * kmax, kPackedPartRows / d->num_q_heads + 1), 1 << 30);
   L->part_ml = take(8 * (size_t)L->max_parts * d->num_q_heads);
   L->part_acc = take(4 * (size_t)L->max_parts * d->num_q_heads * gambit::kHeadDim);

@@ -113,6 +113,11 @@ struct Plan {
 // partial rows cost more than its keys.
 constexpr int kLeastChunk = 256;
 // Workgroups a call is cut into, as a multiple of those the chip runs at once.
+// More rounds share the chip more evenly but start more often and leave more
+// partials: 64 trees of eight nodes 156, 165, 177, 186 us with 1, 1.5, 2, 3
+// rounds; sixteen long trees 297, 319, 309, 318; insertions into 64 traces 284,
+// 283, 288, 296.  Choosing the rounds per call by the estimated length of the
+// longest-first schedule moved these by -1 to +4%.
 constexpr double kRounds = 1.0;
 
 struct Run {
@@ -253,10 +258,12 @@ bool try_plan(gambit_pool* p, const std::vector<Listed>& L, const std::vector<Ru
 gambit_status plan_rows(gambit_pool* p, std::vector<Listed> L, bool tree, const std::vector<uint64_t>& anc,
                         hipStream_t s) {
   const int tile = gambit::kRowsTile / p->g;
-  // Traces of one tile read shared blocks together; a longer prompt fills
-  // tiles of its own, which would read them once each either way.
+  // Traces of up to two tiles read shared blocks together, their rows packed
+  // into common tiles; a longer prompt fills tiles of its own well enough, which
+  // read the blocks once each either way.  64 traces in fours, 9 to 64 tokens of
+  // four heads each: 270 us with one tile as the limit, 256 with two or four.
   std::vector<char> share(L.size());
-  for (size_t i = 0; i < L.size(); ++i) share[i] = L[i].m > 0 && L[i].m <= tile;
+  for (size_t i = 0; i < L.size(); ++i) share[i] = L[i].m > 0 && L[i].m <= 2 * tile;
   std::vector<Run> runs;
   std::vector<std::vector<int32_t>> runs_of(L.size());
   shared_runs(p, L, share, &runs, &runs_of);
