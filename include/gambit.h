@@ -258,8 +258,9 @@ gambit_status gambit_kv_write_layer(gambit_pool* pool, int32_t layer, int32_t n,
  *   trace_ids, n_tokens  host [n]
  *   q         device [total][Hq][head_dim] bf16
  *   out       device [total][Hq][head_dim], bf16 or fp32 (out_dtype)
- * With bf16 output the weights are rounded to bf16 before they meet V (half a
- * step of 2^-7 of each), with fp32 output to 16 bits; sums are fp32. */
+ * fp8: block scales are >= 0.  With bf16 output the weights are rounded to bf16
+ * before they meet V (2^-8 of each, half a step), with fp32 output they are
+ * kept to fp32's precision; sums are fp32. */
 gambit_status gambit_prompt_attn(gambit_pool* pool, int32_t layer, int32_t n, const int32_t* trace_ids,
                                  const int32_t* n_tokens, const void* q, void* out, int32_t out_dtype,
                                  float sm_scale, void* stream);

@@ -11,7 +11,6 @@
 #include <algorithm>
 #include <cmath>
 #include <cstring>
-#include <new>
 #include <numeric>
 #include <vector>
 
@@ -327,7 +326,7 @@ gambit_status launch_rows(gambit_pool* p, int32_t layer, const void* q, const vo
   A.out = out;
   A.out_f32 = out_dtype == GAMBIT_OUT_F32;
   // the sign of the scale goes to the queries, a scale of zero makes them zero
-  A.c = sm_scale == 0.f ? 1.f : std::fabs(sm_scale) * 1.4426950408889634f;
+  A.c = sm_scale == 0.f ? 1.f : std::max(std::fabs(sm_scale) * 1.4426950408889634f, 0x1p-120f);
   A.q_and = sm_scale == 0.f ? 0u : 0xffffffffu;
   A.q_xor = sm_scale < 0.f ? 0x80008000u : 0u;
   A.gshift = __builtin_ctz(p->g);
@@ -474,16 +473,18 @@ gambit_status kv_write_layer(gambit_pool* p, int32_t layer, int32_t n, const int
   return GAMBIT_OK;
 }
 
-// No exception leaves a C entry.
+// No exception leaves a C entry; one that ended a plan half made leaves the
+// planners' per-block scratch as they expect it.
 template <class F>
 gambit_status guarded(gambit_pool* p, F&& f) {
   if (!p) return GAMBIT_ERR_INVALID;
   try {
     return f();
-  } catch (const std::bad_alloc&) {
-    return fail(p, GAMBIT_ERR_DEVICE, "out of host memory");
   } catch (...) {
-    return fail(p, GAMBIT_ERR_DEVICE, "host error");
+    std::fill(p->cnt.begin(), p->cnt.end(), 0);
+    std::fill(p->first.begin(), p->first.end(), -1);
+    p->rows_key.valid = p->write_key.valid = false;
+    return fail(p, GAMBIT_ERR_DEVICE, "out of host memory");
   }
 }
 

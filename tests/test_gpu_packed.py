@@ -4,7 +4,7 @@ Attention is compared with the definition in float64 on the same inputs.  Of
 an output sum_u p_u v_u / sum_u p_u, with S = sum_u p_u |v_u| (p normalised),
 the kernels' errors are at most, relative to S and to |out|:
   * the weights' rounding before they meet V: 2^-8 (bf16 output, half a step
-    of bf16), 2^-16 (fp32 output: a bf16 value and the bf16 remainder);
+    of bf16), 2^-16 at most (fp32 output: bf16 planes, two at least);
   * a score's error d (in its natural-exponent units) makes a weight exp(d)
     of itself: 128 fp32 additions of products, 2^-23 of sum |q k| each, and
     the roundings of the exponent, 2^-23 of twice the largest |score|;
@@ -293,6 +293,20 @@ def test_few_tokens_behind_shared_prefixes(fp8, out_dtype):
     check_prompt(S, [3, 4], [17, 1003], out_dtype)
 
 
+@pytest.mark.parametrize("out_dtype", OUT)
+def test_blocks_of_zero_scale(out_dtype):
+    """Values of a block with scale 0 are zeros: its scores weigh as zeros do, its V adds nothing."""
+    S = Kept(16, 2, T=2, maxb=20, fp8=True)
+    S.extend([0], [200])
+    table = S.pool.block_table[0].cpu().tolist()
+    S.pool.kv_scale[table[1]] = 0.0
+    S.pool.kv_scale[table[7], 0] = 0.0
+    S.pool.kv_scale[table[12], 1] = 0.0
+    S.K[0], S.V[0] = S.tokens(0, 0, 0, 200)
+    check_prompt(S, [0], [200], out_dtype)
+    check_tree(S, [0], [[-1, 0, 0]], out_dtype)
+
+
 def test_a_long_context_is_split_and_joined():
     S = Kept(32, 8, T=4, maxb=1300)
     S.extend([2], [20011])
@@ -312,7 +326,7 @@ def test_partial_slots_of_a_small_pool_suffice(splits):
     check_tree(S, [0, 1], [_random_tree(np.random.default_rng(1), 64)] * 2, torch.float32)
 
 
-@pytest.mark.parametrize("scale", [0.0, -0.05, 0.5])
+@pytest.mark.parametrize("scale", [0.0, -0.05, 0.5, 1e-44])
 def test_softmax_scales(scale):
     S = Kept(8, 2, T=4, maxb=20)
     S.extend([1], [150])
