@@ -109,6 +109,8 @@ __global__ __launch_bounds__(256) void rows_write_fp8_kernel(DevPool P, WriteLau
   auto load = [&](int h0) {
 #pragma unroll
     for (int i = 0; i < kPasses; ++i) {
+      x[i][0] = x[i][1] = make_uint4(0, 0, 0, 0);
+      if (h0 + 2 * i >= P.Hkv) continue;  // uniform
       const size_t h = (size_t)min(h0 + 2 * i + half, P.Hkv - 1) * kHeadDim;
       if (is_v) {
         u32x2 y[4];
@@ -164,6 +166,7 @@ __global__ __launch_bounds__(256) void rows_write_fp8_kernel(DevPool P, WriteLau
     }
 #pragma unroll
     for (int i = 0; i < kPasses; ++i) {
+      if (2 * i >= nh) continue;  // uniform
       const int hh = 2 * i + half;
       const uint4 a = x[i][0], b = x[i][1];
       if (!is_v) {
