@@ -160,10 +160,11 @@ struct Factors {
 };
 
 // The operands in LDS, the lane's 16 bytes.  K is the cache's own image of each
-// block ([d chunk][row]), every second block 128 bytes further, so that the
-// two blocks of a read use different banks; V is [block][32 d][token half][d].
+// block ([d chunk][row]), V is [block][32 d][token half][d].  A read of either
+// has lane l's bytes at 16 l modulo 256, which no bank serves twice a cycle (a
+// shift of every second block by 128 bytes cost a third of the LDS cycles).
 constexpr int kKBlock = kBlock * kHeadDim * 2;
-__host__ __device__ constexpr int k_block_at(int b) { return b * kKBlock + (b & 1) * 128 + (b >> 1) * 256; }
+__host__ __device__ constexpr int k_block_at(int b) { return b * kKBlock; }
 __device__ inline int k_lane(int lane) {
   return k_block_at((lane >> 4) & 1) + (lane >> 5) * 256 + (lane & 15) * 16;
 }
