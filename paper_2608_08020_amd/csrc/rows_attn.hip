@@ -288,7 +288,15 @@ __device__ inline void plain_tile(const uint8_t* v, const uint8_t* k_next, const
     stay(arg[j % 2][0]);
     stay(arg[j % 2][1]);
   };
-  cb[0] = f.k<FP8>(0), nb[0] = shift<FP8, false>(nm, f, 0);
+  f32x4 inv = {1.f, 1.f, 1.f, 1.f};
+  if constexpr (FP8) {
+    const f32x4 fk = *reinterpret_cast<const f32x4*>(f.s), fl = *reinterpret_cast<const f32x4*>(f.s + 8);
+#pragma unroll
+    for (int b = 0; b < 4; ++b) cb[b] = fk[b], nb[b] = nm + fl[b];
+  } else {
+#pragma unroll
+    for (int b = 0; b < 4; ++b) cb[b] = f.c, nb[b] = nm;
+  }
 #pragma unroll
   for (int n = 0; n < kAhead; ++n) ring[n] = load(n);
   args(0);
@@ -305,7 +313,6 @@ __device__ inline void plain_tile(const uint8_t* v, const uint8_t* k_next, const
       stay(e[n % 2][0]);
       stay(e[n % 2][1]);
     }
-    if (n < 12 && n % 4 == 0) cb[n / 4 + 1] = f.k<FP8>(n / 4 + 1), nb[n / 4 + 1] = shift<FP8, false>(nm, f, n / 4 + 1);
     if (n < 15) args(n + 1);
     if (n >= 1 && n < 17) p[(n - 1) / 4][(n - 1) % 4] = pack_bf16x2(e[(n - 1) % 2][0], e[(n - 1) % 2][1]);
     if (n >= 2 && n < 18) {
@@ -314,7 +321,8 @@ __device__ inline void plain_tile(const uint8_t* v, const uint8_t* k_next, const
                                              bf16x2{(__bf16)1.f, (__bf16)1.f}, l[b], false);
       stay(l[b]);
     }
-    if (n >= 6 && n < 22 && n % 4 == 2) st.l += share<FP8, false>(l[(n - 6) / 4], f, (n - 6) / 4);
+    if (FP8 && n == 16) inv = *reinterpret_cast<const f32x4*>(f.s + 12);
+    if (n >= 28) st.l = FP8 ? fmaf(l[n - 28], inv[n - 28], st.l) : st.l + l[n - 28];
     if (n >= 20 && n < 28) {  // y's four blocks, four scores a time
       const int b = n % 4, o = 8 * (b % 2) + 4 * (n / 4 - 5);
       const f32x16& s = y.s[b / 2];
@@ -325,8 +333,9 @@ __device__ inline void plain_tile(const uint8_t* v, const uint8_t* k_next, const
     __builtin_amdgcn_sched_barrier(0);
   }
   if constexpr (FP8) {
+    const f32x4 fk = *reinterpret_cast<const f32x4*>(f_next.s);
 #pragma unroll
-    for (int b = 0; b < 4; ++b) mb[b] *= f_next.k<FP8>(b);
+    for (int b = 0; b < 4; ++b) mb[b] *= fk[b];
   }
   mx = fmaxf(max3(mb[0], mb[1], mb[2]), mb[3]);
   if constexpr (!FP8) mx *= f.c;
