@@ -253,8 +253,8 @@ gambit_status gambit_kv_write_layer(gambit_pool* pool, int32_t layer, int32_t n,
  *     out[token][h] = softmax(q[token][h] . K[0..t, G]^T * sm_scale) V[0..t, G]
  * K and V past a token's own position do not reach its output, whatever they
  * hold.  Blocks that several listed traces share before their tokens are read
- * once for all of them when the traces have few tokens (up to 128 / (Hq / Hkv)
- * each).
+ * once for all of them when the traces have few tokens (up to 256 / (Hq / Hkv)
+ * each).  A row whose scores are all -inf, or one of them NaN, is NaN.
  *   trace_ids, n_tokens  host [n]
  *   q         device [total][Hq][head_dim] bf16
  *   out       device [total][Hq][head_dim], bf16 or fp32 (out_dtype)

@@ -22,6 +22,26 @@
 //
 // A range that is split, or shared by several traces, leaves unnormalised
 // partials that rows_merge_kernel joins by log-sum-exp.
+//
+// Why 128 rows: a key tile's 32 KiB (both operands, bf16) is read from LDS once
+// per 32 rows, 512 matrix cycles a wave, so that four waves of two workgroups
+// keep the CU's four matrix units and its LDS busy together; the 256 registers
+// a lane that two workgroups leave hold the wave's queries (32), outputs (64)
+// and the scores of two tiles (64).  Two buffers of K and of V fill 64 KiB.
+//
+// What bounds it, measured at 4.76 TB/s for a large copy and 1.25 PFLOP/s for a
+// large library product:
+//   long prompts, bf16: the matrix units and what issues beside them.  One of
+//     8192 tokens, 32 query heads over 8: 493 us, 1.11 PFLOP/s of the visible
+//     half (605 us before the order below was written out)
+//   long prompts, fp8: the same, and the codes' way to bf16 through registers
+//     and LDS, once per workgroup.  Four of 1024 to 4096 tokens, 64 query heads
+//     over 8: 559 us, 0.84 PFLOP/s
+//   trees and insertions over long contexts: HBM while the rows of a workgroup
+//     are few.  64 trees of eight nodes in fours: 125 us, 661 MB of keys and
+//     values at 5.3 TB/s, the partials' join 7; 128 fp8 trees: the widening,
+//     271 us with the join against 129 for the bytes
+//   a prompt of 17 tokens: one workgroup's start, chain of loads and end: 8.5 us
 #include <cmath>
 
 #include "lds_dma.h"
@@ -48,9 +68,6 @@ __device__ inline uint32_t pack_bf16x2(float a, float b) {
 // Scalar load of an int the launch does not write.
 __device__ inline int ld_const(const int32_t* p) {
   return *reinterpret_cast<const GAMBIT_CONST int32_t*>(reinterpret_cast<uintptr_t>(p));
-}
-__device__ inline float ld_const(const float* p) {
-  return *reinterpret_cast<const GAMBIT_CONST float*>(reinterpret_cast<uintptr_t>(p));
 }
 
 // One instruction (this source is built without IEEE mode, so the operands
@@ -146,9 +163,9 @@ struct Scores {
   f32x16 s[2];
 };
 
-// The factors of a tile's blocks.  fp8: in LDS, [quantity][block], read where
-// they are used (a tile's worth of them would take 16 registers); bf16: the
-// softmax scale.
+// The factors of a tile's blocks.  fp8: in LDS, [quantity][block], one quantity
+// of all four blocks read when it is needed (all 16 would stay in registers for
+// the tile); bf16: the softmax scale.
 struct Factors {
   const float* s;
   float c;

@@ -356,6 +356,48 @@ def test_later_tokens_do_not_reach_earlier_ones_whatever_they_hold(bad, out_dtyp
     assert torch.isfinite(out[:at, 4:].double()).all()
 
 
+@pytest.mark.parametrize("tree", [False, True])
+@pytest.mark.parametrize("out_dtype", OUT)
+def test_scores_of_minus_infinity_and_nan_in_a_split_context(tree, out_dtype):
+    S = Kept(8, 2, T=2, maxb=200)
+    n, lost, m = 3000, 1500, 4
+    k = S.normal(n, 2, D)
+    k[:lost, 0, 5] = -math.inf                         # KV head 0: the first half scores -inf
+    S.extend([1], [n], k=k)
+    q = S.normal(m, 8, D)
+    q[:, :4, 5] = q[:, :4, 5].abs() + 0.5
+    q[3, 4, 9] = math.nan                              # a row of NaN scores
+    if tree:
+        kn, vn = S.normal(m, 2, D), S.normal(m, 2, D)
+        up = [-1, 0, 0, 2]
+        out = S.pool.tree_attn(0, [1], [m], up, q, kn, vn, out_dtype=out_dtype)
+        K, V = torch.cat([S.K[1], kn.double()]), torch.cat([S.V[1], vn.double()])
+        sees = torch.cat([torch.ones(m, n, dtype=torch.bool, device=DEV), _kin(up)], 1)
+    else:
+        out = S.pool.prompt_attn(0, [1], [m], q, out_dtype=out_dtype)
+        K, V, sees = S.K[1], S.V[1], _causal(n, m)
+    rest = sees.clone()
+    rest[:, :lost] = False
+    _check(out[:, :4], q[:, :4], K[:, :1], V[:, :1], rest)
+    assert torch.isnan(out[3, 4].double()).all()
+    _check(out[:3, 4:], q[:3, 4:], K[:, 1:], V[:, 1:], sees[:3])
+    _check(out[3:, 5:6], q[3:, 5:6], K[:, 1:], V[:, 1:], sees[3:])
+
+
+@pytest.mark.parametrize("n", [40, 3000])
+def test_rows_whose_scores_are_all_minus_infinity_are_nan(n):
+    S = Kept(8, 2, T=2, maxb=200)
+    k = S.normal(n, 2, D)
+    k[:, 0, 5] = -math.inf
+    S.extend([1], [n], k=k)
+    q = S.normal(4, 8, D)
+    q[:, :4, 5] = q[:, :4, 5].abs() + 0.5
+    for out_dtype in OUT:
+        out = S.pool.prompt_attn(0, [1], [4], q, out_dtype=out_dtype)
+        assert torch.isnan(out[:, :4].double()).all()
+        _check(out[:, 4:], q[:, 4:], S.K[1][:, 1:], S.V[1][:, 1:], _causal(n, 4))
+
+
 # -------------------------------------------------------------------- trees --
 @pytest.mark.parametrize("out_dtype", OUT)
 @pytest.mark.parametrize("fp8", [False, True])
