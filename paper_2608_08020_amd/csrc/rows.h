@@ -29,7 +29,8 @@ struct RowItem {
   int32_t draft;   // first packed token of the trace's tree, -1: none
   int32_t ndraft;  // its tokens
   int32_t once;    // 1: no other item reads the range's blocks
-  int32_t pad[5];
+  int32_t first[4];  // the range's first four blocks (the last one again where there are fewer)
+  int32_t pad;
 };
 static_assert(sizeof(RowItem) == 64, "one scalar load");
 

@@ -293,6 +293,9 @@ gambit_status plan_rows(gambit_pool* p, std::vector<Listed> L, bool tree, const 
     ok = try_plan(p, L, runs, runs_of, tree, 1LL << 40, &plan);
   }
   if (!ok) return fail(p, GAMBIT_ERR_UNSUPPORTED, "plan exceeds workspace bounds");
+  for (RowItem& it : plan.items)
+    for (int b = 0; b < 4 && it.end > 16 * it.jb0; ++b)
+      it.first[b] = p->table[it.trace][std::min(it.jb0 + b, (it.end - 1) / 16)];
   // longest first, so that no long one starts late
   std::stable_sort(plan.items.begin(), plan.items.end(), [](const RowItem& a, const RowItem& b) {
     return a.end - 16 * a.jb0 > b.end - 16 * b.jb0;

@@ -108,6 +108,15 @@ __device__ inline uint4 load16(const uint8_t* p, bool once) {
   return __builtin_bit_cast(uint4, once ? __builtin_nontemporal_load(x) : *x);
 }
 
+// The lane, made anew: what the rare parts derive from it does not then wait for
+// them in registers that the loops need (a register reloaded from memory waits
+// for every direct load in flight).
+__device__ inline int lane_again() {
+  uint32_t m = ~0u;
+  asm volatile("" : "+s"(m));
+  return __builtin_amdgcn_mbcnt_hi(m, __builtin_amdgcn_mbcnt_lo(m, 0));
+}
+
 // Every load and LDS access of the wave has ended.
 __device__ inline void wait_all() {
   __builtin_amdgcn_s_waitcnt(0x0070);  // vmcnt 0, lgkmcnt 0
@@ -478,6 +487,39 @@ __device__ inline uint32_t stage_drafts(const RowsLaunch& A, const RowItem& U, i
   return bad;
 }
 
+// A wave's rows times `inv` to their places (`at`: row lane % 32's), fp32 or bf16,
+// turned in the wave's part of LDS.  What would be rows past the last one stores
+// that one again.
+template <class T>
+__device__ inline void store_rows(uint8_t* rows, const Rows& st, float inv, T* out, uint32_t at, int last, int lane) {
+  constexpr int kLanes = kHeadDim * sizeof(T) / 16, kPer = 64 / kLanes;  // lanes a row, rows an instruction stores
+  constexpr int kSteps = 32 / kPer;
+  const int n = lane & 31, h = lane >> 5, c = lane % kLanes;
+  auto row = [&](int k) { return min(k * kPer + lane / kLanes, last); };
+#pragma unroll
+  for (int db = 0; db < 4; ++db)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const f32x4 v = {st.acc[db][4 * j] * inv, st.acc[db][4 * j + 1] * inv, st.acc[db][4 * j + 2] * inv,
+                       st.acc[db][4 * j + 3] * inv};
+      if constexpr (sizeof(T) == 4)
+        *reinterpret_cast<f32x4*>(rows + n * 512 + ((8 * db + 2 * j + h) ^ n) * 16) = v;
+      else
+        *reinterpret_cast<uint2*>(rows + n * 256 + ((4 * db + j) ^ (n & 15)) * 16 + 8 * h) =
+            make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+    }
+  wait_all();
+  uint4 v[kSteps];
+  uint32_t to[kSteps];
+#pragma unroll
+  for (int k = 0; k < kSteps; ++k) {
+    v[k] = *reinterpret_cast<const uint4*>(rows + (row(k) * kLanes + (c ^ (row(k) % kLanes))) * 16);
+    to[k] = __shfl(at, row(k));
+  }
+#pragma unroll
+  for (int k = 0; k < kSteps; ++k) reinterpret_cast<uint4*>(out)[(size_t)to[k] * kLanes + c] = v[k];
+}
+
 constexpr int kRowBytes = kHeadDim * 2;  // of a query
 constexpr int kKTile = k_block_at(4), kVTile = kKeyTile * kHeadDim * 2;  // of a key tile in LDS
 
@@ -492,16 +534,16 @@ __global__ __launch_bounds__(kThreads, 2) void rows_attn_kernel(DevPool P, RowsL
       RowItem, *reinterpret_cast<const GAMBIT_CONST i32x16*>(reinterpret_cast<uintptr_t>(A.items + item)));
   const int t = threadIdx.x, lane = t & 63, w = __builtin_amdgcn_readfirstlane(t >> 6);
   const int h = lane >> 5, gs = A.gshift;
-  const int nrows = U.ntok << gs, row = 32 * w + (lane & 31);
-  const bool here = row < nrows;
-  int tok = 0;
-  if (here) tok = U.listed ? A.list[U.tok + (row >> gs)] : U.tok + (row >> gs);
-  const int head = (kvh << gs) + (row & ((1 << gs) - 1));
+  const int nrows = U.ntok << gs;
+  // the packed token of a row
+  auto token = [&](int row) {
+    const int j = U.tok + (row >> gs);
+    return U.listed ? A.list[j] : j;
+  };
 
-  // positions the lane's row sees, and the fewest and most that a row of the wave does
+  // positions that a row sees, and the fewest and most that one of the wave does
   const int t0 = kBlock * U.jb0;
   auto limit = [&](int r) { return U.pos0 == kNoLimit ? U.end : min(U.end, U.pos0 + (r >> gs) + 1); };
-  const int lim = limit(min(row, nrows - 1));
   const bool active = 32 * w < nrows;
   const int lim_lo = limit(32 * w), lim_hi = limit(min(32 * w + 31, nrows - 1));
   const int ntiles = U.end > t0 ? (U.end - t0 + kKeyTile - 1) / kKeyTile : 0;
@@ -524,7 +566,7 @@ __global__ __launch_bounds__(kThreads, 2) void rows_attn_kernel(DevPool P, RowsL
   auto vbuf = [&](int i) { return lds + 2 * kKTile + (i & 1) * kVTile; };
   uint4 raw_k[2], raw_v[2];  // fp8: the codes on their way,
   float raw_scale = 0.f;     // and the block's K scale (lane 0) and V scale (lanes 1 to 3)
-  auto ask_k = [&](int id, int i) {
+  auto ask_k = [&](int id, int i, int lane) {
     const uint8_t* src = block_at(P.k_cache, id);
     if constexpr (FP8) {
       raw_k[0] = load16(src + lane * 16, U.once);
@@ -534,16 +576,16 @@ __global__ __launch_bounds__(kThreads, 2) void rows_attn_kernel(DevPool P, RowsL
       dma16x4(src, lane * 16, kbuf(i) + k_block_at(w), U.once);
     }
   };
-  auto ask_v = [&](int id, int i) {
+  auto ask_v = [&](int id, int i, int lane) {
     const uint8_t* src = block_at(P.v_cache, id);
     if constexpr (FP8) {
       raw_v[0] = load16(src + lane * 16, U.once);
       raw_v[1] = load16(src + lane * 16 + 1024, U.once);
     } else {
-      dma16x4(src, (2 * (lane & 31) + h) * 16, vbuf(i) + w * kKBlock, U.once);
+      dma16x4(src, (2 * (lane & 31) + (lane >> 5)) * 16, vbuf(i) + w * kKBlock, U.once);
     }
   };
-  auto widen_k = [&](int i) {  // 16 d of a row -> two chunks of 8
+  auto widen_k = [&](int i, int lane) {  // 16 d of a row -> two chunks of 8
     if (lane < 4) {  // lane 0: K's with the softmax scale; lanes 1 to 3: V's, its log2, its reciprocal
       const float x = lane ? fmaxf(raw_scale, 0x1p-100f) : fmaxf(A.c * raw_scale, 0x1p-120f);
       scale_s[i % 3][lane][w] = lane == 2 ? __builtin_amdgcn_logf(x) : lane == 3 ? 1.f / x : x;
@@ -555,10 +597,10 @@ __global__ __launch_bounds__(kThreads, 2) void rows_attn_kernel(DevPool P, RowsL
       *reinterpret_cast<uint4*>(k + kBlock * 16) = widen8(raw_k[y].z, raw_k[y].w);
     }
   };
-  auto widen_v = [&](int i) {  // 16 tokens of a d -> two halves
+  auto widen_v = [&](int i, int lane) {  // 16 tokens of a d -> two halves
 #pragma unroll
     for (int y = 0; y < 2; ++y) {
-      uint8_t* v = vbuf(i) + w * kKBlock + (2 * y + h) * 1024 + (lane & 31) * 16;
+      uint8_t* v = vbuf(i) + w * kKBlock + (2 * y + (lane >> 5)) * 1024 + (lane & 31) * 16;
       *reinterpret_cast<uint4*>(v) = widen8(raw_v[y].x, raw_v[y].y);
       *reinterpret_cast<uint4*>(v + 512) = widen8(raw_v[y].z, raw_v[y].w);
     }
@@ -570,22 +612,29 @@ __global__ __launch_bounds__(kThreads, 2) void rows_attn_kernel(DevPool P, RowsL
   // the first loads: tile 0's K, then the queries, tile 0's V and tile 1's K
   int id0 = 0, id1 = 0, id2 = 0;  // wave's blocks of tiles i, i + 1, i + 2 (past the end: the last block, unused)
   if (ntiles > 0) {
-    id0 = checked(id_of(0, w));
-    id1 = checked(id_of(1, w));
-    ask_k(id0, 0);
+    id0 = checked(w < 2 ? (w ? U.first[1] : U.first[0]) : (w > 2 ? U.first[3] : U.first[2]));
+    ask_k(id0, 0, lane);
+    id1 = id_of(1, w);
   }
   // The wave's queries by way of LDS (V's place), so that whole rows are read:
   // row r's 16-byte chunk c at place c ^ (r % 16).
   uint8_t* mine = lds + 2 * kKTile + w * 32 * kRowBytes;
   if (active) {
+    int rt[8];  // rows past the last one read that one again
+    auto place = [&](int k) { return min(32 * w + 4 * k + (lane >> 4), nrows - 1); };
+#pragma unroll
+    for (int k = 0; k < 8; ++k) rt[k] = U.tok + (place(k) >> gs);
+    if (U.listed) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) rt[k] = A.list[rt[k]];
+    }
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-      const int r = 4 * k + (lane >> 4);
-      const int rt = __shfl(tok, r), rh = (kvh << gs) + (r & ((1 << gs) - 1));  // 32 rows: a whole number of groups
-      const size_t at = 32 * w + r < nrows ? (size_t)rt * P.Hq + rh : (size_t)__shfl(tok, 0) * P.Hq + (kvh << gs);
-      dma16(A.q + at * kHeadDim + 8 * ((lane & 15) ^ (r & 15)), mine + k * 1024);
+      const size_t at = (size_t)rt[k] * P.Hq + (kvh << gs) + (place(k) & ((1 << gs) - 1));
+      dma16(A.q + at * kHeadDim + 8 * ((lane & 15) ^ ((4 * k + (lane >> 4)) & 15)), mine + k * 1024);
     }
   }
+  id1 = checked(id1);
   wait_all();
   bf16x8 q[8];
 #pragma unroll
@@ -601,19 +650,19 @@ __global__ __launch_bounds__(kThreads, 2) void rows_attn_kernel(DevPool P, RowsL
   Scores x, y;
   float mx = -INFINITY;
   if (ntiles > 0) {
-    if constexpr (FP8) widen_k(0);
+    if constexpr (FP8) widen_k(0, lane);
     wait_all();
     barrier_no_fence();
-    ask_v(id0, 0);
-    if (ntiles > 1) ask_k(id1, 1);
+    ask_v(id0, 0, lane);
+    if (ntiles > 1) ask_k(id1, 1, lane);
     id2 = id_of(2, w);
     if (nt > 0) {
       qk(kbuf(0) + k_lane(lane), q, x);
       mx = tile_max<FP8>(x, factors(0));
     }
     if constexpr (FP8) {
-      widen_v(0);
-      if (ntiles > 1) widen_k(1);
+      widen_v(0, lane);
+      if (ntiles > 1) widen_k(1, lane);
     }
   }
   // A tile that ends the range, or that not every row of the workgroup sees
@@ -621,6 +670,7 @@ __global__ __launch_bounds__(kThreads, 2) void rows_attn_kernel(DevPool P, RowsL
   // weights are zero); bad_s says whether the others hold infinities or NaN.
   const int lim_wg = limit(0);
   auto clean_v = [&](int i) {
+    const int lane = lane_again(), h = lane >> 5;
     uint8_t* v = vbuf(i) + w * kKBlock + lane * 16;
     const int n = min(max(U.end - (t0 + kKeyTile * i + kBlock * w + 8 * h), 0), 8);
     const uint32_t there = (1u << n) - 1;
@@ -652,22 +702,22 @@ __global__ __launch_bounds__(kThreads, 2) void rows_attn_kernel(DevPool P, RowsL
   };
   // Start of tile i: its V and the K of tile i + 1 are there in every wave, and
   // no wave reads its K or the V of tile i - 1 any more; the next ones are asked for.
-  auto begin = [&](int i) {
+  auto begin = [&](int i, int lane) {
     wait_all();
     barrier_no_fence();
     id2 = checked(id2);
-    if (i + 2 < ntiles) ask_k(id2, i + 2);
-    if (i + 1 < ntiles) ask_v(id1, i + 1);
+    if (i + 2 < ntiles) ask_k(id2, i + 2, lane);
+    if (i + 1 < ntiles) ask_v(id1, i + 1, lane);
     id1 = id2;
     id2 = id_of(i + 3, w);
   };
-  auto end = [&](int i) {
+  auto end = [&](int i, int lane) {
     if constexpr (FP8) {
-      if (i + 2 < ntiles) widen_k(i + 2);
-      if (i + 1 < ntiles) widen_v(i + 1);
+      if (i + 2 < ntiles) widen_k(i + 2, lane);
+      if (i + 1 < ntiles) widen_v(i + 1, lane);
     }
   };
-  auto plain = [&](int i, const Scores& a, Scores& b) {
+  auto plain = [&](int i, int lane, const Scores& a, Scores& b) {
     rescale(mx, st);
     plain_tile<FP8>(vbuf(i) + lane * 16, kbuf(i + 1) + k_lane(lane), q, factors(i), factors(i + 1), a, b, mx, st);
   };
@@ -678,8 +728,8 @@ __global__ __launch_bounds__(kThreads, 2) void rows_attn_kernel(DevPool P, RowsL
 #pragma unroll 1
     for (; i < ntiles; ++i) {
       settle(i);
-      begin(i);
-      end(i);
+      begin(i, lane);
+      end(i, lane);
     }
   }
   if constexpr (!WIDE) {
@@ -687,21 +737,23 @@ __global__ __launch_bounds__(kThreads, 2) void rows_attn_kernel(DevPool P, RowsL
     const int np = min(lim_wg > t0 ? (lim_wg - t0) / kKeyTile : 0, nt - 1);
 #pragma unroll 1
     for (; i + 1 < np; i += 2) {
-      begin(i);
-      plain(i, x, y);
-      end(i);
-      begin(i + 1);
-      plain(i + 1, y, x);
-      end(i + 1);
+      begin(i, lane);
+      plain(i, lane, x, y);
+      end(i, lane);
+      begin(i + 1, lane);
+      plain(i + 1, lane, y, x);
+      end(i + 1, lane);
     }
   }
 #pragma unroll 1
   for (; i < ntiles; ++i) {
     const int tb = t0 + kKeyTile * i;
     const bool check = settle(i);
-    begin(i);
+    const int lane = lane_again();
+    begin(i, lane);
     if (i < nt) {
       if (tb + kKeyTile > lim_lo) {
+        const int lim = limit(min(32 * w + (lane & 31), nrows - 1));
         mask_scores(lim - tb <= 0 ? 0 : ~0ull >> (64 - min(lim - tb, 64)), lane, x);
         mx = tile_max<FP8>(x, factors(i));
       }
@@ -710,7 +762,7 @@ __global__ __launch_bounds__(kThreads, 2) void rows_attn_kernel(DevPool P, RowsL
         rescale(mx, st);
         slow_tile<FP8, WIDE>(vbuf(i) + lane * 16, factors(i), x, st);
       } else if (!WIDE && more) {
-        if constexpr (!WIDE) plain(i, x, y);
+        if constexpr (!WIDE) plain(i, lane, x, y);
         x = y;
       } else {
         rescale(mx, st);
@@ -721,7 +773,7 @@ __global__ __launch_bounds__(kThreads, 2) void rows_attn_kernel(DevPool P, RowsL
         mx = tile_max<FP8>(x, factors(i + 1));
       }
     }
-    end(i);
+    end(i, lane);
   }
   if constexpr (DRAFT) {
     if (U.draft >= 0) {  // uniform
@@ -734,7 +786,8 @@ __global__ __launch_bounds__(kThreads, 2) void rows_attn_kernel(DevPool P, RowsL
       if (active) {
         const Factors one = factors(0);
         qk(kbuf(0) + k_lane(lane), q, x);
-        mask_scores(here ? A.anc[tok] : 1, lane, x);
+        const int lane = lane_again(), row = 32 * w + (lane & 31);
+        mask_scores(row < nrows ? A.anc[U.tok + (row >> gs)] : 1, lane, x);  // a tree's rows are not listed
         rescale(tile_max<FP8>(x, one), st);
         if (is_bad(0))
           slow_tile<FP8, WIDE>(vbuf(0) + lane * 16, one, x, st);
@@ -744,49 +797,24 @@ __global__ __launch_bounds__(kThreads, 2) void rows_attn_kernel(DevPool P, RowsL
     }
   }
   if (bad_id && lane == 0) atomicOr(P.err, kErrBadBlock);
+  // Rows leave by way of LDS, whole ones at a time: a row's 16-byte chunk c at
+  // place c ^ (row % chunks), a wave's rows in its own part.
   const float l = st.l + other_half(st.l);
-  size_t at = 0;  // the row's place in the output or among the partials
-  if (here) at = (U.kidx >= 0 ? (size_t)(A.off[tok] + U.kidx) : (size_t)tok) * P.Hq + head;
-  if (U.kidx >= 0) {  // uniform
-    if (!here) return;
-    float* dst = A.part_acc + at * kHeadDim + 4 * h;
-#pragma unroll
-    for (int db = 0; db < 4; ++db)
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-        *reinterpret_cast<f32x4*>(dst + 32 * db + 8 * j) =
-            f32x4{st.acc[db][4 * j], st.acc[db][4 * j + 1], st.acc[db][4 * j + 2], st.acc[db][4 * j + 3]};
-    if (h == 0) A.part_ml[at] = float2{st.m, l};
-    return;
+  const bool part = U.kidx >= 0;  // uniform
+  const int again = lane_again(), row = 32 * w + (again & 31);
+  uint32_t at = 0;  // the row's place in the output or among the partials
+  if (row < nrows) {
+    const int tok = token(row);
+    at = (uint32_t)(part ? A.off[tok] + U.kidx : tok) * P.Hq + (kvh << gs) + (row & ((1 << gs) - 1));
+    if (part && again < 32) A.part_ml[at] = float2{st.m, l};
   }
-  // Outputs leave by way of LDS, whole rows at a time: a row's 16-byte chunk c
-  // at place c ^ (row % 16), a wave's rows in its own part.
-  const float inv = 1.f / l;
   __syncthreads();  // no wave reads K or V any more
   if (!active) return;
-  constexpr int kLanes = WIDE ? 32 : 16, kPer = 64 / kLanes;  // lanes a row, rows an instruction stores
-  uint8_t* rows = lds + w * 32 * 16 * kLanes;
-  const int n = lane & 31;
-#pragma unroll
-  for (int db = 0; db < 4; ++db)
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const f32x4 v = {st.acc[db][4 * j] * inv, st.acc[db][4 * j + 1] * inv, st.acc[db][4 * j + 2] * inv,
-                       st.acc[db][4 * j + 3] * inv};
-      if constexpr (WIDE)
-        *reinterpret_cast<f32x4*>(rows + n * 512 + ((8 * db + 2 * j + h) ^ n) * 16) = v;
-      else
-        *reinterpret_cast<uint2*>(rows + n * 256 + ((4 * db + j) ^ (n & 15)) * 16 + 8 * h) =
-            make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
-    }
-  wait_all();
-#pragma unroll
-  for (int k = 0; k < 32 / kPer; ++k) {
-    const int r = k * kPer + lane / kLanes, c = lane % kLanes;
-    const uint4 v = *reinterpret_cast<const uint4*>(rows + (r * kLanes + (c ^ (r % kLanes))) * 16);
-    const size_t to = (size_t)__shfl((uint32_t)(at >> 32), r) << 32 | (uint32_t)__shfl((uint32_t)at, r);
-    if (32 * w + r < nrows) reinterpret_cast<uint4*>(A.out)[to * kLanes + c] = v;
-  }
+  const float inv = part ? 1.f : 1.f / l;
+  if (WIDE || part)
+    store_rows<float>(lds + w * 16384, st, inv, part ? A.part_acc : static_cast<float*>(A.out), at, min(31, nrows - 1 - 32 * w), again);
+  else
+    store_rows<uint16_t>(lds + w * 8192, st, inv, static_cast<uint16_t*>(A.out), at, min(31, nrows - 1 - 32 * w), again);
 }
 
 // out = sum_k 2^(m_k - M) acc_k / sum_k 2^(m_k - M) l_k, M the largest m_k;
