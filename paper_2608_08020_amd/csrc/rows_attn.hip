@@ -588,7 +588,7 @@ __global__ __launch_bounds__(kThreads, 2) void rows_attn_kernel(DevPool P, RowsL
   auto widen_k = [&](int i, int lane) {  // 16 d of a row -> two chunks of 8
     if (lane < 4) {  // lane 0: K's with the softmax scale; lanes 1 to 3: V's, its log2, its reciprocal
       const float x = lane ? fmaxf(raw_scale, 0x1p-100f) : fmaxf(A.c * raw_scale, 0x1p-120f);
-      scale_s[i % 3][lane][w] = lane == 2 ? __builtin_amdgcn_logf(x) : lane == 3 ? 1.f / x : x;
+      scale_s[i % 3][lane][w] = lane == 2 ? __builtin_amdgcn_logf(x) : lane == 3 ? __builtin_amdgcn_rcpf(x) : x;
     }
 #pragma unroll
     for (int y = 0; y < 2; ++y) {
