@@ -23,25 +23,27 @@
 // A range that is split, or shared by several traces, leaves unnormalised
 // partials that rows_merge_kernel joins by log-sum-exp.
 //
-// Why 128 rows: a key tile's 32 KiB (both operands, bf16) is read from LDS once
-// per 32 rows, 512 matrix cycles a wave, so that four waves of two workgroups
-// keep the CU's four matrix units and its LDS busy together; the 256 registers
-// a lane that two workgroups leave hold the wave's queries (32), outputs (64)
-// and the scores of two tiles (64).  Two buffers of K and of V fill 64 KiB.
+// Why 128 rows: a wave reads a key tile's 32 KiB (both operands, bf16) from LDS
+// for 32 rows, 1024 cycles of its matrix unit; with fewer rows LDS would bound
+// (it is busy 27% of the cycles of a long prompt, the matrix units 52%).  Two
+// workgroups a CU leave 256 registers a lane, which hold the wave's queries (32),
+// outputs (64) and the scores of two tiles (64), and 80 KiB of LDS each: two
+// buffers of K and of V fill 64.
 //
-// What bounds it, measured at 4.76 TB/s for a large copy and 1.25 PFLOP/s for a
-// large library product:
+// What bounds it, measured (a large copy: 4.76 TB/s, a large library product:
+// 1.25 PFLOP/s):
 //   long prompts, bf16: the matrix units and what issues beside them.  One of
-//     8192 tokens, 32 query heads over 8: 493 us, 1.11 PFLOP/s of the visible
-//     half (605 us before the order below was written out)
+//     8192 tokens, 32 query heads over 8: 494 us, 1.11 PFLOP/s of what is seen
+//     (605 us before the order of plain_tile was written out)
 //   long prompts, fp8: the same, and the codes' way to bf16 through registers
 //     and LDS, once per workgroup.  Four of 1024 to 4096 tokens, 64 query heads
-//     over 8: 559 us, 0.84 PFLOP/s
-//   trees and insertions over long contexts: HBM while the rows of a workgroup
-//     are few.  64 trees of eight nodes in fours: 125 us, 661 MB of keys and
-//     values at 5.3 TB/s, the partials' join 7; 128 fp8 trees: the widening,
-//     271 us with the join against 129 for the bytes
-//   a prompt of 17 tokens: one workgroup's start, chain of loads and end: 8.5 us
+//     over 8: 535 us, 0.88 PFLOP/s
+//   short prompts: a workgroup's start, masked tile and end, half of its time at
+//     five tiles.  Sixteen of 256 to 1024 tokens: 113 us, 0.61 PFLOP/s
+//   trees and inserted tokens over long contexts: HBM while a workgroup's rows are
+//     few.  64 trees of eight nodes, four to a prefix: 661 MB in 121 us, 5.4 TB/s;
+//     128 fp8 trees: the tiles' widening and products, 242 us, 0.66 PFLOP/s
+//   a prompt of 17 tokens: 7.2 us of loads one after another, one tile and the end
 #include <cmath>
 
 #include "lds_dma.h"
@@ -821,6 +823,8 @@ __global__ __launch_bounds__(kThreads, 2) void rows_attn_kernel(DevPool P, RowsL
 // eight rows a workgroup, a half-wave a row, four d a lane.  Each lane takes the
 // factors of every 32nd partial, four partials' rows are asked for at a time.
 // A partial without a seen position has m = -inf and counts for nothing.
+// Bound by HBM, for few partials by latency: 3 us for 40 tokens of 32 heads, 7
+// for 512, 22 for 1120 of 64 heads.
 __global__ __launch_bounds__(256) void rows_merge_kernel(RowsLaunch A, int32_t Hq) {
   const int r = blockIdx.x * 8 + (threadIdx.x >> 5), x = threadIdx.x & 31;
   if (r >= A.n_merge * Hq) return;
