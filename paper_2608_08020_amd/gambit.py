@@ -21,6 +21,7 @@ OK, ERR_INVALID, ERR_OUT_OF_BLOCKS, ERR_SHARED_WRITE, ERR_UNSUPPORTED, ERR_DEVIC
     0, -1, -2, -3, -4, -5, -6)
 KV_BF16, KV_FP8_E4M3 = 0, 1
 OUT_BF16, OUT_F32 = 0, 1
+OUT_CODES = {torch.float32: OUT_F32, torch.bfloat16: OUT_BF16}
 NEW_CACHE, NEW_BF16 = 0, 1
 UNIT_NARROW, UNIT_COOP_ONE, UNIT_COOP_TWO, UNIT_TAIL_SLOT, UNIT_NARROW_TWO = 1, 2, 4, 16, 32
 CODE_NAMES = {ERR_INVALID: "INVALID", ERR_OUT_OF_BLOCKS: "OUT_OF_BLOCKS",
@@ -158,8 +159,8 @@ def workspace_size(desc: PoolDesc) -> int:
 
 def _stream(stream=None):
     if stream is None:  # the raw handle: a small call is otherwise a tenth stream objects
-        return ctypes.c_void_p(torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()))
-    return ctypes.c_void_p(stream.cuda_stream)
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+    return stream.cuda_stream
 
 
 def _host_i32(x) -> np.ndarray:
@@ -172,6 +173,11 @@ def _ptr(a: np.ndarray):
     return a.__array_interface__["data"][0]
 
 
+def _in(a: np.ndarray):
+    """A host list as an input argument: short ones as a copy, which is had sooner than an array's address."""
+    return a.tobytes() if a.size <= 1024 else _ptr(a)
+
+
 def _spec(t: torch.Tensor, dtype=None, shape=None, what: str = "tensor"):
     """Check a tensor argument's dtype(s), shape and contiguity.  The kernels
     trust these sizes (the C ABI takes bare pointers), so every device
@@ -182,7 +188,7 @@ def _spec(t: torch.Tensor, dtype=None, shape=None, what: str = "tensor"):
         ok = t.dtype in dtype if isinstance(dtype, tuple) else t.dtype == dtype
         if not ok:
             raise ValueError(f"{what}: expected dtype {dtype}, got {t.dtype}")
-    if shape is not None and tuple(t.shape) != tuple(shape):
+    if shape is not None and t.shape != (shape if type(shape) is tuple else tuple(shape)):
         raise ValueError(f"{what}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
     if not t.is_contiguous():
         raise ValueError(f"{what}: expected a contiguous tensor")
@@ -193,7 +199,7 @@ def _dev(t: torch.Tensor, dtype=None, shape=None, what: str = "tensor"):
     _spec(t, dtype, shape, what)
     if not t.is_cuda:
         raise ValueError(f"{what}: expected a device tensor")
-    return ctypes.c_void_p(t.data_ptr())
+    return t.data_ptr()
 
 
 def rank_topk(ids: torch.Tensor, scores: torch.Tensor, keep: int, stream=None) -> torch.Tensor:
@@ -225,8 +231,8 @@ def mlp_score(h: torch.Tensor, w1: torch.Tensor, b1: torch.Tensor, w2: torch.Ten
         raise ValueError("ids: needed when keep > 0")
     if ids is not None:
         _spec(ids, torch.int32, (n,), "ids")
-    m = Mlp(dim, hidden, ACT_RELU if activation == "relu" else ACT_GELU, _dev(w1).value, _dev(b1).value,
-            _dev(w2).value, float(b2))
+    m = Mlp(dim, hidden, ACT_RELU if activation == "relu" else ACT_GELU, _dev(w1), _dev(b1),
+            _dev(w2), float(b2))
     ws_bytes = int(lib().gambit_mlp_workspace_size(n, hidden))
     ws = torch.empty(max(ws_bytes, 4), dtype=torch.uint8, device=h.device)
     scores = torch.empty(n, dtype=torch.float32, device=h.device)
@@ -269,8 +275,8 @@ def mlp_score_static(h: torch.Tensor, w1: torch.Tensor, b1: torch.Tensor, w2: to
         if keep_out is None:
             keep_out = torch.empty(keep, dtype=torch.int32, device=h.device)
         _spec(keep_out, torch.int32, (keep,), "keep_out")
-    m = Mlp(dim, hidden, ACT_RELU if activation == "relu" else ACT_GELU, _dev(w1).value, _dev(b1).value,
-            _dev(w2).value, float(b2))
+    m = Mlp(dim, hidden, ACT_RELU if activation == "relu" else ACT_GELU, _dev(w1), _dev(b1),
+            _dev(w2), float(b2))
     st = lib().gambit_mlp_score_static(n, _dev(h), ctypes.byref(m), _dev(scores_out),
                                        None if ids is None else _dev(ids), keep,
                                        _dev(keep_out) if keep > 0 else None, _stream(stream))
@@ -453,29 +459,32 @@ class Pool:
             if k.dim() != 3:
                 raise ValueError("k: expected [n_rows][Hkv][D]")
         n_rows = total if rows is None else k.shape[0]
-        _spec(k, torch.bfloat16, (n_rows, self.Hkv, self.D), "k")
-        _spec(v, torch.bfloat16, (n_rows, self.Hkv, self.D), "v")
-        self._check(lib().gambit_kv_write_layer(self._h, layer, ids.size, _ptr(ids), _ptr(p0), _ptr(nt),
-                                                None if rows is None else _ptr(rows), n_rows, _dev(k), _dev(v),
+        shape = (n_rows, self.Hkv, self.D)
+        kp, vp = _dev(k, torch.bfloat16, shape, "k"), _dev(v, torch.bfloat16, shape, "v")
+        self._check(lib().gambit_kv_write_layer(self._h, layer, ids.size, _in(ids), _in(p0), _in(nt),
+                                                None if rows is None else _in(rows), n_rows, kp, vp,
                                                 _stream(stream)), "kv_write_layer")
 
-    def _attn_out(self, total: int, q: torch.Tensor, out, out_dtype):
-        """The output of a packed attention call and its code."""
+    def _attn_io(self, total: int, q: torch.Tensor, out, out_dtype):
+        """The queries' address, the output and its code."""
         shape = (total, self.Hq, self.D)
-        _spec(q, torch.bfloat16, shape, "q")
+        qp = _dev(q, torch.bfloat16, shape, "q")
         if out is None:
-            out = torch.empty(shape, dtype=out_dtype, device=q.device)
-        _spec(out, (torch.float32, torch.bfloat16), shape, "out")
-        return out, OUT_F32 if out.dtype == torch.float32 else OUT_BF16
+            out = torch.empty_like(q) if out_dtype is torch.bfloat16 else torch.empty_like(q, dtype=out_dtype)
+        else:
+            _spec(out, None, shape, "out")
+        if out.dtype not in OUT_CODES:
+            raise ValueError(f"out: expected dtype {tuple(OUT_CODES)}, got {out.dtype}")
+        return qp, out, OUT_CODES[out.dtype]
 
     def prompt_attn(self, layer: int, ids, n_tokens, q: torch.Tensor, out: torch.Tensor | None = None,
                     out_dtype=torch.bfloat16, sm_scale=None, stream=None) -> torch.Tensor:
         """gambit_prompt_attn: causal attention of each trace's last n_tokens[i] positions over layer `layer`'s
         cache; q and out [total][Hq][D], packed in list order."""
         ids, nt, total = self._packed(ids, n_tokens, "n_tokens")
-        out, od = self._attn_out(total, q, out, out_dtype)
+        qp, out, od = self._attn_io(total, q, out, out_dtype)
         sm = float(self.D ** -0.5 if sm_scale is None else sm_scale)
-        self._check(lib().gambit_prompt_attn(self._h, layer, ids.size, _ptr(ids), _ptr(nt), _dev(q), _dev(out), od, sm,
+        self._check(lib().gambit_prompt_attn(self._h, layer, ids.size, _in(ids), _in(nt), qp, _dev(out), od, sm,
                                              _stream(stream)), "prompt_attn")
         return out
 
@@ -487,12 +496,12 @@ class Pool:
         up = _host_i32(parents)
         if up.shape != (total,):
             raise ValueError(f"parents: expected {total}, got {up.shape}")
-        out, od = self._attn_out(total, q, out, out_dtype)
-        _spec(k_new, torch.bfloat16, (total, self.Hkv, self.D), "k_new")
-        _spec(v_new, torch.bfloat16, (total, self.Hkv, self.D), "v_new")
+        qp, out, od = self._attn_io(total, q, out, out_dtype)
+        shape = (total, self.Hkv, self.D)
+        kp, vp = _dev(k_new, torch.bfloat16, shape, "k_new"), _dev(v_new, torch.bfloat16, shape, "v_new")
         sm = float(self.D ** -0.5 if sm_scale is None else sm_scale)
-        self._check(lib().gambit_tree_attn(self._h, layer, ids.size, _ptr(ids), _ptr(nn), _ptr(up), _dev(q),
-                                           _dev(k_new), _dev(v_new), _dev(out), od, sm, _stream(stream)), "tree_attn")
+        self._check(lib().gambit_tree_attn(self._h, layer, ids.size, _in(ids), _in(nn), _in(up), qp, kp, vp,
+                                           _dev(out), od, sm, _stream(stream)), "tree_attn")
         return out
 
     def score_prune_branch(self, ids, h: torch.Tensor, w: torch.Tensor, b: float, keep: int,
