@@ -95,6 +95,9 @@ void dump_rows(gambit_pool* p, int st, int total, int launched) {
         << u.listed << "," << u.pos0 << "," << u.kidx << "," << u.draft << "," << u.ndraft << "]";
     }
     o << "]";
+    std::vector<int32_t> first;
+    for (int i = 0; i < A.n_items; ++i) first.insert(first.end(), A.items[i].first, A.items[i].first + 4);
+    print_list(o, "first", first.data(), first.size());
     print_list(o, "list", A.list, listed);
     print_list(o, "off", A.off, total);
     print_list(o, "nk", A.nk, total);

@@ -82,6 +82,10 @@ def check_plan(plan, rows, ids, counts, g, length, ups=None):
             if draft >= 0:
                 assert (draft, ndraft) == (base_of[t], size_of[t])
                 drafts[t] += 1
+    for k, (trace, jb0, end, _, _, listed, _, kidx, draft, _) in enumerate(plan["items"]):
+        assert not listed or (kidx >= 0 and draft < 0)
+        if end > 16 * jb0:
+            assert plan["first"][4 * k:4 * k + 4] == [rows[trace][min(jb0 + b, (end - 1) // 16)] for b in range(4)]
     spans = []
     for t in range(N):
         at = 0
