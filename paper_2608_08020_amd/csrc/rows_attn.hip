@@ -573,7 +573,7 @@ __global__ __launch_bounds__(kThreads, 2) void rows_attn_kernel(DevPool P, RowsL
     if constexpr (FP8) {
       raw_k[0] = load16(src + lane * 16, U.once);
       raw_k[1] = load16(src + lane * 16 + 1024, U.once);
-      if (lane < 4) raw_scale = P.kv_scale[2 * (size_t)id + min(lane, 1)];
+      raw_scale = P.kv_scale[2 * (size_t)id + min(lane, 1)];
     } else {
       dma16x4(src, lane * 16, kbuf(i) + k_block_at(w), U.once);
     }
@@ -588,10 +588,10 @@ __global__ __launch_bounds__(kThreads, 2) void rows_attn_kernel(DevPool P, RowsL
     }
   };
   auto widen_k = [&](int i, int lane) {  // 16 d of a row -> two chunks of 8
-    if (lane < 4) {  // lane 0: K's with the softmax scale; lanes 1 to 3: V's, its log2, its reciprocal
-      const float x = lane ? fmaxf(raw_scale, 0x1p-100f) : fmaxf(A.c * raw_scale, 0x1p-120f);
-      scale_s[i % 3][lane][w] = lane == 2 ? __builtin_amdgcn_logf(x) : lane == 3 ? __builtin_amdgcn_rcpf(x) : x;
-    }
+    // lane 0: K's with the softmax scale; lanes 1 to 3: V's, its log2, its reciprocal
+    const float x = fmaxf(lane ? raw_scale : A.c * raw_scale, lane ? 0x1p-100f : 0x1p-120f);
+    const float y = lane == 2 ? __builtin_amdgcn_logf(x) : lane == 3 ? __builtin_amdgcn_rcpf(x) : x;
+    if (lane < 4) scale_s[i % 3][lane][w] = y;
 #pragma unroll
     for (int y = 0; y < 2; ++y) {
       uint8_t* k = kbuf(i) + k_block_at(w) + (2 * (4 * y + (lane >> 4)) * kBlock + (lane & 15)) * 16;
