@@ -111,13 +111,15 @@ struct Plan {
 // Positions of a chunk at least: below that a workgroup's start and its
 // partial rows cost more than its keys.
 constexpr int kLeastChunk = 256;
-// Workgroups a call is cut into, as a multiple of those the chip runs at once.
-// More rounds share the chip more evenly but start more often and leave more
-// partials: 64 trees of eight nodes 156, 165, 177, 186 us with 1, 1.5, 2, 3
-// rounds; sixteen long trees 297, 319, 309, 318; insertions into 64 traces 284,
-// 283, 288, 296.  Choosing the rounds per call by the estimated length of the
-// longest-first schedule moved these by -1 to +4%.
-constexpr double kRounds = 1.0;
+// Workgroups a call is cut into: as many as the chip runs at once.  More rounds
+// share the chip more evenly but start more often and leave more partials: 64
+// trees of eight nodes 156, 165, 177, 186 us with 1, 1.5, 2, 3 rounds; sixteen long
+// trees 297, 319, 309, 318; insertions into 64 traces 284, 283, 288, 296.
+// Choosing the rounds per call by the estimated length of the longest-first
+// schedule moved these by -1 to +4%.  Where all of a call fits one round, its
+// chunks are the shortest that one round holds (the sixteen trees 290 -> 276 us);
+// where it does not, they are cut to about the even share, no shorter (at most that
+// share: the 64 trees 130 -> 134, the insertions 252 -> 254).
 
 struct Run {
   int j0, j1;                    // blocks
@@ -162,13 +164,17 @@ void shared_runs(gambit_pool* p, std::vector<Listed>& L, const std::vector<char>
   for (int b : touched) p->cnt[b] = 0;
 }
 
-// Chunks of `tokens` positions for a target length.
-int chunks_of(int64_t tokens, int64_t target) {
-  return (int)std::max<int64_t>(1, (tokens + target / 2) / target);
-}
+// The length of a chunk: about `target` positions, or `most` at most.
+struct Cut {
+  int64_t target;
+  bool most;
+  int chunks(int64_t tokens) const {
+    return (int)std::max<int64_t>(1, (tokens + (most ? target - 1 : target / 2)) / target);
+  }
+};
 
 bool try_plan(gambit_pool* p, const std::vector<Listed>& L, const std::vector<Run>& runs,
-              const std::vector<std::vector<int32_t>>& runs_of, bool tree, int64_t target, Plan* out) {
+              const std::vector<std::vector<int32_t>>& runs_of, bool tree, Cut cut, Plan* out) {
   const int tile = gambit::kRowsTile / p->g;  // tokens of a tile
   *out = Plan{};
   int N = 0;
@@ -177,7 +183,7 @@ bool try_plan(gambit_pool* p, const std::vector<Listed>& L, const std::vector<Ru
   out->nk.assign(N, 0);
   // chunks of the shared runs, the same for all of a run's members
   std::vector<int> run_chunks(runs.size());
-  for (size_t r = 0; r < runs.size(); ++r) run_chunks[r] = chunks_of(16LL * (runs[r].j1 - runs[r].j0), target);
+  for (size_t r = 0; r < runs.size(); ++r) run_chunks[r] = cut.chunks(16LL * (runs[r].j1 - runs[r].j0));
   std::vector<int> before(L.size(), 0);  // a trace's partials over its shared runs
   std::vector<std::vector<int32_t>> run_kidx(runs.size());
   for (size_t i = 0; i < L.size(); ++i)
@@ -205,7 +211,7 @@ bool try_plan(gambit_pool* p, const std::vector<Listed>& L, const std::vector<Ru
       const int ntok = std::min(tile, x.m - a);
       const int end = tree ? x.ctx : x.ctx + a + ntok;
       const int64_t tokens = std::max(0, end - 16 * x.priv);
-      int nch = chunks_of(tokens, target);
+      int nch = cut.chunks(tokens);
       nch = std::min(nch, std::max(1, cdiv((int)tokens, gambit::kKeyTile)));
       const int nk = before[i] + nch;
       for (int t = a; t < a + ntok; ++t) {
@@ -266,31 +272,46 @@ gambit_status plan_rows(gambit_pool* p, std::vector<Listed> L, bool tree, const 
   std::vector<Run> runs;
   std::vector<std::vector<int32_t>> runs_of(L.size());
   shared_runs(p, L, share, &runs, &runs_of);
-  // positions that the tiles go over, summed
-  auto work = [&]() {
-    int64_t w = 0;
+  // f(row tiles, positions) of every range
+  auto ranges = [&](auto&& f) {
     for (const Listed& x : L)
       for (int a = 0; a < x.m; a += tile)
-        w += std::max(0, (tree ? x.ctx : x.ctx + std::min(x.m, a + tile)) - 16 * x.priv) + gambit::kKeyTile;
+        f(1, std::max(0, (tree ? x.ctx : x.ctx + std::min(x.m, a + tile)) - 16 * x.priv));
     for (const Run& R : runs) {
       int m = 0;
       for (int i : R.members) m += L[i].m;
-      w += 16LL * (R.j1 - R.j0) * cdiv(m, tile);
+      f(cdiv(m, tile), 16 * (R.j1 - R.j0));
     }
-    return w * p->d.num_kv_heads;
   };
+  const int64_t round = 2 * p->n_cu, heads = p->d.num_kv_heads;
+  auto groups = [&](Cut cut) {
+    int64_t n = 0;
+    ranges([&](int tiles, int tokens) { n += tiles * cut.chunks(tokens); });
+    return n * heads;
+  };
+  int64_t work = 0;  // positions that the row tiles go over; a tile of drafts, or a masked one, with every trace's
+  ranges([&](int tiles, int tokens) { work += (int64_t)tiles * tokens; });
+  for (const Listed& x : L) work += (int64_t)gambit::kKeyTile * cdiv(x.m, tile);
   Plan plan;
-  int64_t target = std::max<int64_t>(kLeastChunk, (int64_t)(work() / (kRounds * 2 * p->n_cu)));
-  bool ok = try_plan(p, L, runs, runs_of, tree, target, &plan);
-  while (!ok && target < (1LL << 31)) {
-    target *= 2;
-    ok = try_plan(p, L, runs, runs_of, tree, target, &plan);
+  Cut cut{std::max<int64_t>(kLeastChunk, work * heads / round), groups(Cut{1LL << 40, true}) <= round};
+  if (cut.most && groups(cut) > round) {
+    int64_t lo = cut.target, hi = 1LL << 31;
+    while (hi - lo > gambit::kKeyTile) {
+      const int64_t mid = (lo + hi) / 2;
+      (groups(Cut{mid, true}) <= round ? hi : lo) = mid;
+    }
+    cut.target = hi;
+  }
+  bool ok = try_plan(p, L, runs, runs_of, tree, cut, &plan);
+  while (!ok && cut.target < (1LL << 31)) {
+    cut.target *= 2;
+    ok = try_plan(p, L, runs, runs_of, tree, cut, &plan);
   }
   if (!ok) {  // every trace by itself, in one piece: no partials
     for (Listed& x : L) x.priv = 0;
     runs.clear();
     for (auto& r : runs_of) r.clear();
-    ok = try_plan(p, L, runs, runs_of, tree, 1LL << 40, &plan);
+    ok = try_plan(p, L, runs, runs_of, tree, Cut{1LL << 40, true}, &plan);
   }
   if (!ok) return fail(p, GAMBIT_ERR_UNSUPPORTED, "plan exceeds workspace bounds");
   for (RowItem& it : plan.items)
