@@ -90,9 +90,9 @@ __device__ inline void dma16x4(const uint8_t* base, uint32_t off, uint8_t* l, bo
   asm volatile(                                                  \
       "s_mov_b32 %0, m0\n\ts_mov_b32 m0, %3\n\ts_nop 0\n\t"     \
       "global_load_lds_dwordx4 %1, %2" hint "\n\t"               \
-      "global_load_lds_dwordx4 %1, %2 offset:1024" hint "\n\t"   \
-      "global_load_lds_dwordx4 %1, %2 offset:2048" hint "\n\t"   \
-      "global_load_lds_dwordx4 %1, %2 offset:3072" hint "\n\t"   \
+      "global_load_lds_dwordx4 %1, %2 offset:0x400" hint "\n\t"   \
+      "global_load_lds_dwordx4 %1, %2 offset:0x800" hint "\n\t"   \
+      "global_load_lds_dwordx4 %1, %2 offset:0xc00" hint "\n\t"   \
       "s_nop 0\n\ts_mov_b32 m0, %0"                              \
       : "=&s"(save)                                              \
       : "v"(off), "s"(sb), "s"(at)                               \
