@@ -822,7 +822,9 @@ __global__ __launch_bounds__(kThreads, 2) void rows_attn_kernel(DevPool P, RowsL
 // out = sum_k 2^(m_k - M) acc_k / sum_k 2^(m_k - M) l_k, M the largest m_k;
 // eight rows a workgroup, a half-wave a row, four d a lane.  Each lane takes the
 // factors of every 32nd partial, four partials' rows are asked for at a time.
-// A partial without a seen position has m = -inf and counts for nothing.
+// A partial without a seen position has m = -inf and sums of zero.  A factor of
+// zero still meets the partial's sums: where a V that its rows see is not finite
+// they are not, and so is the result, as in a range that was not cut.
 // Bound by HBM, for few partials by latency: 3 us for 40 tokens of 32 heads, 7
 // for 512, 22 for 1120 of 64 heads.
 __global__ __launch_bounds__(256) void rows_merge_kernel(RowsLaunch A, int32_t Hq) {
@@ -857,9 +859,9 @@ __global__ __launch_bounds__(256) void rows_merge_kernel(RowsLaunch A, int32_t H
         a[y] = *reinterpret_cast<const f32x4*>(A.part_acc + (p0 + (size_t)(k0 + min(k + y, m - 1)) * Hq) * kHeadDim + 4 * x);
 #pragma unroll
       for (int y = 0; y < 4; ++y) {
-        const float g = k + y < m ? __shfl(f, (threadIdx.x & 32) + k + y) : 0.f;
+        const float g = __shfl(f, (threadIdx.x & 32) + k + y);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) o[e] = g == 0.f ? o[e] : fmaf(g, a[y][e], o[e]);
+        for (int e = 0; e < 4; ++e) o[e] = k + y < m ? fmaf(g, a[y][e], o[e]) : o[e];
       }
     }
   }
