@@ -254,7 +254,9 @@ gambit_status gambit_kv_write_layer(gambit_pool* pool, int32_t layer, int32_t n,
  * K and V past a token's own position do not reach its output, whatever they
  * hold.  Blocks that several listed traces share before their tokens are read
  * once for all of them when the traces have few tokens (up to 256 / (Hq / Hkv)
- * each).  A row whose scores are all -inf, or one of them NaN, is NaN.
+ * each).  A row whose scores are all -inf, or one of them NaN, is NaN.  Where
+ * the V of a position is not finite, that element of every row that sees the
+ * position is not finite, whatever its weight.
  *   trace_ids, n_tokens  host [n]
  *   q         device [total][Hq][head_dim] bf16
  *   out       device [total][Hq][head_dim], bf16 or fp32 (out_dtype)

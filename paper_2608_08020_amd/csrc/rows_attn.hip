@@ -370,17 +370,17 @@ __device__ inline void plain_tile(const uint8_t* v, const uint8_t* k_next, const
 }
 
 // Adds the values of one kind (0: +inf, 1: -inf, 2: NaN) in a block's V to the
-// rows that have a weight for them: the product of the weights with ones where
-// the values are.
-__device__ inline void add_not_finite(const uint4 (&v)[4], bf16x8 p, int kind, Rows& st) {
+// rows that see them, whatever their weights: the product of `seen`, ones where
+// the row sees the token, with ones where the values are.
+__device__ inline void add_not_finite(const uint4 (&v)[4], bf16x8 seen, int kind, Rows& st) {
   const uint32_t what = kind == 2 ? 0x7fc00000u : kind ? 0xff800000u : 0x7f800000u;
 #pragma unroll
   for (int db = 0; db < 4; ++db) {
     const uint4 a = each(v[db], [&](uint32_t x) { return ones_of(x, kind); });
-    const f32x16 n = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), p, f32x16{}, 0, 0, 0);
+    const f32x16 n = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), seen, f32x16{}, 0, 0, 0);
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
-      uint32_t add = what & (uint32_t)(-__float_as_int(n[r]) >> 31);  // where the weights' sum is not zero
+      uint32_t add = what & (uint32_t)(-__float_as_int(n[r]) >> 31);  // where the row sees one
       asm("" : "+v"(add));  // the source's arithmetic is compiled as if NaN did not occur
       st.acc[db][r] += __uint_as_float(add);
     }
@@ -432,10 +432,11 @@ __device__ inline void last_tile(const uint8_t* v, const Factors& f, const Score
 
 // The same for a tile whose V holds infinities or NaN that not every row sees:
 // where a row's weight is zero the product would make them NaN, so they are
-// zeros in the product and go to the rows with a weight for them beside it.
+// zeros in the product and go to the rows that see them (bits of `vis`) beside it.
 template <bool FP8, bool WIDE>
-__device__ inline void slow_tile(const uint8_t* vt, const Factors& f, const Scores& x, Rows& st) {
+__device__ inline void slow_tile(const uint8_t* vt, const Factors& f, const Scores& x, uint64_t vis, int lane, Rows& st) {
   const float nm = reference(st);
+  vis >>= 8 * (lane >> 5);
 #pragma unroll
   for (int b = 0; b < 4; ++b) {
     uint32_t p[WIDE ? 3 : 1][4];
@@ -447,8 +448,14 @@ __device__ inline void slow_tile(const uint8_t* vt, const Factors& f, const Scor
     uint4 v[4];
 #pragma unroll
     for (int db = 0; db < 4; ++db) v[db] = __builtin_bit_cast(uint4, v_operand(vt, b, db));
+    uint32_t seen[4];  // ones (bf16) of the lane's eight tokens
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const uint32_t two = (uint32_t)(vis >> (16 * b + 2 * j));
+      seen[j] = (two & 1) * 0x3f80u | (two >> 1 & 1) * 0x3f800000u;
+    }
 #pragma unroll 1
-    for (int kind = 0; kind < 3; ++kind) add_not_finite(v, operand(p[0]), kind, st);
+    for (int kind = 0; kind < 3; ++kind) add_not_finite(v, operand(seen), kind, st);
 #pragma unroll
     for (int db = 0; db < 4; ++db) {
       v[db] = each(v[db], [](uint32_t y) { return y & ~widen_flags(not_finite2(y)); });
@@ -753,16 +760,20 @@ __global__ __launch_bounds__(kThreads, 2) void rows_attn_kernel(DevPool P, RowsL
     const bool check = settle(i);
     const int lane = lane_again();
     begin(i, lane);
+    auto seen = [&](int lane) {  // tokens of the tile that the lane's row sees
+      const int lim = limit(min(32 * w + (lane & 31), nrows - 1));
+      return lim - tb <= 0 ? 0 : ~0ull >> (64 - min(lim - tb, 64));
+    };
     if (i < nt) {
       if (tb + kKeyTile > lim_lo) {
-        const int lim = limit(min(32 * w + (lane & 31), nrows - 1));
-        mask_scores(lim - tb <= 0 ? 0 : ~0ull >> (64 - min(lim - tb, 64)), lane, x);
+        mask_scores(seen(lane), lane, x);
         mx = tile_max<FP8>(x, factors(i));
       }
       const bool more = i + 1 < nt;
       if (check && is_bad(i)) {
         rescale(mx, st);
-        slow_tile<FP8, WIDE>(vbuf(i) + lane * 16, factors(i), x, st);
+        const int lane = lane_again();
+        slow_tile<FP8, WIDE>(vbuf(i) + lane * 16, factors(i), x, seen(lane), lane, st);
       } else if (!WIDE && more) {
         if constexpr (!WIDE) plain(i, lane, x, y);
         x = y;
@@ -788,11 +799,15 @@ __global__ __launch_bounds__(kThreads, 2) void rows_attn_kernel(DevPool P, RowsL
       if (active) {
         const Factors one = factors(0);
         qk(kbuf(0) + k_lane(lane), q, x);
-        const int lane = lane_again(), row = 32 * w + (lane & 31);
-        mask_scores(row < nrows ? A.anc[U.tok + (row >> gs)] : 1, lane, x);  // a tree's rows are not listed
+        auto seen = [&](int lane) {  // a tree's rows are not listed
+          const int row = 32 * w + (lane & 31);
+          return row < nrows ? A.anc[U.tok + (row >> gs)] : 1;
+        };
+        const int lane = lane_again();
+        mask_scores(seen(lane), lane, x);
         rescale(tile_max<FP8>(x, one), st);
         if (is_bad(0))
-          slow_tile<FP8, WIDE>(vbuf(0) + lane * 16, one, x, st);
+          slow_tile<FP8, WIDE>(vbuf(0) + lane * 16, one, x, seen(lane), lane, st);
         else
           last_tile<FP8, WIDE>(vbuf(0) + lane * 16, one, x, st);
       }

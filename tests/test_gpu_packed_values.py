@@ -32,8 +32,9 @@ def _without(out, V, d):
     return out, V
 
 
-# 200: a token of a tile that every row sees; 3000: chunks of 256 positions, the first ones with no other weight
-@pytest.mark.parametrize("n,low,at", [(200, 11, 10), (200, 199, 190), (3000, 1500, 700)])
+# 40: one tile that no row sees whole; 200: a token of a tile that every row sees; 3000: chunks of 256 positions,
+# the first ones with no other weight
+@pytest.mark.parametrize("n,low,at", [(40, 11, 10), (200, 11, 10), (200, 199, 190), (3000, 1500, 700), (3000, 2990, 2985)])
 @pytest.mark.parametrize("bad", [math.inf, math.nan])
 @pytest.mark.parametrize("out_dtype", OUT)
 @pytest.mark.parametrize("tree", [False, True])
@@ -60,7 +61,7 @@ def test_a_value_that_is_not_finite_reaches_every_row_that_sees_it(n, low, at, b
     _check(out, q, K, V, sees)
 
 
-@pytest.mark.parametrize("n,low,at", [(3000, 1500, 700)])
+@pytest.mark.parametrize("n,low,at", [(40, 11, 10), (3000, 1500, 700)])
 @pytest.mark.parametrize("out_dtype", OUT)
 def test_a_nan_value_of_an_fp8_pool_reaches_every_row_that_sees_it(n, low, at, out_dtype):
     S = Kept(16, 2, T=2, maxb=200, fp8=True)
@@ -74,3 +75,26 @@ def test_a_nan_value_of_an_fp8_pool_reaches_every_row_that_sees_it(n, low, at, o
     assert torch.isnan(out[:, :8, d].double()).all()
     out, V = _without(out, S.V[1], d)
     _check(out, q, S.K[1], V, _causal(n, m))
+
+
+@pytest.mark.parametrize("bad", [math.inf, math.nan])
+@pytest.mark.parametrize("out_dtype", OUT)
+def test_a_draft_that_is_not_finite_reaches_its_branch_and_no_other(bad, out_dtype):
+    S = Kept(8, 2, T=2, maxb=20)
+    n, d = 70, 3
+    S.extend([1], [n])
+    up = [-1, 0, 1, -1, 3, 2]
+    seen, free = [0, 1, 2, 5], [3, 4]
+    q = _queries(S, 6, seen)
+    kn, vn = S.normal(6, 2, D), S.normal(6, 2, D)
+    kn[0, 0, 5] = LOW
+    vn[0, 0, d] = bad
+    out = S.pool.tree_attn(0, [1], [6], up, q, kn, vn, out_dtype=out_dtype)
+    assert not torch.isfinite(out[seen, :4, d].double()).any()
+    K, V = torch.cat([S.K[1], kn.double()]), torch.cat([S.V[1], vn.double()])
+    sees = torch.cat([torch.ones(6, n, dtype=torch.bool, device=DEV), _kin(up)], 1)
+    clean = V.clone()
+    clean[n, 0, d] = 0.0                               # nodes 3 and 4 do not see it
+    _check(out[free], q[free], K, clean, sees[free])
+    out, V = _without(out, V, d)
+    _check(out, q, K, V, sees)
