@@ -235,13 +235,13 @@ gambit_status gambit_decode_attn_layer(gambit_pool* pool, int32_t layer, int32_t
  *             for token i, n_rows = total tokens
  * A bf16 pool stores the values.  An fp8 pool quantises them as gambit_decode_
  * attn_layer does (nearest E4M3FN value of x / s, ties to the even code,
- * saturating; NaN stays NaN).  A block whose first position is written takes
- * its scales from the call: for K and for V the largest magnitude written into
- * the block, over its tokens and KV heads (infinities as the largest finite
- * value), / 448, and at least 2^-20, or at least fp8_append_scale when the
- * write ends inside the block (later tokens are quantised with that scale).
- * Values of the block's other positions are lost.  Other blocks keep their
- * scales. */
+ * saturating; NaN stays NaN; zero stays zero, also for a scale of zero).  A
+ * block whose first position is written takes its scales from the call: for K
+ * and for V the largest magnitude written into the block, over its tokens and
+ * KV heads (infinities as the largest finite value), / 448, and at least
+ * 2^-20, or at least fp8_append_scale when the write ends inside the block
+ * (later tokens are quantised with that scale).  Values of the block's other
+ * positions are lost.  Other blocks keep their scales. */
 gambit_status gambit_kv_write_layer(gambit_pool* pool, int32_t layer, int32_t n, const int32_t* trace_ids,
                                     const int32_t* pos0, const int32_t* n_tokens, const int32_t* rows,
                                     int32_t n_rows, const void* k, const void* v, void* stream);

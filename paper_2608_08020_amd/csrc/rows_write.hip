@@ -22,7 +22,8 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 // x / s rounded to fp32, r = 1 / s rounded: a product with the reciprocal and
 // one correction by the exact remainder is the rounded quotient (Markstein's
 // theorem).  Quotients beyond E4M3FN's range saturate whatever their last bits,
-// and so small ones that the remainder underflows have code zero.
+// and so small ones that the remainder underflows have code zero.  (The
+// caller keeps the reciprocal inside fp32.)
 __device__ inline float quotient(float x, float s, float r) {
   const float q = x * r, e = fmaf(-q, s, x);
   return fabsf(q) < 512.f ? fmaf(e, r, q) : q;
@@ -158,14 +159,28 @@ __global__ __launch_bounds__(256) void rows_write_fp8_kernel(DevPool P, WriteLau
   } else {
     s = *scale_at;
   }
-  const float r = 1.f / s;
+  // a scale near zero and the values both times 2^64 (exact, or beyond where the
+  // quotient saturates); of a scale of zero, zero stays zero and the rest saturates
+  const bool tiny = fabsf(s) < 0x1p-64f;  // uniform
+  if (tiny) s *= 0x1p64f;
+  const float r = fminf(1.f / s, 0x1.fffffep127f);
   auto q = [&](float y) { return quotient(y, s, r); };
+  auto grown = [](uint32_t w) {
+    return __float_as_uint(bf16_lo(w) * 0x1p64f) >> 16 | (__float_as_uint(bf16_hi(w) * 0x1p64f) & 0xffff0000u);
+  };
   uint8_t* cache = (is_v ? P.v_cache : P.k_cache) + (size_t)U.blk * P.Hkv * kTile;
   for (int h0 = 0; h0 < P.Hkv; h0 += kHeads) {
     const int nh = min(kHeads, P.Hkv - h0);
     if (h0) {
       __syncthreads();  // the heads before are stored
       load(h0);
+    }
+    if (tiny) {
+#pragma unroll
+      for (int i = 0; i < 2 * kPasses; ++i) {
+        uint4& y = x[i / 2][i % 2];
+        y = make_uint4(grown(y.x), grown(y.y), grown(y.z), grown(y.w));
+      }
     }
 #pragma unroll
     for (int i = 0; i < kPasses; ++i) {

@@ -1,4 +1,4 @@
-"""Packed tokens on the GPU: values that are not finite.
+"""Packed tokens on the GPU: values that are not finite, and block scales of zero or next to it.
 
 A position that a row sees counts for it whatever its weight: where its V is
 not finite, that element of the row's output is not, however small the weight,
@@ -7,10 +7,11 @@ that a row does not see never counts.
 """
 import math
 
+import numpy as np
 import pytest
 import torch
 
-from test_gpu_packed import D, DEV, OUT, Kept, _causal, _check, _kin
+from test_gpu_packed import D, DEV, OUT, Kept, _causal, _check, _k_phys, _kin
 
 pytestmark = pytest.mark.gpu
 
@@ -98,3 +99,33 @@ def test_a_draft_that_is_not_finite_reaches_its_branch_and_no_other(bad, out_dty
     _check(out[free], q[free], K, clean, sees[free])
     out, V = _without(out, V, d)
     _check(out, q, K, V, sees)
+
+
+# ------------------------------------------------------------ block scales next to zero --
+@pytest.mark.parametrize("scale", [0.0, 1e-44, 1e-39, 2.0 ** -128, 2.0 ** -127, 2.0 ** -100])
+@pytest.mark.parametrize("Hkv", [2, 12])
+def test_write_into_a_begun_block_of_a_tiny_scale(Hkv, scale):
+    """Codes of x / s (fp32 quotient) for scales whose reciprocal is beyond fp32; zero stays zero for any scale."""
+    n, a = 9, 4
+    S = Kept(Hkv, Hkv, T=2, maxb=2, fp8=True)
+    S.pool.kv_alloc([0], [a + n])
+    S.pool.kv_scale.fill_(scale)
+    s = np.float32(scale)
+    k, v = S.normal(n, Hkv, D), S.normal(n, Hkv, D)
+    for x in (k, v):
+        x[:, :, ::4] = 0.0
+        x[:, :, 1::8] *= 2.0 ** -126                   # quotients inside E4M3FN's range
+    S.pool.kv_write_layer(0, [0], [a], [n], k, v)
+    b = int(S.pool.block_table[0, 0])
+    t = np.arange(a, a + n)
+    d = np.arange(D)
+    for i, (x, cache) in enumerate(((k, S.pool.k_cache), (v, S.pool.v_cache))):
+        y = x.float().cpu().numpy()
+        with np.errstate(divide="ignore", invalid="ignore", over="ignore"):
+            y = np.where(y == 0, y, y / s)
+        want = torch.from_numpy(np.clip(y, -448, 448)).to(torch.float8_e4m3fn).float()
+        idx = ((d // 16) * 16 + _k_phys(t)[:, None]) * 16 + d % 16 if i == 0 else d * 16 + t[:, None]
+        got = cache[b].reshape(Hkv, -1)[:, torch.from_numpy(idx).to(DEV)].permute(1, 0, 2).cpu()
+        got = got.contiguous().view(torch.float8_e4m3fn).float()
+        assert torch.equal(got, want), (i, int((got != want).sum()))
+        assert (S.pool.kv_scale[b].cpu().numpy() == s).all()
