@@ -213,8 +213,10 @@ gambit_status gambit_decode_attn_layer(gambit_pool* pool, int32_t layer, int32_t
  *     per layer l:  gambit_tree_attn(l, ...)          drafts stay outside the pool
  *     gambit_kv_alloc(traces, accepted)
  *     per layer l:  gambit_kv_write_layer(l, ..., rows of the accepted drafts)
- * Calls that list the same while the pool does not change (the layers of a
- * step) share one plan, made by the first.  Device buffers are 16-byte
+ * The pool keeps the last plan of each kind of call (write, prompt, tree); calls
+ * that list what the last one of their kind listed, with no length or table
+ * changed since (the layers of a step), use it.  Any other call makes a plan on
+ * the host, after the upload of its kind's last one has ended.  Device buffers are 16-byte
  * aligned and contiguous; inputs and outputs do not overlap.  At most
  * GAMBIT_MAX_PACKED tokens a call (fewer for a pool that cannot hold as many:
  * 16 max_traces max_blocks_per_trace positions, or 64 nodes a slot).  A

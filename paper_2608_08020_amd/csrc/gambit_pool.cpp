@@ -104,12 +104,17 @@ bool layout_of(const gambit_pool_desc* d, Layout* L) {
   L->tourn = take(4 * ((size_t)gambit::kTournHeader + 3 * (size_t)T));
   const size_t held = (size_t)T * d->max_blocks_per_trace * 16;
   L->max_packed = (int)std::min<size_t>(GAMBIT_MAX_PACKED, std::max<size_t>(held, (size_t)T * gambit::kMaxNodes));
-  L->max_items = L->max_packed / (gambit::kRowsTile / g) + 2 * T + L->max_parts;
-  L->rows_plan_bytes = align_up(sizeof(gambit::RowItem) * (size_t)L->max_items) + align_up(8 * (size_t)L->max_packed) +
-                       3 * align_up(4 * (size_t)L->max_packed) + align_up(4 * (size_t)L->max_parts);
+  for (int kind : {kPromptPlan, kTreePlan}) {
+    const bool tree = kind == kTreePlan;
+    const size_t tokens = tree ? std::min<size_t>(L->max_packed, (size_t)T * gambit::kMaxNodes) : L->max_packed;
+    L->max_items[kind] = (int)tokens / (gambit::kRowsTile / g) + 2 * T + L->max_parts;
+    L->rows_plan_bytes[kind] = align_up(sizeof(gambit::RowItem) * (size_t)L->max_items[kind]) +
+                               align_up(4 * (size_t)L->max_parts) + 3 * align_up(4 * tokens) +
+                               (tree ? align_up(8 * tokens) : 0);
+  }
   L->write_plan_bytes = align_up(sizeof(gambit::WriteItem) * ((size_t)L->max_packed / 16 + 2 * (size_t)T)) +
                         align_up(4 * (size_t)L->max_packed);
-  L->rows_plan = take(L->rows_plan_bytes);
+  for (int kind : {kPromptPlan, kTreePlan}) L->rows_plan[kind] = take(L->rows_plan_bytes[kind]);
   L->write_plan = take(L->write_plan_bytes);
   L->total = o;
   return true;
@@ -745,9 +750,15 @@ gambit_status gambit_pool_create(const gambit_pool_desc* desc, void* stream, gam
   hipError_t e = hipHostMalloc(reinterpret_cast<void**>(&p->stage), p->stage_ints * 4, hipHostMallocDefault);
   if (e == hipSuccess) e = hipHostMalloc(reinterpret_cast<void**>(&p->plan_stage), p->plan_stage_bytes, hipHostMallocDefault);
   if (e == hipSuccess)
-    e = hipHostMalloc(reinterpret_cast<void**>(&p->packed_stage), L.rows_plan_bytes + L.write_plan_bytes, hipHostMallocDefault);
-  if (e == hipSuccess) e = hipEventCreateWithFlags(&p->rows_ev, hipEventDisableTiming);
-  if (e == hipSuccess) e = hipEventCreateWithFlags(&p->write_ev, hipEventDisableTiming);
+    e = hipHostMalloc(reinterpret_cast<void**>(&p->packed_stage),
+                      L.rows_plan_bytes[kPromptPlan] + L.rows_plan_bytes[kTreePlan] + L.write_plan_bytes, hipHostMallocDefault);
+  if (e == hipSuccess) {
+    p->rows[kPromptPlan].image = p->packed_stage;
+    p->rows[kTreePlan].image = p->packed_stage + L.rows_plan_bytes[kPromptPlan];
+    p->write.image = p->rows[kTreePlan].image + L.rows_plan_bytes[kTreePlan];
+  }
+  for (hipEvent_t* ev : {&p->rows[kPromptPlan].ev, &p->rows[kTreePlan].ev, &p->write.ev})
+    if (e == hipSuccess) e = hipEventCreateWithFlags(ev, hipEventDisableTiming);
   if (e == hipSuccess) e = hipEventCreateWithFlags(&p->stage_ev, hipEventDisableTiming);
   if (e == hipSuccess) e = hipEventCreateWithFlags(&p->plan_ev, hipEventDisableTiming);
 
@@ -760,8 +771,8 @@ gambit_status gambit_pool_create(const gambit_pool_desc* desc, void* stream, gam
   }
   if (e == hipSuccess) e = hipEventRecord(p->stage_ev, S(stream));
   if (e == hipSuccess) e = hipEventRecord(p->plan_ev, S(stream));
-  if (e == hipSuccess) e = hipEventRecord(p->rows_ev, S(stream));
-  if (e == hipSuccess) e = hipEventRecord(p->write_ev, S(stream));
+  for (hipEvent_t ev : {p->rows[kPromptPlan].ev, p->rows[kTreePlan].ev, p->write.ev})
+    if (e == hipSuccess) e = hipEventRecord(ev, S(stream));
   if (e == hipSuccess) e = hipMemsetAsync(p->ws + L.ticket, 0, 64, S(stream));
   if (e == hipSuccess) e = hipMemsetAsync(p->ws + L.queues, 0, 64, S(stream));
   if (e == hipSuccess) e = gambit::launch_pool_init(D, S(stream));
@@ -777,16 +788,16 @@ gambit_status gambit_pool_destroy(gambit_pool* p) {
   if (!p) return GAMBIT_ERR_INVALID;
   if (p->stage_ev) (void)hipEventSynchronize(p->stage_ev);
   if (p->plan_ev) (void)hipEventSynchronize(p->plan_ev);
-  if (p->rows_ev) (void)hipEventSynchronize(p->rows_ev);
-  if (p->write_ev) (void)hipEventSynchronize(p->write_ev);
+  for (hipEvent_t ev : {p->rows[kPromptPlan].ev, p->rows[kTreePlan].ev, p->write.ev})
+    if (ev) (void)hipEventSynchronize(ev);
   if (p->stage) (void)hipHostFree(p->stage);
   if (p->packed_stage) (void)hipHostFree(p->packed_stage);
   if (p->plan_stage) (void)hipHostFree(p->plan_stage);
   for (hipEvent_t e : p->prof_ev) (void)hipEventDestroy(e);
   if (p->stage_ev) (void)hipEventDestroy(p->stage_ev);
   if (p->plan_ev) (void)hipEventDestroy(p->plan_ev);
-  if (p->rows_ev) (void)hipEventDestroy(p->rows_ev);
-  if (p->write_ev) (void)hipEventDestroy(p->write_ev);
+  for (hipEvent_t ev : {p->rows[kPromptPlan].ev, p->rows[kTreePlan].ev, p->write.ev})
+    if (ev) (void)hipEventDestroy(ev);
 
   delete p;
   return GAMBIT_OK;

@@ -28,12 +28,12 @@ inline int cdiv(int a, int b) { return (a + b - 1) / b; }
 // Workspace carve-up.  All offsets are kAlign-aligned.
 struct Layout {
   size_t list, ids, req_trace, req_ntok, pairs, free_list, nk, ticket, queues, err, scales, freebits,
-      alloc_list, units, members, part_ml, part_acc, sbar, nscore, gen, ghost, tourn, rows_plan, write_plan, total;
+      alloc_list, units, members, part_ml, part_acc, sbar, nscore, gen, ghost, tourn, rows_plan[2], write_plan, total;
   int kmax, max_units, max_members, nwords;
-  // packed tokens: most of one call, partials (Hq rows each) of a rows plan,
-  // its items, and the bytes of the two plans
-  int max_packed, max_parts, max_items;
-  size_t rows_plan_bytes, write_plan_bytes;
+  // packed tokens: most of one call, partials (Hq rows each) of a rows plan;
+  // the items of a plan of prompts and of one of trees, and their bytes
+  int max_packed, max_parts, max_items[2];
+  size_t rows_plan_bytes[2], write_plan_bytes;
 };
 
 // A plan of packed tokens kept for calls that list the same (the layers of a
@@ -43,6 +43,17 @@ struct PackedKey {
   uint64_t epoch = 0;
   std::vector<int32_t> listed;
 };
+
+// The kept plan of one kind of call, and its pinned image, reused after `ev`.
+// A kind each, so that a layer's write, prompt and tree calls keep theirs.
+template <class Launch>
+struct KeptPlan {
+  PackedKey key;
+  Launch launch{};
+  uint8_t* image = nullptr;
+  hipEvent_t ev = nullptr;
+};
+enum { kPromptPlan = 0, kTreePlan = 1 };
 
 }  // namespace host
 }  // namespace gambit
@@ -91,15 +102,13 @@ struct gambit_pool {
   gambit_stats stats{};            // of plan_list, kept current by decode steps
   std::vector<int32_t> plan_kinds;  // per list position: GAMBIT_UNIT_* bits of the units covering it
 
-  // packed tokens (rows_attn.cpp): pinned images of the two plans, each reused
-  // after its event; changes of the mirror's lengths or rows so far
+  // packed tokens (rows_attn.cpp): the kept plans, their images one pinned
+  // buffer; changes of the mirror's lengths or rows so far
   uint64_t epoch = 0;
   int device = 0;
   uint8_t* packed_stage = nullptr;
-  hipEvent_t rows_ev = nullptr, write_ev = nullptr;
-  gambit::host::PackedKey rows_key, write_key;
-  gambit::RowsLaunch rows{};
-  gambit::WriteLaunch write{};
+  gambit::host::KeptPlan<gambit::RowsLaunch> rows[2];
+  gambit::host::KeptPlan<gambit::WriteLaunch> write;
 
   // attention-kernel event timing
   std::vector<hipEvent_t> prof_ev;

@@ -5,7 +5,8 @@
 //
 // A call's plan depends on what it lists and on the mirror alone, so the
 // layers of a step, which list the same, share one: it is made and uploaded
-// by the first call and kept until the list or the mirror changes.
+// by the first call and kept until the mirror changes or a call of its kind
+// (write, prompt, tree) lists something else.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -56,12 +57,11 @@ gambit_status check_call(gambit_pool* p, int32_t layer, int32_t n, const int32_t
 
 bool aligned16(const void* x) { return reinterpret_cast<uintptr_t>(x) % 16 == 0; }
 
-// What a call lists, as one list of ints to compare with the next call's.
-std::vector<int32_t> listing(int32_t kind, int32_t n, const int32_t* ids, const int32_t* a, const int32_t* b,
-                             const int32_t* c, size_t nc) {
+// What a call lists, as one list of ints to compare with its kind's next call's.
+std::vector<int32_t> listing(int32_t n, const int32_t* ids, const int32_t* a, const int32_t* b, const int32_t* c,
+                             size_t nc) {
   std::vector<int32_t> v;
   v.reserve(2 + 3 * (size_t)n + nc);
-  v.push_back(kind);
   v.push_back(n);
   v.insert(v.end(), ids, ids + n);
   v.insert(v.end(), a, a + n);
@@ -256,7 +256,7 @@ bool try_plan(gambit_pool* p, const std::vector<Listed>& L, const std::vector<Ru
     }
   }
   out->parts = (int)parts;
-  return (int)out->items.size() <= p->L.max_items && (int)out->list.size() <= p->L.max_parts;
+  return (int)out->items.size() <= p->L.max_items[tree] && (int)out->list.size() <= p->L.max_parts;
 }
 
 // Plans the call and uploads the plan: `anc` (trees) rides along.
@@ -321,10 +321,12 @@ gambit_status plan_rows(gambit_pool* p, std::vector<Listed> L, bool tree, const 
   std::stable_sort(plan.items.begin(), plan.items.end(), [](const RowItem& a, const RowItem& b) {
     return a.end - 16 * a.jb0 > b.end - 16 * b.jb0;
   });
-  HIP_TRY(p, hipEventSynchronize(p->rows_ev), "plan fence");
-  p->rows_key.valid = false;
-  Image im{p->packed_stage, p->ws + p->L.rows_plan, p->L.rows_plan_bytes};
-  gambit::RowsLaunch& A = p->rows;
+  const int kind = tree ? kTreePlan : kPromptPlan;
+  KeptPlan<gambit::RowsLaunch>& slot = p->rows[kind];
+  HIP_TRY(p, hipEventSynchronize(slot.ev), "plan fence");
+  slot.key.valid = false;
+  Image im{slot.image, p->ws + p->L.rows_plan[kind], p->L.rows_plan_bytes[kind]};
+  gambit::RowsLaunch& A = slot.launch;
   A = gambit::RowsLaunch{};
   A.items = im.put(plan.items.data(), plan.items.size());
   A.n_items = (int)plan.items.size();
@@ -336,14 +338,14 @@ gambit_status plan_rows(gambit_pool* p, std::vector<Listed> L, bool tree, const 
   A.n_merge = (int)plan.merge.size();
   if (!im.fits) return fail(p, GAMBIT_ERR_UNSUPPORTED, "plan exceeds workspace bounds");
   HIP_TRY(p, hipMemcpyAsync(im.dev, im.host, im.at, hipMemcpyHostToDevice, s), "plan upload");
-  HIP_TRY(p, hipEventRecord(p->rows_ev, s), "plan fence");
+  HIP_TRY(p, hipEventRecord(slot.ev, s), "plan fence");
   return GAMBIT_OK;
 }
 
-// Launches the kept plan on one layer.
-gambit_status launch_rows(gambit_pool* p, int32_t layer, const void* q, const void* k_new, const void* v_new, void* out,
+// Launches a kept plan on one layer.
+gambit_status launch_rows(gambit_pool* p, int kind, int32_t layer, const void* q, const void* k_new, const void* v_new, void* out,
                           int32_t out_dtype, float sm_scale, hipStream_t s) {
-  gambit::RowsLaunch A = p->rows;
+  gambit::RowsLaunch A = p->rows[kind].launch;
   A.q = static_cast<const uint16_t*>(q);
   A.k_new = static_cast<const uint16_t*>(k_new);
   A.v_new = static_cast<const uint16_t*>(v_new);
@@ -379,8 +381,6 @@ void keep(gambit_pool* p, PackedKey* k, std::vector<int32_t>&& now) {
   k->valid = true;
 }
 
-enum : int32_t { kPrompt = 1, kTree = 2, kWrite = 3 };
-
 gambit_status prompt_attn(gambit_pool* p, int32_t layer, int32_t n, const int32_t* ids, const int32_t* ntok,
                           const void* q, void* out, int32_t out_dtype, float sm_scale, hipStream_t s) {
   int64_t total = 0;
@@ -391,17 +391,17 @@ gambit_status prompt_attn(gambit_pool* p, int32_t layer, int32_t n, const int32_
       return fail(p, GAMBIT_ERR_INVALID, "%d tokens of trace %d, which holds %d", ntok[i], ids[i], p->seq_len[ids[i]]);
   if (total == 0) return GAMBIT_OK;
   if ((st = check_attention(p, q, out, out_dtype, sm_scale))) return st;
-  std::vector<int32_t> now = listing(kPrompt, n, ids, ntok, nullptr, nullptr, 0);
-  if (!kept(p, p->rows_key, now)) {
+  std::vector<int32_t> now = listing(n, ids, ntok, nullptr, nullptr, 0);
+  if (!kept(p, p->rows[kPromptPlan].key, now)) {
     std::vector<Listed> L;
     for (int i = 0, base = 0; i < n; base += ntok[i++]) {
       const int ctx = p->seq_len[ids[i]] - ntok[i];
       L.push_back(Listed{ids[i], base, ntok[i], ctx, ctx / 16, 0});
     }
     if ((st = plan_rows(p, std::move(L), false, {}, s))) return st;
-    keep(p, &p->rows_key, std::move(now));
+    keep(p, &p->rows[kPromptPlan].key, std::move(now));
   }
-  return launch_rows(p, layer, q, nullptr, nullptr, out, out_dtype, sm_scale, s);
+  return launch_rows(p, kPromptPlan, layer, q, nullptr, nullptr, out, out_dtype, sm_scale, s);
 }
 
 gambit_status tree_attn(gambit_pool* p, int32_t layer, int32_t n, const int32_t* ids, const int32_t* nodes,
@@ -422,8 +422,8 @@ gambit_status tree_attn(gambit_pool* p, int32_t layer, int32_t n, const int32_t*
   if ((st = check_attention(p, q, out, out_dtype, sm_scale))) return st;
   if (!k_new || !v_new) return fail(p, GAMBIT_ERR_INVALID, "NULL buffer");
   if (!aligned16(k_new) || !aligned16(v_new)) return fail(p, GAMBIT_ERR_INVALID, "a buffer is not 16-byte aligned");
-  std::vector<int32_t> now = listing(kTree, n, ids, nodes, nullptr, parents, (size_t)total);
-  if (!kept(p, p->rows_key, now)) {
+  std::vector<int32_t> now = listing(n, ids, nodes, nullptr, parents, (size_t)total);
+  if (!kept(p, p->rows[kTreePlan].key, now)) {
     std::vector<Listed> L;
     std::vector<uint64_t> anc((size_t)total);
     for (int i = 0, base = 0; i < n; base += nodes[i++]) {
@@ -435,9 +435,9 @@ gambit_status tree_attn(gambit_pool* p, int32_t layer, int32_t n, const int32_t*
       }
     }
     if ((st = plan_rows(p, std::move(L), true, anc, s))) return st;
-    keep(p, &p->rows_key, std::move(now));
+    keep(p, &p->rows[kTreePlan].key, std::move(now));
   }
-  return launch_rows(p, layer, q, k_new, v_new, out, out_dtype, sm_scale, s);
+  return launch_rows(p, kTreePlan, layer, q, k_new, v_new, out, out_dtype, sm_scale, s);
 }
 
 gambit_status kv_write_layer(gambit_pool* p, int32_t layer, int32_t n, const int32_t* ids, const int32_t* pos0,
@@ -466,8 +466,8 @@ gambit_status kv_write_layer(gambit_pool* p, int32_t layer, int32_t n, const int
       for (int j = pos0[i] / 16; j <= (pos0[i] + ntok[i] - 1) / 16; ++j)
         if (p->refcount[p->table[ids[i]][j]] != 1)
           return fail(p, GAMBIT_ERR_SHARED_WRITE, "block %d of trace %d is shared", j, ids[i]);
-  std::vector<int32_t> now = listing(kWrite, n, ids, ntok, pos0, rows, (size_t)total);
-  if (!kept(p, p->write_key, now)) {
+  std::vector<int32_t> now = listing(n, ids, ntok, pos0, rows, (size_t)total);
+  if (!kept(p, p->write.key, now)) {
     std::vector<WriteItem> items;
     for (int i = 0, base = 0; i < n; base += ntok[i++]) {
       const int a = pos0[i], e = a + ntok[i];
@@ -477,20 +477,20 @@ gambit_status kv_write_layer(gambit_pool* p, int32_t layer, int32_t n, const int
         items.push_back(WriteItem{p->table[ids[i]][j], base + 16 * j + r0 - a, (int16_t)r0, (int16_t)r1, floor});
       }
     }
-    HIP_TRY(p, hipEventSynchronize(p->write_ev), "plan fence");
-    p->write_key.valid = false;
-    Image im{p->packed_stage + p->L.rows_plan_bytes, p->ws + p->L.write_plan, p->L.write_plan_bytes};
-    gambit::WriteLaunch& W = p->write;
+    HIP_TRY(p, hipEventSynchronize(p->write.ev), "plan fence");
+    p->write.key.valid = false;
+    Image im{p->write.image, p->ws + p->L.write_plan, p->L.write_plan_bytes};
+    gambit::WriteLaunch& W = p->write.launch;
     W = gambit::WriteLaunch{};
     W.items = im.put(items.data(), items.size());
     W.n_items = (int)items.size();
     W.rows = rows ? im.put(rows, (size_t)total) : nullptr;
     if (!im.fits) return fail(p, GAMBIT_ERR_UNSUPPORTED, "plan exceeds workspace bounds");
     HIP_TRY(p, hipMemcpyAsync(im.dev, im.host, im.at, hipMemcpyHostToDevice, s), "plan upload");
-    HIP_TRY(p, hipEventRecord(p->write_ev, s), "plan fence");
-    keep(p, &p->write_key, std::move(now));
+    HIP_TRY(p, hipEventRecord(p->write.ev, s), "plan fence");
+    keep(p, &p->write.key, std::move(now));
   }
-  gambit::WriteLaunch W = p->write;
+  gambit::WriteLaunch W = p->write.launch;
   W.k = static_cast<const uint16_t*>(k);
   W.v = static_cast<const uint16_t*>(v);
   HIP_TRY(p, gambit::launch_rows_write(p->dev.layer(layer), W, s), "layer write");
@@ -507,7 +507,8 @@ gambit_status guarded(gambit_pool* p, F&& f) {
   } catch (...) {
     std::fill(p->cnt.begin(), p->cnt.end(), 0);
     std::fill(p->first.begin(), p->first.end(), -1);
-    p->rows_key.valid = p->write_key.valid = false;
+    for (auto& x : p->rows) x.key.valid = false;
+    p->write.key.valid = false;
     return fail(p, GAMBIT_ERR_DEVICE, "out of host memory");
   }
 }

@@ -10,6 +10,7 @@
 //   prompt LAYER t n ...                  gambit_prompt_attn, then its plan
 //   tree LAYER ntraces t m ... parents..  gambit_tree_attn, then its plan
 //   write LAYER n_rows t pos0 n ... [rows r ...]   gambit_kv_write_layer, then its items
+//   uploads                               copies to the device so far
 #include <hip/hip_runtime.h>
 
 enum hipStreamCaptureStatus { hipStreamCaptureStatusNone = 0, hipStreamCaptureStatusActive = 1 };
@@ -20,6 +21,12 @@ inline hipError_t hipStreamIsCapturing(hipStream_t, hipStreamCaptureStatus* s) {
   return hipSuccess;
 }
 #define hipGetDevice(d) (*(d) = g_device, hipSuccess)
+static int g_uploads = 0;
+inline hipError_t counted_copy(void* d, const void* s, size_t n, hipMemcpyKind k, hipStream_t q) {
+  g_uploads += k == hipMemcpyHostToDevice;
+  return hipMemcpyAsync(d, s, n, k, q);
+}
+#define hipMemcpyAsync counted_copy
 
 #include "../../paper_2608_08020_amd/csrc/gambit_pool.cpp"
 #include "../../paper_2608_08020_amd/csrc/rows_attn.cpp"
@@ -160,6 +167,8 @@ int main() {
       d.workspace = reinterpret_cast<void*>(base), d.workspace_bytes = ws;
       const int st = gambit_pool_create(&d, nullptr, &p);
       std::cout << "{\"status\":" << st << ",\"max_packed\":" << (p ? p->L.max_packed : 0) << "}\n";
+    } else if (op == "uploads") {
+      std::cout << "{\"status\":0,\"uploads\":" << g_uploads << "}\n";
     } else if (op == "capturing" || op == "device") {
       if (op == "device") g_device = a[0];
       if (op == "capturing") g_capturing = a[0] != 0;
