@@ -98,7 +98,8 @@ typedef struct {
   int32_t kv_dtype;              /* GAMBIT_KV_*                             */
   int32_t max_traces;            /* trace ids are 0 .. max_traces-1         */
   int32_t max_blocks_per_trace;
-  int32_t max_splits;            /* attention partials per (trace, head), <= 64; 0 = 64 */
+  int32_t max_splits;            /* attention partials per (trace, head), <= 64; 0 = 64, and
+                                    room for what packed calls are cut into (below) */
   float fp8_append_scale;        /* scale of blocks a decode step allocates; 0 = 2^-6 */
   int32_t num_layers;            /* layers sharing the block table; 0 = 1   */
   void* k_cache;
@@ -219,7 +220,10 @@ gambit_status gambit_decode_attn_layer(gambit_pool* pool, int32_t layer, int32_t
  * the host, after the upload of its kind's last one has ended.  Device buffers are 16-byte
  * aligned and contiguous; inputs and outputs do not overlap.  At most
  * GAMBIT_MAX_PACKED tokens a call (fewer for a pool that cannot hold as many:
- * 16 max_traces max_blocks_per_trace positions, or 64 nodes a slot).  A
+ * 16 max_traces max_blocks_per_trace positions, or 64 nodes a slot).  A pool
+ * with max_splits set holds max_traces max_splits partials of a head for these
+ * calls too: long contexts of few tokens, and shared blocks of many, are then
+ * read in fewer pieces or trace by trace, which costs time, not results.  A
  * slot that holds a ghost cannot be listed.  Not while a decode step is open,
  * not on a stream that is being captured (GAMBIT_ERR_UNSUPPORTED: the plan is
  * uploaded by the call), and with the pool's device current.

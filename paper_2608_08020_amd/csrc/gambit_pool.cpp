@@ -32,7 +32,17 @@ using gambit::AttnUnit;
 namespace {
 
 constexpr int kDefaultChunkBlocks = 64;  // blocks per attention chunk before balancing
-constexpr size_t kPackedPartRows = 262144;  // partial rows of a packed call: four rounds of 512 workgroups of 128
+
+// Partial rows that a pool without a limit of its own (max_splits 0) holds for
+// packed calls.  A workgroup leaves up to 128; a call is cut into about 512
+// workgroups, and a third more where every range rounds up to two pieces.
+// Traces that share blocks besides leave one partial for what they share and one
+// for the rest, at most 256 rows of each KV head (two tiles) twice.
+constexpr size_t kPackedPartRows = 262144;
+constexpr int kMostPieces = 8192;
+size_t packed_part_rows(const gambit_pool_desc* d) {
+  return std::min(kPackedPartRows, 512 * 128 * 4 / 3 + 512 * (size_t)d->num_kv_heads * d->max_traces);
+}
 
 // Per-token times of one attention unit on MI355X (microseconds), by kind and
 // cache dtype: narrow units per wave, cooperative items per workgroup.  fp8:
@@ -92,9 +102,10 @@ bool layout_of(const gambit_pool_desc* d, Layout* L) {
   L->alloc_list = take(4 * (size_t)d->num_blocks);
   L->units = take(sizeof(AttnUnit) * (size_t)L->max_units);
   L->members = take(4 * ((size_t)L->max_members + gambit::kMemberPad));
-  // decode steps write up to kmax partials a trace; the packed rows of a
-  // prompt or tree call as many as four rounds of workgroups
-  L->max_parts = (int)std::min<size_t>(std::max<size_t>((size_t)T * kmax, kPackedPartRows / d->num_q_heads + 1), 1 << 30);
+  // decode steps write up to kmax partials a trace; packed calls use the same
+  // room, their plans cut into no more, and get more unless the caller set a limit
+  const size_t packed = d->max_splits ? 0 : packed_part_rows(d) / d->num_q_heads + 1;
+  L->max_parts = (int)std::min<size_t>(std::max<size_t>((size_t)T * kmax, packed), 1 << 30);
   L->part_ml = take(8 * (size_t)L->max_parts * d->num_q_heads);
   L->part_acc = take(4 * (size_t)L->max_parts * d->num_q_heads * gambit::kHeadDim);
   L->sbar = take(4 * (size_t)T);
@@ -104,10 +115,12 @@ bool layout_of(const gambit_pool_desc* d, Layout* L) {
   L->tourn = take(4 * ((size_t)gambit::kTournHeader + 3 * (size_t)T));
   const size_t held = (size_t)T * d->max_blocks_per_trace * 16;
   L->max_packed = (int)std::min<size_t>(GAMBIT_MAX_PACKED, std::max<size_t>(held, (size_t)T * gambit::kMaxNodes));
+  // a plan has an item for each tile of tokens, and one more for each piece that
+  // leaves partials (a plan with more is made again with fewer pieces)
   for (int kind : {kPromptPlan, kTreePlan}) {
     const bool tree = kind == kTreePlan;
     const size_t tokens = tree ? std::min<size_t>(L->max_packed, (size_t)T * gambit::kMaxNodes) : L->max_packed;
-    L->max_items[kind] = (int)tokens / (gambit::kRowsTile / g) + 2 * T + L->max_parts;
+    L->max_items[kind] = (int)tokens / (gambit::kRowsTile / g) + 2 * T + std::min(L->max_parts, kMostPieces);
     L->rows_plan_bytes[kind] = align_up(sizeof(gambit::RowItem) * (size_t)L->max_items[kind]) +
                                align_up(4 * (size_t)L->max_parts) + 3 * align_up(4 * tokens) +
                                (tree ? align_up(8 * tokens) : 0);
