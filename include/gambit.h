@@ -266,7 +266,8 @@ gambit_status gambit_kv_write_layer(gambit_pool* pool, int32_t layer, int32_t n,
  *   trace_ids, n_tokens  host [n]
  *   q         device [total][Hq][head_dim] bf16
  *   out       device [total][Hq][head_dim], bf16 or fp32 (out_dtype)
- * fp8: block scales are >= 0.  With bf16 output the weights are rounded to bf16
+ * fp8: block scales are >= 0; a V scale below 2^-100 counts as 2^-100 (zero
+ * too: values of at most 2^-91 for it).  With bf16 output the weights are rounded to bf16
  * before they meet V (2^-8 of each, half a step), with fp32 output they are
  * kept to fp32's precision; sums are fp32. */
 gambit_status gambit_prompt_attn(gambit_pool* pool, int32_t layer, int32_t n, const int32_t* trace_ids,

@@ -30,20 +30,24 @@
 // outputs (64) and the scores of two tiles (64), and 80 KiB of LDS each: two
 // buffers of K and of V fill 64.
 //
-// What bounds it, measured (a large copy: 4.76 TB/s, a large library product:
-// 1.25 PFLOP/s):
+// What bounds it, measured (medians of kernel times; a large copy: 4.76 TB/s, a
+// large library product: 1.25 PFLOP/s):
 //   long prompts, bf16: the matrix units and what issues beside them.  One of
-//     8192 tokens, 32 query heads over 8: 494 us, 1.11 PFLOP/s of what is seen
-//     (605 us before the order of plain_tile was written out)
+//     8192 tokens, 32 query heads over 8: 505 us, 1.09 PFLOP/s of what is seen
+//     (about a fifth longer before the order of plain_tile was written out)
 //   long prompts, fp8: the same, and the codes' way to bf16 through registers
 //     and LDS, once per workgroup.  Four of 1024 to 4096 tokens, 64 query heads
-//     over 8: 535 us, 0.88 PFLOP/s
-//   short prompts: a workgroup's start, masked tile and end, half of its time at
-//     five tiles.  Sixteen of 256 to 1024 tokens: 113 us, 0.61 PFLOP/s
+//     over 8: 522 us, 0.90 PFLOP/s
+//   short prompts: a workgroup's start, masked tile and end, over a third of its
+//     time at six to seven tiles.  Sixteen of 256 to 1024 tokens: 112 us, 0.62 PFLOP/s
 //   trees and inserted tokens over long contexts: HBM while a workgroup's rows are
-//     few.  64 trees of eight nodes, four to a prefix: 661 MB in 121 us, 5.4 TB/s;
-//     128 fp8 trees: the tiles' widening and products, 242 us, 0.66 PFLOP/s
-//   a prompt of 17 tokens: 7.2 us of loads one after another, one tile and the end
+//     few.  64 trees of eight nodes, four to a prefix: 662 MB in 124 us, 5.3 TB/s;
+//     128 fp8 trees: the tiles' widening and products, 244 us, 0.66 PFLOP/s
+//   a prompt of 17 tokens: one tile, 7.4 us
+//   fp32 output at these sizes: 64 products a tile for 32, in the generic loop;
+//     whole calls 1.2 to 1.8 times as long
+// All 256 registers are taken, and 15 (bf16 pool and output) to 48 (fp8 pool,
+// fp32 output, drafts) more lie in scratch; only the generic loop reloads them.
 #include <cmath>
 
 #include "lds_dma.h"
@@ -596,6 +600,8 @@ __global__ __launch_bounds__(kThreads, 2) void rows_attn_kernel(DevPool P, RowsL
   };
   auto widen_k = [&](int i, int lane) {  // 16 d of a row -> two chunks of 8
     // lane 0: K's with the softmax scale; lanes 1 to 3: V's, its log2, its reciprocal
+    // (bf16 output; instructions of one ulp, at most 2^-17 of a weight that is
+    // rounded to bf16 next; fp32 output takes the scale itself)
     const float x = fmaxf(lane ? raw_scale : A.c * raw_scale, lane ? 0x1p-100f : 0x1p-120f);
     const float y = lane == 2 ? __builtin_amdgcn_logf(x) : lane == 3 ? __builtin_amdgcn_rcpf(x) : x;
     if (lane < 4) scale_s[i % 3][lane][w] = y;
@@ -840,7 +846,7 @@ __global__ __launch_bounds__(kThreads, 2) void rows_attn_kernel(DevPool P, RowsL
 // A partial without a seen position has m = -inf and sums of zero.  A factor of
 // zero still meets the partial's sums: where a V that its rows see is not finite
 // they are not, and so is the result, as in a range that was not cut.
-// Bound by HBM, for few partials by latency: 3 us for 40 tokens of 32 heads, 7
+// Bound by HBM, for few partials by latency: 4 us for 40 tokens of 32 heads, 7
 // for 512, 22 for 1120 of 64 heads.
 __global__ __launch_bounds__(256) void rows_merge_kernel(RowsLaunch A, int32_t Hq) {
   const int r = blockIdx.x * 8 + (threadIdx.x >> 5), x = threadIdx.x & 31;

@@ -7,7 +7,7 @@
 // E4M3FN's largest value).  Both are bound by HBM: token rows are read whole
 // (256 bytes a head), turned in LDS into the caches' tile layout, and stored
 // 16 bytes a lane in order.  Measured with 8 KV heads (a large copy: 4.76 TB/s):
-// bf16, eight segments of 2048 to 8192 tokens, 375 MB, 68 us, 5.5 TB/s; eight traces of
+// bf16, eight segments of 2048 to 8192 tokens, 374 MB, 71 us, 5.3 TB/s; eight traces of
 // one to five tokens 3 us, latency; fp8, sixteen prompts of 256 to 1024 tokens,
 // 60 MB, 16 us (26 us with one workgroup for a block's K and V).
 #include "rows.h"
