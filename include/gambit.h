@@ -217,16 +217,17 @@ gambit_status gambit_decode_attn_layer(gambit_pool* pool, int32_t layer, int32_t
  * The pool keeps the last plan of each kind of call (write, prompt, tree); calls
  * that list what the last one of their kind listed, with no length or table
  * changed since (the layers of a step), use it.  Any other call makes a plan on
- * the host, after the upload of its kind's last one has ended.  Device buffers are 16-byte
- * aligned and contiguous; inputs and outputs do not overlap.  At most
- * GAMBIT_MAX_PACKED tokens a call (fewer for a pool that cannot hold as many:
- * 16 max_traces max_blocks_per_trace positions, or 64 nodes a slot).  A pool
- * with max_splits set holds max_traces max_splits partials of a head for these
- * calls too: long contexts of few tokens, and shared blocks of many, are then
- * read in fewer pieces or trace by trace, which costs time, not results.  A
- * slot that holds a ghost cannot be listed.  Not while a decode step is open,
- * not on a stream that is being captured (GAMBIT_ERR_UNSUPPORTED: the plan is
- * uploaded by the call), and with the pool's device current.
+ * the host, after the upload of its kind's last one has ended.
+ * Device buffers are 16-byte aligned and contiguous; inputs and outputs do not
+ * overlap.  At most GAMBIT_MAX_PACKED tokens a call (fewer for a pool that
+ * cannot hold as many: 16 max_traces max_blocks_per_trace positions, or 64
+ * nodes a slot).  A pool with max_splits set holds max_traces max_splits
+ * partials of a head for these calls too: long contexts of few tokens, and
+ * shared blocks of many, are then read in fewer pieces or trace by trace, which
+ * costs time, not results.  A slot that holds a ghost cannot be listed.  Not
+ * while a decode step is open, not on a stream that is being captured
+ * (GAMBIT_ERR_UNSUPPORTED: the plan is uploaded by the call), and with the
+ * pool's device current.
  */
 #define GAMBIT_MAX_PACKED 262144
 #define GAMBIT_MAX_NODES 64

@@ -45,7 +45,7 @@
 //     128 fp8 trees: the tiles' widening and products, 244 us, 0.66 PFLOP/s
 //   a prompt of 17 tokens: one tile, 7.4 us
 //   fp32 output at these sizes: 64 products a tile for 32, in the generic loop;
-//     whole calls 1.2 to 1.8 times as long
+//     whole calls 1.2 to 1.9 times as long
 // All 256 registers are taken, and 15 (bf16 pool and output) to 48 (fp8 pool,
 // fp32 output, drafts) more lie in scratch; only the generic loop reloads them.
 #include <cmath>
