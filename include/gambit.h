@@ -64,6 +64,7 @@ enum {
 
 enum { GAMBIT_KV_BF16 = 0, GAMBIT_KV_FP8_E4M3 = 1 };
 enum { GAMBIT_OUT_BF16 = 0, GAMBIT_OUT_F32 = 1 };
+enum { GAMBIT_BF16 = 0, GAMBIT_F32 = 1, GAMBIT_E4M3 = 2 };  /* types of a dense operator's rows */
 
 typedef struct gambit_pool gambit_pool;
 
@@ -252,6 +253,29 @@ gambit_status gambit_decode_attn_layer(gambit_pool* pool, int32_t layer, int32_t
 gambit_status gambit_kv_write_layer(gambit_pool* pool, int32_t layer, int32_t n, const int32_t* trace_ids,
                                     const int32_t* pos0, const int32_t* n_tokens, const int32_t* rows,
                                     int32_t n_rows, const void* k, const void* v, void* stream);
+
+/* gambit_kv_write_layer with the position rotation on the way.  Of each head's
+ * first `rot` values (a multiple of 16, at most 128; the others stay), pair i
+ * becomes
+ *     (a, b) -> (a c - b s, b c + a s)
+ * with c, s = table[position][i], table[position][rot / 2 + i]; pair i is
+ * values (i, i + rot / 2), or (2 i, 2 i + 1) when `pairs` is set.  Keys and
+ * queries turn in fp32; keys are rounded once, to bf16 or, in an fp8 pool, to
+ * the codes of the turned values (whose magnitudes a block's scale goes by);
+ * values enter as they are.
+ *   k, v, q   device, bf16: rows of [Hkv][128], [Hkv][128], [Hq][128] that begin
+ *             k_stride, v_stride, q_stride values apart (multiples of 8, so that
+ *             parts of packed q, k, v rows can be given); all take `rows`
+ *   q, q_out  NULL: no queries.  q_out [total][Hq][128] bf16, in packed order;
+ *             without `rows`, q_out may be q itself
+ *   table     device fp32 [n_pos][rot], 16-byte aligned; every written position
+ *             lies below n_pos
+ * Otherwise as gambit_kv_write_layer. */
+gambit_status gambit_kv_write_rotated(gambit_pool* pool, int32_t layer, int32_t n, const int32_t* trace_ids,
+                                      const int32_t* pos0, const int32_t* n_tokens, const int32_t* rows,
+                                      int32_t n_rows, const void* k, int64_t k_stride, const void* v,
+                                      int64_t v_stride, const void* q, int64_t q_stride, void* q_out,
+                                      const float* table, int32_t n_pos, int32_t rot, int32_t pairs, void* stream);
 
 /* Causal attention of prompt tokens over the cache: the last n_tokens[i]
  * positions of trace i, whose K and V are in layer `layer`'s cache, attend to
@@ -554,6 +578,102 @@ int32_t gambit_scorer_steps(const gambit_scorer* scorer, int32_t trace_id);
  * error word (synchronises the stream).  GAMBIT_OK when they agree. */
 gambit_status gambit_scorer_check(gambit_scorer* scorer, void* stream);
 const char* gambit_scorer_last_error(const gambit_scorer* scorer);
+
+/*
+ * What a model's layer does between its attention calls, on rows of tokens.
+ * These calls hold no state and take no workspace: they may run on several
+ * streams at once and be captured into a graph.  Device buffers are those of
+ * the current device, 16-byte aligned unless a line says otherwise; n (or m)
+ * = 0 does nothing.  GAMBIT_ERR_INVALID for a bad argument, GAMBIT_ERR_
+ * UNSUPPORTED for a size beyond the kernels', GAMBIT_ERR_DEVICE when the launch
+ * fails.
+ */
+
+/* Root-mean-square norm of the rows x (n x heads of them, row (i, j) at
+ * i row_stride + j head_stride values; strides are multiples of 16 bytes),
+ * after the addition of a residual where there is one:
+ *     h = x + residual,  residual_out = h,
+ *     y = weight h / sqrt(mean(h^2) + eps)
+ * The sum h is normed as it is in fp32; residual_out holds it rounded to its
+ * type.  Rows whose squares leave fp32 are normed over 2^72.
+ *   dim       a multiple of 8 (of 16 for E4M3 output), at most 32768
+ *   x, weight, residual  device; dtypes GAMBIT_BF16 or GAMBIT_F32;
+ *             residual NULL: none.  residual, residual_out and out are
+ *             contiguous [n][heads][dim]; residual_out may be residual, out
+ *             may be x (contiguous, of the same type)
+ *   eps       at least 2^-80
+ *   out       GAMBIT_BF16, GAMBIT_F32, or GAMBIT_E4M3 with out_scale device
+ *             fp32 [ceil(dim / 128)][n heads]: the scale s of each group of
+ *             128 values of a row is max(max |y| / 448, 2^-60), a code the
+ *             E4M3FN value nearest to y / s (ties to the even code, saturating;
+ *             NaN stays NaN and does not count for the scale, an infinity
+ *             counts as the largest finite value) */
+gambit_status gambit_rms_norm(int32_t n, int32_t heads, int32_t dim, const void* x, int32_t x_dtype,
+                              int64_t row_stride, int64_t head_stride, const void* weight, int32_t weight_dtype,
+                              float eps, const void* residual, void* residual_out, int32_t residual_dtype,
+                              void* out, int32_t out_dtype, float* out_scale, void* stream);
+
+/* Rows x [n][dim] (row_stride values apart, a multiple of 16 bytes) as E4M3
+ * codes and scales, as gambit_rms_norm gives them.  gated: a row of x holds two
+ * halves a, b of dim values each, and what is quantised is silu(a) b =
+ * a / (1 + exp(-a)) b.  dim is a multiple of 16. */
+gambit_status gambit_quantize(int32_t n, int32_t dim, const void* x, int32_t x_dtype, int64_t row_stride,
+                              int32_t gated, void* out, float* out_scale, void* stream);
+
+/* The product of token rows with a weight matrix, both in E4M3FN:
+ *     out[t][f] = sum_b x_scale[b][t] w_scale[f / 128][b] sum_{k in block b} x[t][k] w[f][k]
+ * over blocks b of 128 values (the last one may be shorter), sums in fp32, the
+ * blocks in an order that depends on the sizes alone.
+ *   x         device [m][k] codes, x_scale fp32 [ceil(k / 128)][m] (4-byte
+ *             aligned), as gambit_rms_norm and gambit_quantize write them
+ *   w         device [n][k] codes, w_scale fp32 [ceil(n / 128)][ceil(k / 128)]
+ *             (4-byte aligned)
+ *   out       device [m][n], GAMBIT_BF16 or GAMBIT_F32
+ *   k         a multiple of 16; m, n at most 2^24 */
+gambit_status gambit_linear_fp8(int32_t m, int32_t n, int32_t k, const void* x, const float* x_scale,
+                                const void* w, const float* w_scale, void* out, int32_t out_dtype, void* stream);
+
+/* The position rotation of gambit_kv_write_rotated for new tokens that do not
+ * enter a cache by that call (a decode step's, a draft tree's, whose
+ * attention takes them itself).
+ *   q, k      device bf16 [n] rows of [q_heads][128] and [k_heads][128],
+ *             q_stride and k_stride values apart (multiples of 8); a side
+ *             of no heads is left out
+ *   positions device int32 [n]; a position outside the table turns into NaN
+ *   table     device fp32 [n_pos][rot]
+ *   q_out, k_out  contiguous [n][heads][128] bf16; may be q and k themselves
+ *             where those are contiguous */
+gambit_status gambit_rotate(int32_t n, int32_t q_heads, int32_t k_heads, const void* q, int64_t q_stride,
+                            const void* k, int64_t k_stride, const int32_t* positions, const float* table,
+                            int32_t n_pos, int32_t rot, int32_t pairs, void* q_out, void* k_out, void* stream);
+
+/* One token a row of logits z.  With w_i = exp((z_i - max z) / temperature):
+ *   top_k     keeps the k largest z (of equal ones the lower index);
+ *             k <= 0 or >= vocab: all
+ *   top_p     of those keeps the shortest front part, largest z first (of
+ *             equal ones the lower index first), whose weight is at least
+ *             top_p of theirs; >= 1 or NaN: all, <= 0: the first
+ *   min_p     of those keeps the ones with w_i >= min_p; <= 0 or NaN: all,
+ *             above 1 counts as 1
+ *   token     the first kept index whose kept weights up to and with it sum
+ *             to more than u times the sum of all kept weights
+ * A temperature of 0, below it or NaN takes the largest z (of equal ones the
+ * lower index).  In logits NaN counts as -inf (which is never drawn), +inf as
+ * the largest finite value; a row that holds nothing else gives -1.  u below 0
+ * or NaN counts as 0; from 1 on, the last kept index.
+ * Weights are rounded to 2^-S, S = 62 - ceil(log2(vocab)), at most 50; sums
+ * are exact.
+ *   logits    device, GAMBIT_BF16 or GAMBIT_F32, rows row_stride values
+ *             apart, aligned to their type
+ *   u         device fp32 [n], in [0, 1)
+ *   temperature, top_k, top_p, min_p  device [n] (fp32, int32, fp32, fp32); NULL:
+ *             the call's *_all for every row
+ *   ids_out   device int32 [n]
+ *   vocab     at most 2^18 */
+gambit_status gambit_sample(int32_t n, int32_t vocab, const void* logits, int32_t dtype, int64_t row_stride,
+                            const float* u, const float* temperature, float temperature_all,
+                            const int32_t* top_k, int32_t top_k_all, const float* top_p, float top_p_all,
+                            const float* min_p, float min_p_all, int32_t* ids_out, void* stream);
 
 /* Measurement, not a step of the method: the device's streaming-read rate,
  * the practical ceiling beside the published HBM peak for the attention

@@ -125,7 +125,8 @@ bool layout_of(const gambit_pool_desc* d, Layout* L) {
                                align_up(4 * (size_t)L->max_parts) + 3 * align_up(4 * tokens) +
                                (tree ? align_up(8 * tokens) : 0);
   }
-  L->write_plan_bytes = align_up(sizeof(gambit::WriteItem) * ((size_t)L->max_packed / 16 + 2 * (size_t)T)) +
+  const size_t write_items = (size_t)L->max_packed / 16 + 2 * (size_t)T;
+  L->write_plan_bytes = align_up(sizeof(gambit::WriteItem) * write_items) + align_up(4 * write_items) +
                         align_up(4 * (size_t)L->max_packed);
   for (int kind : {kPromptPlan, kTreePlan}) L->rows_plan[kind] = take(L->rows_plan_bytes[kind]);
   L->write_plan = take(L->write_plan_bytes);

@@ -1,0 +1,350 @@
+// The product of token rows and a weight matrix, both in E4M3 with scales of
+// 128 (gambit_linear_fp8), kernels and host entry point.
+//
+//     y[t][f] = sum over k blocks b of xs[b][t] ws[f / 128][b] sum_{k in b} x[t][k] w[f][k]
+//
+// A block's sum, started from zero in the matrix unit, is carried into the
+// running sum (fp32) by the two scales' product.  The weights are the
+// instruction's first operand, so a lane holds four neighbouring features of
+// one token: one factor a lane and block, and outputs stored four at a time.
+//
+// bf16 output: v_mfma_f32_16x16x128_f8f6f4, a whole block an instruction.  It aligns the
+// products of eight neighbouring k to the largest of them and drops what lies
+// 13 bits below (measured, as for the 16x16x32 fp8 form): 1.5e-5 of normal rows'
+// outputs, 1 / 130 of the rounding to bf16 that follows.  That is too coarse for
+// fp32 output: there the codes become bf16 (exact) and four v_mfma_f32_16x16x32_bf16
+// make a block, at half the rate and 1e-8.
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+#include <type_traits>
+
+#include "../../include/gambit.h"
+#include "kernels.h"
+#include "lds_dma.h"
+
+namespace gambit {
+namespace {
+
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+
+constexpr int kKB = 128;  // values of a block, bytes of a row's block
+
+struct LinearArgs {
+  const uint8_t* x;   // [m][k]
+  const float* xs;    // [blocks][m]
+  const uint8_t* w;   // [n][k]
+  const float* ws;    // [ceil(n / 128)][blocks]
+  void* out;          // [m][n]
+  int32_t m, n, k, blocks;
+  int32_t f32;
+  int32_t tiles_f, tiles_t;
+};
+
+__device__ inline i32x8 join(i32x4 a, i32x4 b) { return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7); }
+
+// A lane's 32 values of a block of one row, as the matrix unit takes them.
+template <bool kExact>
+struct Operand;
+template <>
+struct Operand<false> {
+  i32x8 v;
+  __device__ void set(i32x8 codes) { v = codes; }
+};
+template <>
+struct Operand<true> {
+  bf16x8 v[4];
+  __device__ void set(i32x8 codes) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes[2 * i], 1.f, false);
+      const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes[2 * i], 1.f, true);
+      const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes[2 * i + 1], 1.f, false);
+      const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes[2 * i + 1], 1.f, true);
+      v[i] = bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+    }
+  }
+};
+__device__ inline f32x4 block_sum(const Operand<false>& a, const Operand<false>& b) {
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a.v, b.v, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, 0, 0, 0);
+}
+__device__ inline f32x4 block_sum(const Operand<true>& a, const Operand<true>& b) {
+  f32x4 y{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) y = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.v[i], b.v[i], y, 0, 0, 0);
+  return y;
+}
+
+__device__ inline uint32_t bf16_pair(float a, float b) {
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, bf16x2));
+}
+
+// Four neighbouring features of a token.
+__device__ inline void store4(const LinearArgs& A, int t, int f, f32x4 y) {
+  if (t >= A.m || f >= A.n) return;
+  const size_t at = (size_t)t * A.n + f;
+  const bool whole = A.n % 4 == 0;  // then f + 3 is inside, and the address a multiple of four values
+  if (A.f32) {
+    float* p = static_cast<float*>(A.out) + at;
+    if (whole) {
+      *reinterpret_cast<f32x4*>(p) = y;
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (f + e < A.n) p[e] = y[e];
+    }
+  } else {
+    uint16_t* p = static_cast<uint16_t*>(A.out) + at;
+    const uint32_t lo = bf16_pair(y[0], y[1]), hi = bf16_pair(y[2], y[3]);
+    if (whole) {
+      *reinterpret_cast<uint2*>(p) = make_uint2(lo, hi);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (f + e < A.n) p[e] = (uint16_t)((e < 2 ? lo : hi) >> (16 * (e % 2)));
+    }
+  }
+}
+
+// ---- few tokens --------------------------------------------------------------
+// Bound by the weights' bytes.  A workgroup takes 16 kF features and up to
+// 16 kT tokens; its eight waves take every eighth block of k each, weights and
+// tokens straight into registers, and add up through LDS.
+constexpr int kSkinnyWaves = 8;
+
+template <bool kExact, int kT, int kF>
+__global__ __launch_bounds__(64 * kSkinnyWaves) void linear_skinny_kernel(LinearArgs A) {
+  __shared__ f32x4 sums[kSkinnyWaves][kT * kF][64];
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, i = lane & 15, q = lane >> 4;
+  const int f0 = blockIdx.x * 16 * kF, t0 = blockIdx.y * 16 * kT;
+  const uint8_t *wp[kF], *xp[kT];
+  const float* sp[kT];
+#pragma unroll
+  for (int f = 0; f < kF; ++f) wp[f] = A.w + (size_t)min(f0 + 16 * f + i, A.n - 1) * A.k + 32 * q;
+#pragma unroll
+  for (int t = 0; t < kT; ++t) {
+    const int tok = min(t0 + 16 * t + i, A.m - 1);  // tokens past the end repeat the last one (never stored)
+    xp[t] = A.x + (size_t)tok * A.k + 32 * q;
+    sp[t] = A.xs + tok;
+  }
+  const float* ws = A.ws + (size_t)(f0 / kKB) * A.blocks;
+  f32x4 acc[kF][kT] = {};
+  auto add = [&](const i32x8* w, const i32x8* x, int b) {
+    const float s = ws[b];
+    Operand<kExact> wo[kF], xo;
+#pragma unroll
+    for (int f = 0; f < kF; ++f) wo[f].set(w[f]);
+#pragma unroll
+    for (int t = 0; t < kT; ++t) {
+      const float c = sp[t][(size_t)b * A.m] * s;
+      xo.set(x[t]);
+#pragma unroll
+      for (int f = 0; f < kF; ++f) {
+        const f32x4 y = block_sum(wo[f], xo);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[f][t][e] = fmaf(y[e], c, acc[f][t][e]);
+      }
+    }
+  };
+  const int whole = A.k / kKB;
+#pragma unroll 2
+  for (int b = wave; b < whole; b += kSkinnyWaves) {
+    i32x8 w[kF], x[kT];
+#pragma unroll
+    for (int f = 0; f < kF; ++f) {
+      const i32x4* p = reinterpret_cast<const i32x4*>(wp[f] + (size_t)b * kKB);
+      w[f] = join(__builtin_nontemporal_load(p), __builtin_nontemporal_load(p + 1));
+    }
+#pragma unroll
+    for (int t = 0; t < kT; ++t) {
+      const i32x4* p = reinterpret_cast<const i32x4*>(xp[t] + (size_t)b * kKB);
+      x[t] = join(p[0], p[1]);
+    }
+    add(w, x, b);
+  }
+  if (whole < A.blocks && wave == whole % kSkinnyWaves) {  // the last block's values behind k are zero
+    const int left = A.k - whole * kKB - 32 * q;
+    auto get = [&](const uint8_t* base) {
+      const i32x4* p = reinterpret_cast<const i32x4*>(base + (size_t)whole * kKB);
+      return join(left > 0 ? p[0] : i32x4{}, left > 16 ? p[1] : i32x4{});
+    };
+    i32x8 w[kF], x[kT];
+#pragma unroll
+    for (int f = 0; f < kF; ++f) w[f] = get(wp[f]);
+#pragma unroll
+    for (int t = 0; t < kT; ++t) x[t] = get(xp[t]);
+    add(w, x, whole);
+  }
+#pragma unroll
+  for (int f = 0; f < kF; ++f)
+#pragma unroll
+    for (int t = 0; t < kT; ++t) sums[wave][f * kT + t][lane] = acc[f][t];
+  __syncthreads();
+  for (int s = threadIdx.x; s < kT * kF * 64; s += 64 * kSkinnyWaves) {
+    const int tile = s >> 6, l = s & 63;
+    f32x4 y = sums[0][tile][l];
+#pragma unroll
+    for (int v = 1; v < kSkinnyWaves; ++v) y += sums[v][tile][l];
+    store4(A, t0 + 16 * (tile % kT) + (l & 15), f0 + 16 * (tile / kT) + 4 * (l >> 4), y);
+  }
+}
+
+// ---- many tokens ---------------------------------------------------------------
+// Tiles of kTF features x kTT tokens, kWF x kWT waves.  A block of k of both
+// operands and of the tokens' scales goes from global memory straight into an
+// LDS stage while the block before it is multiplied.  Row r's 16-byte chunk c
+// sits at chunk position c ^ ((r >> 1) & 7) of its 128-byte row, so that the sixteen
+// rows of one operand read fall on sixteen different 16-byte bank groups.
+template <bool kExact, int kTF, int kTT, int kWF, int kWT>
+__global__ __launch_bounds__(64 * kWF * kWT) void linear_tile_kernel(LinearArgs A) {
+  constexpr int kWaves = kWF * kWT, kRows = kTF + kTT, kLoads = kRows / 8 / kWaves;
+  constexpr int kA = kTF / kWF / 16, kB = kTT / kWT / 16, kSlices = kTT / 64;
+  constexpr int kStage = kRows * kKB + kWaves * 256;
+  static_assert(kRows % (8 * kWaves) == 0 && kTF % (8 * kLoads) == 0, "a wave's rows are of one operand");
+  static_assert(128 % (kTF / kWF) == 0 || (kTF / kWF) % 128 == 0, "a wave's features share their scale");
+  static_assert(kTF / kWF <= 128 && kWaves >= kSlices, "");
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[2 * kStage];
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, i = lane & 15, q = lane >> 4;
+  // Tiles in groups of four token tiles; consecutive ones go to the same XCD
+  // (workgroup b runs on XCD b % 8) where the grid divides, so that what an
+  // XCD's L2 holds serves several tiles.
+  const int G = gridDim.x;
+  const int item = (G & 7) ? blockIdx.x : (blockIdx.x & 7) * (G >> 3) + (blockIdx.x >> 3);
+  const int group = item / (4 * A.tiles_f), gt = min(4, A.tiles_t - 4 * group), in = item - group * 4 * A.tiles_f;
+  const int f0 = in / gt * kTF, t0 = (4 * group + in % gt) * kTT;
+
+  // this lane's load sources: rows past the end re-read the last one (never stored)
+  const uint8_t* src[kLoads];
+#pragma unroll
+  for (int d = 0; d < kLoads; ++d) {
+    const int r = 8 * (kLoads * wave + d) + (lane >> 3), c = (lane & 7) ^ ((r >> 1) & 7);
+    src[d] = (r < kTF ? A.w + (size_t)min(f0 + r, A.n - 1) * A.k : A.x + (size_t)min(t0 + r - kTF, A.m - 1) * A.k) + 16 * c;
+  }
+  const int slice = wave % kSlices;
+  const float* ssrc = A.xs + min(t0 + 64 * slice + lane, A.m - 1);
+  auto issue = [&](int b) {
+    uint8_t* st = lds + (b & 1) * kStage;
+#pragma unroll
+    for (int d = 0; d < kLoads; ++d) dma16(src[d] + (size_t)b * kKB, st + 8 * (kLoads * wave + d) * kKB);
+    dma4(ssrc + (size_t)b * A.m, st + kRows * kKB + 256 * wave);
+  };
+
+  const int wf = wave / kWT, wt = wave % kWT, swz = (i >> 1) & 7;
+  const int offa = (kTF / kWF * wf + i) * kKB, offb = (kTF + kTT / kWT * wt + i) * kKB;
+  const int pos0 = (q ^ swz) * 16, pos1 = ((q | 4) ^ swz) * 16;
+  const int offs = kRows * kKB + 4 * (kTT / kWT * wt + i);
+  const float* ws = A.ws + (size_t)min((f0 + kTF / kWF * wf) / kKB, (A.n - 1) / kKB) * A.blocks;
+  f32x4 acc[kA][kB] = {};
+  auto multiply = [&](const uint8_t* st, float s) {
+    Operand<kExact> x[kB], w;
+    float c[kB];
+#pragma unroll
+    for (int b = 0; b < kB; ++b) {
+      const uint8_t* p = st + offb + b * 16 * kKB;
+      x[b].set(join(*reinterpret_cast<const i32x4*>(p + pos0), *reinterpret_cast<const i32x4*>(p + pos1)));
+      c[b] = *reinterpret_cast<const float*>(st + offs + 64 * b) * s;
+    }
+#pragma unroll
+    for (int a = 0; a < kA; ++a) {
+      const uint8_t* p = st + offa + a * 16 * kKB;
+      w.set(join(*reinterpret_cast<const i32x4*>(p + pos0), *reinterpret_cast<const i32x4*>(p + pos1)));
+#pragma unroll
+      for (int b = 0; b < kB; ++b) {
+        const f32x4 y = block_sum(w, x[b]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[a][b][e] = fmaf(y[e], c[b], acc[a][b][e]);
+      }
+    }
+  };
+
+  const int whole = A.k / kKB;
+  if (whole > 0) issue(0);
+  for (int b = 0; b < whole; ++b) {
+    const float s = ws[b];
+    wait_vmcnt<0>();
+    __builtin_amdgcn_s_waitcnt(0xC07F);  // this wave's LDS reads
+    barrier_no_fence();                  // block b is in LDS; every wave is done with block b - 1
+    if (b + 1 < whole) issue(b + 1);
+    multiply(lds + (b & 1) * kStage, s);
+  }
+  if (whole < A.blocks) {  // the last block: its values behind k are zero
+    __syncthreads();
+    const int chunks = (A.k - whole * kKB) / 16;
+    uint8_t* st = lds + (whole & 1) * kStage;
+#pragma unroll
+    for (int d = 0; d < kLoads; ++d) {
+      const int r = 8 * (kLoads * wave + d) + (lane >> 3), c = (lane & 7) ^ ((r >> 1) & 7);
+      i32x4 v{};
+      if (c < chunks) v = *reinterpret_cast<const i32x4*>(src[d] + (size_t)whole * kKB);
+      *reinterpret_cast<i32x4*>(st + r * kKB + (lane & 7) * 16) = v;
+    }
+    *reinterpret_cast<float*>(st + kRows * kKB + 256 * wave + 4 * lane) = ssrc[(size_t)whole * A.m];
+    __syncthreads();
+    multiply(st, ws[whole]);
+  }
+#pragma unroll
+  for (int a = 0; a < kA; ++a)
+#pragma unroll
+    for (int b = 0; b < kB; ++b)
+      store4(A, t0 + kTT / kWT * wt + 16 * b + i, f0 + kTF / kWF * wf + 16 * a + 4 * q, acc[a][b]);
+}
+
+}  // namespace
+}  // namespace gambit
+
+extern "C" gambit_status gambit_linear_fp8(int32_t m, int32_t n, int32_t k, const void* x, const float* x_scale,
+                                           const void* w, const float* w_scale, void* out, int32_t out_dtype,
+                                           void* stream) {
+  using namespace gambit;
+  if (m < 0 || n < 1 || k < 16 || k % 16 || (out_dtype != GAMBIT_BF16 && out_dtype != GAMBIT_F32)) return GAMBIT_ERR_INVALID;
+  if (m > 1 << 24 || n > 1 << 24) return GAMBIT_ERR_UNSUPPORTED;
+  if (m == 0) return GAMBIT_OK;
+  if (!x || !x_scale || !w || !w_scale || !out) return GAMBIT_ERR_INVALID;
+  for (const void* p : {x, w, static_cast<const void*>(out)})
+    if (reinterpret_cast<uintptr_t>(p) % 16) return GAMBIT_ERR_INVALID;
+  for (const float* p : {x_scale, w_scale})
+    if (reinterpret_cast<uintptr_t>(p) % 4) return GAMBIT_ERR_INVALID;
+  LinearArgs A{};
+  A.x = static_cast<const uint8_t*>(x);
+  A.xs = x_scale;
+  A.w = static_cast<const uint8_t*>(w);
+  A.ws = w_scale;
+  A.out = out;
+  A.m = m;
+  A.n = n;
+  A.k = k;
+  A.blocks = (k + kKB - 1) / kKB;
+  A.f32 = out_dtype == GAMBIT_F32;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  auto skinny = [&](auto kernel, int tokens, int features) {
+    hipLaunchKernelGGL(kernel, dim3((n + features - 1) / features, (m + tokens - 1) / tokens), dim3(64 * kSkinnyWaves), 0, s, A);
+  };
+  auto tile = [&](auto kernel, int features, int tokens, int threads) {
+    A.tiles_f = (n + features - 1) / features;
+    A.tiles_t = (m + tokens - 1) / tokens;
+    hipLaunchKernelGGL(kernel, dim3(A.tiles_f * A.tiles_t), dim3(threads), 0, s, A);
+  };
+  auto choose = [&](auto exact) {
+    constexpr bool kExact = decltype(exact)::value;
+    const bool wide = n >= 32 * 512;
+    if (m <= 16)
+      wide ? skinny(linear_skinny_kernel<kExact, 1, 2>, 16, 32) : skinny(linear_skinny_kernel<kExact, 1, 1>, 16, 16);
+    else if (m <= 32)
+      wide ? skinny(linear_skinny_kernel<kExact, 2, 2>, 32, 32) : skinny(linear_skinny_kernel<kExact, 2, 1>, 32, 16);
+    else if (m <= 64)
+      wide ? skinny(linear_skinny_kernel<kExact, 4, 2>, 64, 32) : skinny(linear_skinny_kernel<kExact, 4, 1>, 64, 16);
+    else if (m <= 128 && !wide)
+      skinny(linear_skinny_kernel<kExact, 8, 1>, 128, 16);
+    else if ((int64_t)((n + 255) / 256) * ((m + 255) / 256) >= 256)
+      tile(linear_tile_kernel<kExact, 256, 256, 2, 4>, 256, 256, 512);
+    else
+      tile(linear_tile_kernel<kExact, 128, 128, 2, 4>, 128, 128, 512);
+  };
+  A.f32 ? choose(std::true_type{}) : choose(std::false_type{});
+  return hipGetLastError() == hipSuccess ? GAMBIT_OK : GAMBIT_ERR_DEVICE;
+}

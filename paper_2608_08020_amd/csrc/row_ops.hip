@@ -1,0 +1,342 @@
+// Token rows between a layer's products: the residual's addition and the
+// root-mean-square norm, and rows as E4M3 codes with a scale for every 128
+// values - kernels and host entry points.
+//
+//     h = x + r,   y = w h / sqrt(mean(h^2) + eps)          gambit_rms_norm
+//     y = x   or   y = silu(a) b of a row's halves          gambit_quantize
+//     s = max(max |y| / 448, 2^-60) over 128 values, code = E4M3(y / s)
+//
+// Bound by HBM: a row is read once, 16 bytes a lane and load, and stays in
+// registers between its sum of squares and its output.  A lane holds eight
+// neighbouring values, so a group of 128 is sixteen neighbouring lanes, whose
+// largest magnitude takes four rotations within them.
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+#include <cstdint>
+
+#include "../../include/gambit.h"
+#include "fp8_codes.h"
+#include "kernels.h"
+
+namespace gambit {
+namespace {
+
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
+constexpr int kGroup = 128;             // values that share a scale
+constexpr float kLeastScale = 0x1p-60f;  // a group of smaller values has codes below one step
+constexpr int kMaxNormDim = 32768;
+
+struct RowArgs {
+  const void* x;               // row (i, j) at i * row_stride + j * head_stride values
+  int64_t row_stride, head_stride;
+  uint32_t rows, heads;        // rows in all, heads of each
+  int32_t dim;
+  const void* w;               // [dim]
+  int32_t w_f32;
+  float eps;
+  const void* res;             // [rows][dim]
+  void* res_out;
+  void* out;                   // [rows][dim]
+  int32_t out_dtype;
+  float* scale;                // [ceil(dim / 128)][rows]
+};
+
+__device__ inline uint32_t bf16_pair(float a, float b) {
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, bf16x2));
+}
+
+// Eight neighbouring values.
+struct Eight {
+  float v[8];
+};
+__device__ inline Eight from_bf16(uint4 a) {
+  return {{bf16_lo(a.x), bf16_hi(a.x), bf16_lo(a.y), bf16_hi(a.y), bf16_lo(a.z), bf16_hi(a.z), bf16_lo(a.w), bf16_hi(a.w)}};
+}
+template <bool kF32>
+__device__ inline Eight load8(const void* p, size_t at) {
+  if constexpr (kF32) {
+    const float4* q = reinterpret_cast<const float4*>(static_cast<const float*>(p) + at);
+    const float4 a = q[0], b = q[1];
+    return {{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}};
+  } else {
+    return from_bf16(*reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p) + at));
+  }
+}
+__device__ inline void store8_f32(void* p, size_t at, const Eight& y) {
+  float4* q = reinterpret_cast<float4*>(static_cast<float*>(p) + at);
+  q[0] = make_float4(y.v[0], y.v[1], y.v[2], y.v[3]);
+  q[1] = make_float4(y.v[4], y.v[5], y.v[6], y.v[7]);
+}
+__device__ inline void store8_bf16(void* p, size_t at, const Eight& y) {
+  *reinterpret_cast<uint4*>(static_cast<uint16_t*>(p) + at) = make_uint4(
+      bf16_pair(y.v[0], y.v[1]), bf16_pair(y.v[2], y.v[3]), bf16_pair(y.v[4], y.v[5]), bf16_pair(y.v[6], y.v[7]));
+}
+
+// The largest of sixteen neighbouring lanes, in each of them.
+template <int kBy>
+__device__ inline float ror_max(float m) {
+  const int o = __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, m), 0x120 + kBy, 0xf, 0xf, false);
+  return fmaxf(m, __builtin_bit_cast(float, o));
+}
+__device__ inline float max16(float m) { return ror_max<1>(ror_max<2>(ror_max<4>(ror_max<8>(m)))); }
+
+// The group's scale and this lane's eight codes.  NaN does not count for the
+// scale, an infinity counts as the largest finite value.
+__device__ inline uint2 codes8(const Eight& y, float* scale) {
+  float m = 0.f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) m = fmaxf(m, fabsf(y.v[i]));
+  m = fminf(max16(m), 0x1.fffffep127f);
+  constexpr float kInv = 1.f / 448.f;
+  const float q = m * kInv, s = fmaxf(fmaf(fmaf(-q, 448.f, m), kInv, q), kLeastScale);
+  // the hardware's reciprocal and one Newton step
+  const float r0 = __builtin_amdgcn_rcpf(s), r = fmaf(fmaf(-s, r0, 1.f), r0, r0);
+  *scale = s;
+  float c[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) c[i] = quotient(y.v[i], s, r);
+  return make_uint2(fp8_codes(c[0], c[1], c[2], c[3]), fp8_codes(c[4], c[5], c[6], c[7]));
+}
+
+// Sum over the kLanes neighbouring lanes of a row, the same in each of them.
+template <int kLanes>
+__device__ inline float row_sum(float x, float* lds) {
+#pragma unroll
+  for (int o = 1; o < (kLanes < 64 ? kLanes : 64); o <<= 1) x += __shfl_xor(x, o);
+  if constexpr (kLanes > 64) {
+    __syncthreads();  // an earlier sum has been read
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = x;
+    __syncthreads();
+    x = 0.f;
+#pragma unroll
+    for (int i = 0; i < kLanes / 64; ++i) x += lds[i];
+  }
+  return x;
+}
+
+// kLanes lanes a row, kVec loads of eight values a lane.
+// kRes: 0 no residual, 1 bf16, 2 fp32.
+template <int kLanes, int kVec, bool kX32, int kRes>
+__global__ __launch_bounds__(kLanes > 256 ? kLanes : 256) void rms_norm_kernel(RowArgs A) {
+  constexpr int kThreads = kLanes > 256 ? kLanes : 256;
+  __shared__ float sums[kThreads / 64];
+  const int l = threadIdx.x % kLanes;
+  const uint32_t row = blockIdx.x * (kThreads / kLanes) + threadIdx.x / kLanes;
+  const uint32_t r = row < A.rows ? row : A.rows - 1;  // rows past the end re-read the last one (never stored)
+  const size_t xat = (size_t)(r / A.heads) * A.row_stride + (size_t)(r % A.heads) * A.head_stride, at = (size_t)r * A.dim;
+  Eight h[kVec], res[kVec];
+  bool there[kVec];
+#pragma unroll
+  for (int i = 0; i < kVec; ++i) {
+    const int d = 8 * (i * kLanes + l);
+    there[i] = d < A.dim;
+    if (there[i]) {
+      h[i] = load8<kX32>(A.x, xat + d);
+      if constexpr (kRes) res[i] = load8<kRes == 2>(A.res, at + d);
+    } else {
+      h[i] = Eight{};
+      res[i] = Eight{};
+    }
+  }
+  float ss = 0.f;
+#pragma unroll
+  for (int i = 0; i < kVec; ++i)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      if constexpr (kRes) h[i].v[e] += res[i].v[e];
+      ss = fmaf(h[i].v[e], h[i].v[e], ss);
+    }
+  if constexpr (kRes) {
+    if (row < A.rows)
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) {
+        if (!there[i]) continue;
+        const int d = 8 * (i * kLanes + l);
+        if constexpr (kRes == 2)
+          store8_f32(A.res_out, at + d, h[i]);
+        else
+          store8_bf16(A.res_out, at + d, h[i]);
+      }
+  }
+  ss = row_sum<kLanes>(ss, sums);
+  float inv = 1.f / sqrtf(ss / A.dim + A.eps);
+  // Squares beyond fp32: the row over 2^72 (then 32768 of the largest stay inside), where eps is below its last bit.  (Every lane of a row takes the same way;
+  // rows of one workgroup that do not need it go along where they share its barriers: there is one row then.)
+  if (__builtin_expect(kLanes > 64 ? !(ss < INFINITY) : __any(!(ss < INFINITY)), 0)) {
+    const bool mine = !(ss < INFINITY);
+    float s2 = 0.f;
+#pragma unroll
+    for (int i = 0; i < kVec; ++i)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float x = h[i].v[e] * 0x1p-72f;
+        s2 = fmaf(x, x, s2);
+        if (mine) h[i].v[e] = x;
+      }
+    s2 = row_sum<kLanes>(s2, sums);
+    if (mine) inv = 1.f / sqrtf(s2 / A.dim);
+  }
+#pragma unroll
+  for (int i = 0; i < kVec; ++i) {
+    const int d = 8 * (i * kLanes + l);
+    Eight y{};
+    if (there[i]) {
+      const Eight w = A.w_f32 ? load8<true>(A.w, d) : load8<false>(A.w, d);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) y.v[e] = h[i].v[e] * inv * w.v[e];
+    }
+    if (A.out_dtype == GAMBIT_E4M3) {
+      float s;
+      const uint2 c = codes8(y, &s);
+      if (there[i] && row < A.rows) {
+        *reinterpret_cast<uint2*>(static_cast<uint8_t*>(A.out) + at + d) = c;
+        if (d % kGroup == 0) A.scale[(size_t)(d / kGroup) * A.rows + row] = s;
+      }
+    } else if (there[i] && row < A.rows) {
+      if (A.out_dtype == GAMBIT_F32)
+        store8_f32(A.out, at + d, y);
+      else
+        store8_bf16(A.out, at + d, y);
+    }
+  }
+}
+
+// a / (1 + e^-a), by the hardware's exponential and reciprocal: within 2^-21 + |a| 2^-23 of it, far below half a
+// step of a code (2^-4).  Of -inf it is -0, as where e^-a is beyond fp32.
+__device__ inline float silu(float a) {
+  const float e = __builtin_amdgcn_exp2f(a * -1.44269504f);
+  return fmaxf(a, -0x1p100f) * __builtin_amdgcn_rcpf(1.f + e);
+}
+
+// Sixteen lanes a group, kUnroll groups a lane.
+template <bool kX32, bool kGated>
+__global__ __launch_bounds__(256) void quantize_kernel(RowArgs A, uint32_t groups, uint32_t total) {
+  constexpr int kUnroll = kX32 && kGated ? 2 : 4;
+  const int l = threadIdx.x % 16;
+  const uint32_t g0 = blockIdx.x * (16 * kUnroll) + threadIdx.x / 16;
+  Eight a[kUnroll], b[kUnroll];
+#pragma unroll
+  for (int i = 0; i < kUnroll; ++i) {
+    const uint32_t g = g0 + 16 * i, row = g / groups;
+    const int d = (g % groups) * kGroup + 8 * l;
+    a[i] = Eight{};
+    b[i] = Eight{};
+    if (g < total && d < A.dim) {
+      a[i] = load8<kX32>(A.x, (size_t)row * A.row_stride + d);
+      if constexpr (kGated) b[i] = load8<kX32>(A.x, (size_t)row * A.row_stride + A.dim + d);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < kUnroll; ++i) {
+    const uint32_t g = g0 + 16 * i, row = g / groups;
+    const int d = (g % groups) * kGroup + 8 * l;
+    if constexpr (kGated)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) a[i].v[e] = silu(a[i].v[e]) * b[i].v[e];
+    float s;
+    const uint2 c = codes8(a[i], &s);
+    if (g < total && d < A.dim) {
+      *reinterpret_cast<uint2*>(static_cast<uint8_t*>(A.out) + (size_t)row * A.dim + d) = c;
+      if (l == 0) A.scale[(size_t)(g % groups) * A.rows + row] = s;
+    }
+  }
+}
+
+template <bool kX32, int kRes>
+void launch_norm(const RowArgs& A, hipStream_t s) {
+  auto go = [&](auto kernel, int lanes) {
+    const int threads = lanes > 256 ? lanes : 256, per = threads / lanes;
+    hipLaunchKernelGGL(kernel, dim3((A.rows + per - 1) / per), dim3(threads), 0, s, A);
+  };
+  // the fewest lanes and loads that hold a row
+  if (A.dim <= 128) return go(rms_norm_kernel<16, 1, kX32, kRes>, 16);
+  if (A.dim <= 512) return go(rms_norm_kernel<64, 1, kX32, kRes>, 64);
+  if (A.dim <= 1024) return go(rms_norm_kernel<64, 2, kX32, kRes>, 64);
+  if (A.dim <= 2048) return go(rms_norm_kernel<256, 1, kX32, kRes>, 256);
+  if (A.dim <= 4096) return go(rms_norm_kernel<256, 2, kX32, kRes>, 256);
+  if (A.dim <= 8192) return go(rms_norm_kernel<256, 4, kX32, kRes>, 256);
+  if (A.dim <= 16384) return go(rms_norm_kernel<1024, 2, kX32, kRes>, 1024);
+  return go(rms_norm_kernel<1024, 4, kX32, kRes>, 1024);
+}
+
+bool misaligned(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 != 0; }
+bool is_float(int32_t t) { return t == GAMBIT_BF16 || t == GAMBIT_F32; }
+
+}  // namespace
+}  // namespace gambit
+
+extern "C" {
+
+gambit_status gambit_rms_norm(int32_t n, int32_t heads, int32_t dim, const void* x, int32_t x_dtype, int64_t row_stride,
+                              int64_t head_stride, const void* weight, int32_t weight_dtype, float eps,
+                              const void* residual, void* residual_out, int32_t residual_dtype, void* out,
+                              int32_t out_dtype, float* out_scale, void* stream) {
+  using namespace gambit;
+  if (n < 0 || heads < 1 || dim < 8 || dim % 8) return GAMBIT_ERR_INVALID;
+  if (!is_float(x_dtype) || !is_float(weight_dtype) || (!is_float(out_dtype) && out_dtype != GAMBIT_E4M3)) return GAMBIT_ERR_INVALID;
+  if (!(eps >= 0x1p-80f && eps < INFINITY)) return GAMBIT_ERR_INVALID;
+  if (out_dtype == GAMBIT_E4M3 && dim % 16) return GAMBIT_ERR_INVALID;
+  if (residual && (!is_float(residual_dtype) || !residual_out)) return GAMBIT_ERR_INVALID;
+  if (dim > kMaxNormDim || (int64_t)n * heads > 0x7fffffff) return GAMBIT_ERR_UNSUPPORTED;
+  if (n == 0) return GAMBIT_OK;
+  const int per16 = x_dtype == GAMBIT_F32 ? 4 : 8;
+  if (!x || !weight || !out || (out_dtype == GAMBIT_E4M3 && (!out_scale || reinterpret_cast<uintptr_t>(out_scale) % 4))) return GAMBIT_ERR_INVALID;
+  if (misaligned(x) || misaligned(weight) || misaligned(out) || row_stride % per16 || head_stride % per16 || row_stride < 0 || head_stride < 0)
+    return GAMBIT_ERR_INVALID;
+  if (residual && (misaligned(residual) || misaligned(residual_out))) return GAMBIT_ERR_INVALID;
+  RowArgs A{};
+  A.x = x;
+  A.row_stride = row_stride;
+  A.head_stride = head_stride;
+  A.rows = (uint32_t)n * heads;
+  A.heads = heads;
+  A.dim = dim;
+  A.w = weight;
+  A.w_f32 = weight_dtype == GAMBIT_F32;
+  A.eps = eps;
+  A.res = residual;
+  A.res_out = residual_out;
+  A.out = out;
+  A.out_dtype = out_dtype;
+  A.scale = out_scale;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  const int res = !residual ? 0 : residual_dtype == GAMBIT_F32 ? 2 : 1;
+  if (x_dtype == GAMBIT_F32)
+    res == 0 ? launch_norm<true, 0>(A, s) : res == 1 ? launch_norm<true, 1>(A, s) : launch_norm<true, 2>(A, s);
+  else
+    res == 0 ? launch_norm<false, 0>(A, s) : res == 1 ? launch_norm<false, 1>(A, s) : launch_norm<false, 2>(A, s);
+  return hipGetLastError() == hipSuccess ? GAMBIT_OK : GAMBIT_ERR_DEVICE;
+}
+
+gambit_status gambit_quantize(int32_t n, int32_t dim, const void* x, int32_t x_dtype, int64_t row_stride, int32_t gated,
+                              void* out, float* out_scale, void* stream) {
+  using namespace gambit;
+  if (n < 0 || dim < 16 || dim % 16 || !is_float(x_dtype)) return GAMBIT_ERR_INVALID;
+  const int64_t groups = (dim + kGroup - 1) / kGroup, total = n * groups;
+  if (total > 0x7fffffff - 64) return GAMBIT_ERR_UNSUPPORTED;
+  if (n == 0) return GAMBIT_OK;
+  if (!x || !out || !out_scale || reinterpret_cast<uintptr_t>(out_scale) % 4 || misaligned(x) || misaligned(out) || row_stride < 0 || row_stride % (x_dtype == GAMBIT_F32 ? 4 : 8))
+    return GAMBIT_ERR_INVALID;
+  RowArgs A{};
+  A.x = x;
+  A.row_stride = row_stride;
+  A.rows = n;
+  A.heads = 1;
+  A.dim = dim;
+  A.out = out;
+  A.scale = out_scale;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  auto go = [&](auto kernel, int per) {
+    hipLaunchKernelGGL(kernel, dim3((unsigned)((total + per - 1) / per)), dim3(256), 0, s, A, (uint32_t)groups, (uint32_t)total);
+  };
+  if (x_dtype == GAMBIT_F32)
+    gated ? go(quantize_kernel<true, true>, 32) : go(quantize_kernel<true, false>, 64);
+  else
+    gated ? go(quantize_kernel<false, true>, 64) : go(quantize_kernel<false, false>, 64);
+  return hipGetLastError() == hipSuccess ? GAMBIT_OK : GAMBIT_ERR_DEVICE;
+}
+
+}  // extern "C"

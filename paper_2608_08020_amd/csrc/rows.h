@@ -68,9 +68,17 @@ static_assert(sizeof(WriteItem) == 16, "one scalar load");
 struct WriteLaunch {
   const WriteItem* items;
   int32_t n_items;
-  const int32_t* rows;     // [N] row of k / v of a packed token, or null: its own index
-  const uint16_t* k;       // [*][Hkv][128] bf16
+  const int32_t* at;       // [n_items] position of an item's block
+  const int32_t* rows;     // [N] row of k / v (and q) of a packed token, or null: its own index
+  const uint16_t* k;       // [*][Hkv][128] bf16, rows k_stride values apart
   const uint16_t* v;
+  int64_t k_stride, v_stride;
+  // rotated writes (table not null): keys, and the queries that go to q_out
+  const float* table;      // [position][rot]: rot / 2 cosines, rot / 2 sines
+  int32_t rot, pairs;      // values of a head that turn; pairs: (2i, 2i + 1), else (i, i + rot / 2)
+  const uint16_t* q;       // [*][Hq][128] bf16, rows q_stride values apart, or null
+  int64_t q_stride;
+  uint16_t* q_out;         // [N][Hq][128]
 };
 hipError_t launch_rows_write(const DevPool& P, const WriteLaunch& L, hipStream_t s);
 

@@ -1,6 +1,6 @@
 // Host side of the packed-token calls: layer writes (gambit_kv_write_layer),
 // prompt attention (gambit_prompt_attn) and draft-tree attention
-// (gambit_tree_attn) - validation against the host mirror and the plans that
+// (gambit_tree_attn), rotated writes (gambit_kv_write_rotated) - validation against the host mirror and the plans that
 // their kernels read.
 //
 // A call's plan depends on what it lists and on the mirror alone, so the
@@ -440,9 +440,12 @@ gambit_status tree_attn(gambit_pool* p, int32_t layer, int32_t n, const int32_t*
   return launch_rows(p, kTreePlan, layer, q, k_new, v_new, out, out_dtype, sm_scale, s);
 }
 
-gambit_status kv_write_layer(gambit_pool* p, int32_t layer, int32_t n, const int32_t* ids, const int32_t* pos0,
-                             const int32_t* ntok, const int32_t* rows, int32_t n_rows, const void* k, const void* v,
-                             hipStream_t s) {
+// Packed K and V (rows of the given strides) into a layer; a rotated write
+// carries its table, and the queries that turn along (W's fields).
+gambit_status write_layer(gambit_pool* p, int32_t layer, int32_t n, const int32_t* ids, const int32_t* pos0,
+                          const int32_t* ntok, const int32_t* rows, int32_t n_rows, const gambit::WriteLaunch& in,
+                          int32_t n_pos, hipStream_t s) {
+  const void *k = in.k, *v = in.v;
   int64_t total = 0;
   gambit_status st = check_call(p, layer, n, ids, ntok, s, &total);
   if (st) return st;
@@ -452,6 +455,8 @@ gambit_status kv_write_layer(gambit_pool* p, int32_t layer, int32_t n, const int
     if (pos0[i] < 0 || (int64_t)pos0[i] + ntok[i] > p->seq_len[t])
       return fail(p, GAMBIT_ERR_INVALID, "write of %d tokens at %d outside trace %d's %d positions", ntok[i], pos0[i], t,
                   p->seq_len[t]);
+    if (in.table && ntok[i] > 0 && pos0[i] + ntok[i] > n_pos)
+      return fail(p, GAMBIT_ERR_INVALID, "position %d of a table of %d", pos0[i] + ntok[i] - 1, n_pos);
   }
   if (n_rows < 0 || (!rows && n_rows != total))
     return fail(p, GAMBIT_ERR_INVALID, "%d rows of K and V for %lld tokens", n_rows, (long long)total);
@@ -469,12 +474,14 @@ gambit_status kv_write_layer(gambit_pool* p, int32_t layer, int32_t n, const int
   std::vector<int32_t> now = listing(n, ids, ntok, pos0, rows, (size_t)total);
   if (!kept(p, p->write.key, now)) {
     std::vector<WriteItem> items;
+    std::vector<int32_t> at;
     for (int i = 0, base = 0; i < n; base += ntok[i++]) {
       const int a = pos0[i], e = a + ntok[i];
       for (int j = a / 16; 16 * j < e && ntok[i] > 0; ++j) {
         const int r0 = std::max(a - 16 * j, 0), r1 = std::min(e - 16 * j, 16);
         const float floor = r0 ? 0.f : r1 == 16 ? 0x1p-20f : p->append_scale;
         items.push_back(WriteItem{p->table[ids[i]][j], base + 16 * j + r0 - a, (int16_t)r0, (int16_t)r1, floor});
+        at.push_back(16 * j);
       }
     }
     HIP_TRY(p, hipEventSynchronize(p->write.ev), "plan fence");
@@ -484,17 +491,55 @@ gambit_status kv_write_layer(gambit_pool* p, int32_t layer, int32_t n, const int
     W = gambit::WriteLaunch{};
     W.items = im.put(items.data(), items.size());
     W.n_items = (int)items.size();
+    W.at = im.put(at.data(), at.size());
     W.rows = rows ? im.put(rows, (size_t)total) : nullptr;
     if (!im.fits) return fail(p, GAMBIT_ERR_UNSUPPORTED, "plan exceeds workspace bounds");
     HIP_TRY(p, hipMemcpyAsync(im.dev, im.host, im.at, hipMemcpyHostToDevice, s), "plan upload");
     HIP_TRY(p, hipEventRecord(p->write.ev, s), "plan fence");
     keep(p, &p->write.key, std::move(now));
   }
-  gambit::WriteLaunch W = p->write.launch;
-  W.k = static_cast<const uint16_t*>(k);
-  W.v = static_cast<const uint16_t*>(v);
+  gambit::WriteLaunch W = in;
+  W.items = p->write.launch.items;
+  W.n_items = p->write.launch.n_items;
+  W.at = p->write.launch.at;
+  W.rows = p->write.launch.rows;
   HIP_TRY(p, gambit::launch_rows_write(p->dev.layer(layer), W, s), "layer write");
   return GAMBIT_OK;
+}
+
+gambit_status kv_write_layer(gambit_pool* p, int32_t layer, int32_t n, const int32_t* ids, const int32_t* pos0,
+                             const int32_t* ntok, const int32_t* rows, int32_t n_rows, const void* k, const void* v,
+                             hipStream_t s) {
+  gambit::WriteLaunch W{};
+  W.k = static_cast<const uint16_t*>(k);
+  W.v = static_cast<const uint16_t*>(v);
+  W.k_stride = W.v_stride = (int64_t)p->d.num_kv_heads * gambit::kHeadDim;
+  return write_layer(p, layer, n, ids, pos0, ntok, rows, n_rows, W, 0, s);
+}
+
+gambit_status kv_write_rotated(gambit_pool* p, int32_t layer, int32_t n, const int32_t* ids, const int32_t* pos0,
+                               const int32_t* ntok, const int32_t* rows, int32_t n_rows, const void* k, int64_t k_stride,
+                               const void* v, int64_t v_stride, const void* q, int64_t q_stride, void* q_out,
+                               const float* table, int32_t n_pos, int32_t rot, int32_t pairs, hipStream_t s) {
+  if (rot < 16 || rot > gambit::kHeadDim || rot % 16)
+    return fail(p, GAMBIT_ERR_INVALID, "%d rotated values of a head: a multiple of 16 up to %d", rot, gambit::kHeadDim);
+  if (!table || !aligned16(table) || n_pos < 1) return fail(p, GAMBIT_ERR_INVALID, "no table, or not 16-byte aligned");
+  if (k_stride < 0 || k_stride % 8 || v_stride < 0 || v_stride % 8 || (q && (q_stride < 0 || q_stride % 8)))
+    return fail(p, GAMBIT_ERR_INVALID, "a row stride is not a multiple of 8");
+  if (q && (!q_out || !aligned16(q) || !aligned16(q_out)))
+    return fail(p, GAMBIT_ERR_INVALID, "no output for the queries, or a buffer is not 16-byte aligned");
+  gambit::WriteLaunch W{};
+  W.k = static_cast<const uint16_t*>(k);
+  W.v = static_cast<const uint16_t*>(v);
+  W.k_stride = k_stride;
+  W.v_stride = v_stride;
+  W.table = table;
+  W.rot = rot;
+  W.pairs = pairs != 0;
+  W.q = static_cast<const uint16_t*>(q);
+  W.q_stride = q_stride;
+  W.q_out = static_cast<uint16_t*>(q_out);
+  return write_layer(p, layer, n, ids, pos0, ntok, rows, n_rows, W, n_pos, s);
 }
 
 // No exception leaves a C entry; one that ended a plan half made leaves the
@@ -521,6 +566,17 @@ gambit_status gambit_kv_write_layer(gambit_pool* p, int32_t layer, int32_t n, co
                                     const int32_t* ntok, const int32_t* rows, int32_t n_rows, const void* k,
                                     const void* v, void* stream) {
   return guarded(p, [&] { return kv_write_layer(p, layer, n, ids, pos0, ntok, rows, n_rows, k, v, S(stream)); });
+}
+
+gambit_status gambit_kv_write_rotated(gambit_pool* p, int32_t layer, int32_t n, const int32_t* ids, const int32_t* pos0,
+                                      const int32_t* ntok, const int32_t* rows, int32_t n_rows, const void* k,
+                                      int64_t k_stride, const void* v, int64_t v_stride, const void* q, int64_t q_stride,
+                                      void* q_out, const float* table, int32_t n_pos, int32_t rot, int32_t pairs,
+                                      void* stream) {
+  return guarded(p, [&] {
+    return kv_write_rotated(p, layer, n, ids, pos0, ntok, rows, n_rows, k, k_stride, v, v_stride, q, q_stride, q_out,
+                            table, n_pos, rot, pairs, S(stream));
+  });
 }
 
 gambit_status gambit_prompt_attn(gambit_pool* p, int32_t layer, int32_t n, const int32_t* ids, const int32_t* ntok,

@@ -10,6 +10,8 @@
 // bf16, eight segments of 2048 to 8192 tokens, 374 MB, 71 us, 5.3 TB/s; eight traces of
 // one to five tokens 3 us, latency; fp8, sixteen prompts of 256 to 1024 tokens,
 // 60 MB, 16 us (26 us with one workgroup for a block's K and V).
+#include "fp8_codes.h"
+#include "rotary.h"
 #include "rows.h"
 
 namespace gambit {
@@ -19,48 +21,76 @@ constexpr int kRow = kHeadDim * 2;  // bytes of a token's head in the caller's K
 
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
-// x / s rounded to fp32, r = 1 / s rounded: a product with the reciprocal and
-// one correction by the exact remainder is the rounded quotient (Markstein's
-// theorem).  Quotients beyond E4M3FN's range saturate whatever their last bits,
-// and so small ones that the remainder underflows have code zero.  (The
-// caller keeps the reciprocal inside fp32.)
-__device__ inline float quotient(float x, float s, float r) {
-  const float q = x * r, e = fmaf(-q, s, x);
-  return fabsf(q) < 512.f ? fmaf(e, r, q) : q;
-}
-
-// Nearest E4M3FN codes of four quotients (ties to even; beyond 448 saturating;
-// NaN stays), one byte each.
-__device__ inline uint32_t fp8_codes(float a, float b, float c, float d) {
-  const float y[4] = {a, b, c, d};
-  float z[4];
-  uint32_t nan = 0;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    z[i] = __builtin_amdgcn_fmed3f(y[i], -448.f, 448.f);
-    nan |= y[i] != y[i] ? 0xffu << (8 * i) : 0u;
-  }
-  int w = __builtin_amdgcn_cvt_pk_fp8_f32(z[0], z[1], 0, false);
-  w = __builtin_amdgcn_cvt_pk_fp8_f32(z[2], z[3], w, true);
-  return ((uint32_t)w & ~nan) | (0x7f7f7f7fu & nan);
-}
-
-__device__ inline float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
-__device__ inline float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
-
 __device__ inline size_t source_row(const WriteLaunch& L, int tok) { return L.rows ? L.rows[tok] : tok; }
 
-__global__ __launch_bounds__(256) void rows_write_bf16_kernel(DevPool P, WriteLaunch L) {
+// The queries of an item's tokens, turned: kQHeads heads of them from head h0.
+// A thread takes one unit of a token's head, two heads a pass.
+constexpr int kQHeads = 8;
+__device__ inline void rotate_queries(const DevPool& P, const WriteLaunch& L, const WriteItem& U, int at, int h0) {
+  const int row = (threadIdx.x & 127) >> 3, unit = threadIdx.x & 7, half = threadIdx.x >> 7;
+  if (row >= U.r1 - U.r0) return;
+  const int tok = U.src + row;
+  const bool turns = unit < L.rot / 16;
+  const Turn turn = load_turn(L.table + (size_t)(at + U.r0 + row) * L.rot, L.rot, turns ? unit : 0);
+  int c0, c1;
+  unit_chunks(unit, L.rot, L.pairs, &c0, &c1);
+  const uint16_t* src = L.q + source_row(L, tok) * L.q_stride;
+  uint16_t* dst = L.q_out + (size_t)tok * P.Hq * kHeadDim;
+  uint4 x[kQHeads / 2][2];
+#pragma unroll
+  for (int i = 0; i < kQHeads / 2; ++i) {
+    const int h = h0 + 2 * i + half;
+    if (h >= P.Hq) continue;
+    x[i][0] = *reinterpret_cast<const uint4*>(src + h * kHeadDim + 8 * c0);
+    x[i][1] = *reinterpret_cast<const uint4*>(src + h * kHeadDim + 8 * c1);
+  }
+#pragma unroll
+  for (int i = 0; i < kQHeads / 2; ++i) {
+    const int h = h0 + 2 * i + half;
+    if (h >= P.Hq) continue;
+    if (turns) turn_unit(x[i][0], x[i][1], turn, L.pairs);
+    *reinterpret_cast<uint4*>(dst + h * kHeadDim + 8 * c0) = x[i][0];
+    *reinterpret_cast<uint4*>(dst + h * kHeadDim + 8 * c1) = x[i][1];
+  }
+}
+
+// Chunk c of a head whose unit u lies in chunks c0 and c1 is one of the two.
+__device__ inline int unit_of(int c, int rot, int pairs) {
+  if (pairs || c >= rot / 8) return c >> 1;
+  return c < rot / 16 ? c : c - rot / 16;
+}
+
+// kTurn: the keys turn, and workgroups behind an item's heads turn its queries.
+template <bool kTurn>
+__global__ __launch_bounds__(256) void rows_write_bf16_kernel(DevPool P, WriteLaunch L, int parts) {
   constexpr int kVRow = kRow + 8, kKCol = kBlock * 16 + 16;
   __shared__ __attribute__((aligned(16))) uint8_t klds[16 * kKCol], vlds[kBlock * kVRow];
-  const int head = blockIdx.x % P.Hkv, t = threadIdx.x;
-  const WriteItem U = L.items[blockIdx.x / P.Hkv];
+  const int item = blockIdx.x / parts, head = blockIdx.x % parts, t = threadIdx.x;
+  const WriteItem U = L.items[item];
   const int r0 = U.r0, r1 = U.r1;
+  if constexpr (kTurn)
+    if (head >= P.Hkv) return rotate_queries(P, L, U, L.at[item], (head - P.Hkv) * kQHeads);
   {
     const int row = t >> 4, c = t & 15;
     // rows outside the write re-read one inside it (never stored)
-    const size_t src = (source_row(L, U.src + min(max(row, r0), r1 - 1) - r0) * P.Hkv + head) * kHeadDim + 8 * c;
-    const uint4 kk = *reinterpret_cast<const uint4*>(L.k + src), vv = *reinterpret_cast<const uint4*>(L.v + src);
+    const int in = min(max(row, r0), r1 - 1);
+    const size_t src = source_row(L, U.src + in - r0);
+    const uint16_t* ks = L.k + src * L.k_stride + head * kHeadDim;
+    const uint4 vv = *reinterpret_cast<const uint4*>(L.v + src * L.v_stride + head * kHeadDim + 8 * c);
+    uint4 kk;
+    if constexpr (kTurn) {
+      // a unit is two threads', each turns all of it and keeps its own chunk
+      const int unit = unit_of(c, L.rot, L.pairs);
+      const bool turns = unit < L.rot / 16;
+      const Turn turn = load_turn(L.table + (size_t)(L.at[item] + in) * L.rot, L.rot, turns ? unit : 0);
+      int c0, c1;
+      unit_chunks(unit, L.rot, L.pairs, &c0, &c1);
+      uint4 x0 = *reinterpret_cast<const uint4*>(ks + 8 * c0), x1 = *reinterpret_cast<const uint4*>(ks + 8 * c1);
+      if (turns) turn_unit(x0, x1, turn, L.pairs);
+      kk = c == c0 ? x0 : x1;
+    } else {
+      kk = *reinterpret_cast<const uint4*>(ks + 8 * c);
+    }
     *reinterpret_cast<uint4*>(klds + c * kKCol + k_phys(row) * 16) = kk;
     uint2* vd = reinterpret_cast<uint2*>(vlds + row * kVRow + c * 16);
     vd[0] = make_uint2(vv.x, vv.y);
@@ -87,11 +117,96 @@ __global__ __launch_bounds__(256) void rows_write_bf16_kernel(DevPool P, WriteLa
   }
 }
 
+// The turned keys of an item into an fp8 block.  A thread takes a unit of a
+// row, two heads a pass (kPasses in registers, so a block of at most eight heads
+// is read once, a larger one twice: magnitudes, then codes); a unit's two pieces
+// of eight codes pass LDS on their way into the tile's 16-byte chunks.
+__device__ inline void write_turned_keys(const DevPool& P, const WriteLaunch& L, const WriteItem& U, int at, uint8_t* lds,
+                                         uint32_t* most_s) {
+  constexpr int kPasses = 4, kHeads = 2 * kPasses, kTile = kBlock * kHeadDim;
+  const int t = threadIdx.x, half = t >> 7, row = (t & 127) >> 3, unit = t & 7, r0 = U.r0, r1 = U.r1;
+  const int in = min(max(row, r0), r1 - 1);  // rows outside the write re-read one inside it (never stored)
+  const bool turns = unit < L.rot / 16;
+  const Turn turn = load_turn(L.table + (size_t)(at + in) * L.rot, L.rot, turns ? unit : 0);
+  int c0, c1;
+  unit_chunks(unit, L.rot, L.pairs, &c0, &c1);
+  const uint16_t* src = L.k + source_row(L, U.src + in - r0) * L.k_stride;
+  float y[kPasses][16];  // a unit's chunks, turned
+  auto load = [&](int h0) {
+    uint4 x[kPasses][2];
+#pragma unroll
+    for (int i = 0; i < kPasses; ++i) {
+      const int h = min(h0 + 2 * i + half, P.Hkv - 1);
+      x[i][0] = *reinterpret_cast<const uint4*>(src + h * kHeadDim + 8 * c0);
+      x[i][1] = *reinterpret_cast<const uint4*>(src + h * kHeadDim + 8 * c1);
+    }
+#pragma unroll
+    for (int i = 0; i < kPasses; ++i) turn_unit_f32(x[i][0], x[i][1], turn, L.pairs, turns, y[i]);
+  };
+  float* scale_at = P.kv_scale + 2 * (size_t)U.blk;
+  float s;
+  load(0);
+  if (U.floor > 0.f) {
+    float most = 0.f;  // NaN counts for nothing, an infinity as the largest finite value
+    for (int h0 = 0; h0 < P.Hkv; h0 += kHeads) {
+      if (h0) load(h0);
+#pragma unroll
+      for (int i = 0; i < kPasses; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) most = fmaxf(most, fabsf(y[i][e]));
+    }
+#pragma unroll
+    for (int o = 32; o; o >>= 1) most = fmaxf(most, __shfl_xor(most, o));
+    if ((t & 63) == 0) most_s[t >> 6] = __float_as_uint(most);
+    __syncthreads();
+    most = fmaxf(fmaxf(__uint_as_float(most_s[0]), __uint_as_float(most_s[1])),
+                 fmaxf(__uint_as_float(most_s[2]), __uint_as_float(most_s[3])));
+    s = fmaxf(fminf(most, 0x1.fffffep127f) / 448.f, U.floor);
+    if (t == 0) *scale_at = s;
+    if (P.Hkv > kHeads) load(0);
+  } else {
+    s = *scale_at;
+  }
+  const bool tiny = fabsf(s) < 0x1p-64f;  // uniform; as for the values that do not turn
+  if (tiny) s *= 0x1p64f;
+  const float grow = tiny ? 0x1p64f : 1.f, r = fminf(1.f / s, 0x1.fffffep127f);
+  uint8_t* cache = P.k_cache + (size_t)U.blk * P.Hkv * kTile;
+  for (int h0 = 0; h0 < P.Hkv; h0 += kHeads) {
+    const int nh = min(kHeads, P.Hkv - h0);
+    if (h0) {
+      __syncthreads();  // the heads before are stored
+      load(h0);
+    }
+#pragma unroll
+    for (int i = 0; i < kPasses; ++i) {
+      if (2 * i >= nh) continue;  // uniform
+      float z[16];
+#pragma unroll
+      for (int e = 0; e < 16; ++e) z[e] = quotient(y[i][e] * grow, s, r);
+      // 8-code piece p of a head: chunk p / 2 of the tile, its row, half p % 2
+      uint8_t* tile = lds + (2 * i + half) * kTile + k_phys(row) * 16;
+      *reinterpret_cast<uint2*>(tile + (c0 >> 1) * (kBlock * 16) + (c0 & 1) * 8) =
+          make_uint2(fp8_codes(z[0], z[1], z[2], z[3]), fp8_codes(z[4], z[5], z[6], z[7]));
+      *reinterpret_cast<uint2*>(tile + (c1 >> 1) * (kBlock * 16) + (c1 & 1) * 8) =
+          make_uint2(fp8_codes(z[8], z[9], z[10], z[11]), fp8_codes(z[12], z[13], z[14], z[15]));
+    }
+    __syncthreads();
+    for (int i = t; i < nh * (kTile / 16); i += 256) {
+      const int kr = k_phys(i & 15);  // its own inverse
+      if (kr >= r0 && kr < r1) *reinterpret_cast<uint4*>(cache + (size_t)h0 * kTile + i * 16) = *reinterpret_cast<const uint4*>(lds + i * 16);
+    }
+  }
+}
+
 // blockIdx.y: 0 K, 1 V.  Two heads of the block a pass, a half of the workgroup
 // each, four passes in registers (so a block of at most eight heads is read
 // once, a larger one twice: magnitudes, then codes).  K: a thread takes 16 d of
 // a row, one 16-byte chunk of the tile, in the tile's order, so its stores need
 // no turning.  V: four tokens by four d, turned in LDS.
+//
+// kTurn: the keys turn in fp32 on the way (a scale goes by the turned values,
+// which are rounded once, to their codes); blockIdx.y from 2: the item's queries.
+template <bool kTurn>
 __global__ __launch_bounds__(256) void rows_write_fp8_kernel(DevPool P, WriteLaunch L) {
   constexpr int kPasses = 4, kHeads = 2 * kPasses, kTile = kBlock * kHeadDim;
   __shared__ __attribute__((aligned(16))) uint8_t lds[kHeads * kTile];
@@ -100,6 +215,10 @@ __global__ __launch_bounds__(256) void rows_write_fp8_kernel(DevPool P, WriteLau
   const bool is_v = blockIdx.y != 0;
   const WriteItem U = L.items[blockIdx.x];
   const int r0 = U.r0, r1 = U.r1;
+  if constexpr (kTurn) {
+    if (blockIdx.y >= 2) return rotate_queries(P, L, U, L.at[blockIdx.x], (blockIdx.y - 2) * kQHeads);
+    if (!is_v) return write_turned_keys(P, L, U, L.at[blockIdx.x], lds, most_s);
+  }
   // the thread's rows: K one, V four; rows outside the write re-read one inside it (never stored)
   const int krow = k_phys(u & 15), c = u >> 4;   // K: 16-byte chunk c of row krow
   const int tg = u >> 5, dg = u & 31;            // V: tokens 4 tg .., d 4 dg ..
@@ -107,7 +226,7 @@ __global__ __launch_bounds__(256) void rows_write_fp8_kernel(DevPool P, WriteLau
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int row = is_v ? 4 * tg + i : krow;
-    src[i] = source_row(L, U.src + min(max(row, r0), r1 - 1) - r0) * P.Hkv * kHeadDim + (is_v ? 4 * dg : 16 * c);
+    src[i] = source_row(L, U.src + min(max(row, r0), r1 - 1) - r0) * (is_v ? L.v_stride : L.k_stride) + (is_v ? 4 * dg : 16 * c);
   }
   uint4 x[kPasses][2];  // K: 16 values of a row; V: 4 values of 4 rows
   auto load = [&](int h0) {
@@ -218,10 +337,18 @@ __global__ __launch_bounds__(256) void rows_write_fp8_kernel(DevPool P, WriteLau
 
 hipError_t launch_rows_write(const DevPool& P, const WriteLaunch& L, hipStream_t s) {
   if (L.n_items <= 0) return hipSuccess;
-  if (P.esize == 2)
-    hipLaunchKernelGGL(rows_write_bf16_kernel, dim3((unsigned)L.n_items * P.Hkv), dim3(256), 0, s, P, L);
-  else
-    hipLaunchKernelGGL(rows_write_fp8_kernel, dim3(L.n_items, 2), dim3(256), 0, s, P, L);
+  const int parts = L.q ? (P.Hq + kQHeads - 1) / kQHeads : 0;
+  if (P.esize == 2) {
+    const dim3 grid((unsigned)L.n_items * (P.Hkv + parts));
+    if (L.table)
+      hipLaunchKernelGGL(rows_write_bf16_kernel<true>, grid, dim3(256), 0, s, P, L, P.Hkv + parts);
+    else
+      hipLaunchKernelGGL(rows_write_bf16_kernel<false>, grid, dim3(256), 0, s, P, L, P.Hkv);
+  } else if (L.table) {
+    hipLaunchKernelGGL(rows_write_fp8_kernel<true>, dim3(L.n_items, 2 + parts), dim3(256), 0, s, P, L);
+  } else {
+    hipLaunchKernelGGL(rows_write_fp8_kernel<false>, dim3(L.n_items, 2), dim3(256), 0, s, P, L);
+  }
   return hipGetLastError();
 }
 

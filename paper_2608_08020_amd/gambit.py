@@ -22,6 +22,9 @@ OK, ERR_INVALID, ERR_OUT_OF_BLOCKS, ERR_SHARED_WRITE, ERR_UNSUPPORTED, ERR_DEVIC
 KV_BF16, KV_FP8_E4M3 = 0, 1
 OUT_BF16, OUT_F32 = 0, 1
 OUT_CODES = {torch.float32: OUT_F32, torch.bfloat16: OUT_BF16}
+E4M3 = torch.float8_e4m3fn
+FLOAT_CODES = {torch.bfloat16: 0, torch.float32: 1}
+ROW_CODES = {**FLOAT_CODES, E4M3: 2}
 NEW_CACHE, NEW_BF16 = 0, 1
 UNIT_NARROW, UNIT_COOP_ONE, UNIT_COOP_TWO, UNIT_TAIL_SLOT, UNIT_NARROW_TWO = 1, 2, 4, 16, 32
 CODE_NAMES = {ERR_INVALID: "INVALID", ERR_OUT_OF_BLOCKS: "OUT_OF_BLOCKS",
@@ -92,7 +95,8 @@ EXPORTS = ["gambit_workspace_size", "gambit_pool_create", "gambit_pool_destroy",
            "gambit_scorer_destroy", "gambit_scorer_step", "gambit_scorer_fork", "gambit_scorer_free",
            "gambit_scorer_steps", "gambit_scorer_check", "gambit_scorer_last_error", "gambit_stream_read",
            "gambit_plan_kinds", "gambit_mlp_score_static", "gambit_kv_write_layer", "gambit_prompt_attn",
-           "gambit_tree_attn"]
+           "gambit_tree_attn", "gambit_kv_write_rotated", "gambit_rms_norm", "gambit_quantize", "gambit_linear_fp8",
+           "gambit_rotate", "gambit_sample"]
 
 
 def lib() -> ctypes.CDLL:
@@ -102,7 +106,7 @@ def lib() -> ctypes.CDLL:
     if not os.path.exists(LIB_PATH):
         raise RuntimeError(f"{LIB_PATH} is not built; run `python -m paper_2608_08020_amd.build`")
     L = ctypes.CDLL(LIB_PATH)
-    vp, i32, f32 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_float
+    vp, i32, i64, f32 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float
     sig = {
         "gambit_workspace_size": (ctypes.c_size_t, [ctypes.POINTER(PoolDesc)]),
         "gambit_pool_create": (i32, [ctypes.POINTER(PoolDesc), vp, ctypes.POINTER(vp)]),
@@ -145,6 +149,13 @@ def lib() -> ctypes.CDLL:
         "gambit_prompt_attn": (i32, [vp, i32, i32, vp, vp, vp, vp, i32, f32, vp]),
         "gambit_tree_attn": (i32, [vp, i32, i32, vp, vp, vp, vp, vp, vp, vp, i32, f32, vp]),
         "gambit_mlp_score_static": (i32, [i32, vp, ctypes.POINTER(Mlp), vp, vp, i32, vp, vp]),
+        "gambit_kv_write_rotated": (i32, [vp, i32, i32, vp, vp, vp, vp, i32, vp, i64, vp, i64, vp, i64, vp, vp, i32, i32,
+                                          i32, vp]),
+        "gambit_rms_norm": (i32, [i32, i32, i32, vp, i32, i64, i64, vp, i32, f32, vp, vp, i32, vp, i32, vp, vp]),
+        "gambit_quantize": (i32, [i32, i32, vp, i32, i64, i32, vp, vp, vp]),
+        "gambit_linear_fp8": (i32, [i32, i32, i32, vp, vp, vp, vp, vp, i32, vp]),
+        "gambit_rotate": (i32, [i32, i32, i32, vp, i64, vp, i64, vp, vp, i32, i32, i32, vp, vp, vp]),
+        "gambit_sample": (i32, [i32, i32, vp, i32, i64, vp, vp, f32, vp, i32, vp, f32, vp, f32, vp, vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(L, name)
@@ -295,6 +306,192 @@ def stream_read(buf: torch.Tensor, nontemporal: bool, grid: int, sink: torch.Ten
                                   int(grid), sink.data_ptr(), _stream(stream))
     if st != OK:
         raise GambitError(st, "stream_read")
+
+
+# -- what a layer does between its attention calls
+
+def _strided(t: torch.Tensor, dtypes, shape, what: str):
+    """Address and outer strides of a device tensor of rows: the last dimension dense, the others of any stride >= 0
+    (that of a dimension of one does not matter)."""
+    if not isinstance(t, torch.Tensor):
+        raise ValueError(f"{what}: expected a tensor, got {type(t).__name__}")
+    if t.dtype not in dtypes:
+        raise ValueError(f"{what}: expected dtype {tuple(dtypes)}, got {t.dtype}")
+    if shape is not None and t.shape != shape:
+        raise ValueError(f"{what}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
+    if not t.is_cuda:
+        raise ValueError(f"{what}: expected a device tensor")
+    if t.stride(-1) != 1 and t.shape[-1] > 1:
+        raise ValueError(f"{what}: expected a dense last dimension")
+    return t.data_ptr()
+
+
+def _outer(t: torch.Tensor, i: int) -> int:
+    return t.stride(i) if t.shape[i] > 1 else 0
+
+
+def _here(t: torch.Tensor, *others):
+    """All of a call's tensors are the current device's."""
+    d = t.get_device()
+    if d != torch.cuda.current_device():
+        raise ValueError(f"the tensors are on device {d}, device {torch.cuda.current_device()} is current")
+    for o in others:
+        if o is not None and o.get_device() != d:
+            raise ValueError(f"tensors on devices {d} and {o.get_device()}")
+
+
+def rms_norm(x: torch.Tensor, weight: torch.Tensor, eps: float = 1e-6, residual: torch.Tensor | None = None,
+             residual_out: torch.Tensor | None = None, out_dtype=torch.bfloat16, out: torch.Tensor | None = None,
+             out_scale: torch.Tensor | None = None, stream=None):
+    """gambit_rms_norm of x [n][dim] or [n][heads][dim] (bf16 or fp32, dense last dimension), after the addition of
+    `residual`; residual_out (default: residual itself) takes the sum.  Returns out, or (codes, scales
+    [ceil(dim / 128)][rows]) for out_dtype float8_e4m3fn."""
+    if x.dim() not in (2, 3):
+        raise ValueError("x: expected [n][dim] or [n][heads][dim]")
+    shape, dim = x.shape, x.shape[-1]
+    n, heads = shape[0], shape[1] if len(shape) == 3 else 1
+    xp = _strided(x, FLOAT_CODES, None, "x")
+    if out is None:
+        out = torch.empty(shape, dtype=out_dtype, device=x.device)
+    if out.dtype not in ROW_CODES:
+        raise ValueError(f"out: expected dtype {tuple(ROW_CODES)}, got {out.dtype}")
+    op = _dev(out, None, shape, "out")
+    wp = _dev(weight, (torch.bfloat16, torch.float32), (dim,), "weight")
+    fp8, sp = out.dtype is E4M3, None
+    if fp8:
+        if out_scale is None:
+            out_scale = torch.empty((-(-dim // 128), n * heads), dtype=torch.float32, device=x.device)
+        sp = _dev(out_scale, torch.float32, (-(-dim // 128), n * heads), "out_scale")
+    elif out_scale is not None:
+        raise ValueError("out_scale: only E4M3 rows have scales")
+    rp = rop = None
+    rd = 0
+    if residual is not None:
+        if residual_out is None:
+            residual_out = residual
+        rp, rd = _dev(residual, (torch.bfloat16, torch.float32), shape, "residual"), FLOAT_CODES[residual.dtype]
+        rop = _dev(residual_out, residual.dtype, shape, "residual_out")
+    elif residual_out is not None:
+        raise ValueError("residual_out: there is no residual")
+    _here(x, weight, out, out_scale, residual, residual_out)
+    st = lib().gambit_rms_norm(n, heads, dim, xp, FLOAT_CODES[x.dtype], _outer(x, 0), _outer(x, 1) if len(shape) == 3 else 0,
+                               wp, FLOAT_CODES[weight.dtype], eps, rp, rop, rd, op, ROW_CODES[out.dtype], sp, _stream(stream))
+    if st != OK:
+        raise GambitError(st, "rms_norm")
+    return (out, out_scale) if fp8 else out
+
+
+def quantize(x: torch.Tensor, gated: bool = False, out: torch.Tensor | None = None, out_scale: torch.Tensor | None = None,
+             stream=None):
+    """gambit_quantize of rows x [n][dim], or [n][2 dim] with gated (silu of the first half times the second):
+    (codes [n][dim] float8_e4m3fn, scales [ceil(dim / 128)][n])."""
+    if x.dim() != 2 or (gated and x.shape[1] % 2):
+        raise ValueError("x: expected [n][dim], or [n][2 dim] when gated")
+    n, dim = x.shape[0], x.shape[1] // 2 if gated else x.shape[1]
+    xp = _strided(x, FLOAT_CODES, None, "x")
+    if out is None:
+        out = torch.empty((n, dim), dtype=E4M3, device=x.device)
+    if out_scale is None:
+        out_scale = torch.empty((-(-dim // 128), n), dtype=torch.float32, device=x.device)
+    op = _dev(out, E4M3, (n, dim), "out")
+    sp = _dev(out_scale, torch.float32, (-(-dim // 128), n), "out_scale")
+    _here(x, out, out_scale)
+    st = lib().gambit_quantize(n, dim, xp, FLOAT_CODES[x.dtype], _outer(x, 0), gated, op, sp, _stream(stream))
+    if st != OK:
+        raise GambitError(st, "quantize")
+    return out, out_scale
+
+
+def linear_fp8(x: torch.Tensor, x_scale: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor,
+               out: torch.Tensor | None = None, out_dtype=torch.bfloat16, stream=None) -> torch.Tensor:
+    """gambit_linear_fp8: x [m][k] times w [n][k], both float8_e4m3fn with scales [ceil(k / 128)][m] and
+    [ceil(n / 128)][ceil(k / 128)]; out [m][n] in bf16 or fp32."""
+    if x.dim() != 2 or w.dim() != 2:
+        raise ValueError("x: expected [m][k], w: expected [n][k]")
+    m, k = x.shape
+    n = w.shape[0]
+    blocks = -(-k // 128)
+    xp, wp = _dev(x, E4M3, None, "x"), _dev(w, E4M3, (n, k), "w")
+    xsp = _dev(x_scale, torch.float32, (blocks, m), "x_scale")
+    wsp = _dev(w_scale, torch.float32, (-(-n // 128), blocks), "w_scale")
+    if out is None:
+        out = torch.empty((m, n), dtype=out_dtype, device=x.device)
+    if out.dtype not in OUT_CODES:
+        raise ValueError(f"out: expected dtype {tuple(OUT_CODES)}, got {out.dtype}")
+    op = _dev(out, None, (m, n), "out")
+    _here(x, x_scale, w, w_scale, out)
+    st = lib().gambit_linear_fp8(m, n, k, xp, xsp, wp, wsp, op, OUT_CODES[out.dtype], _stream(stream))
+    if st != OK:
+        raise GambitError(st, "linear_fp8")
+    return out
+
+
+def _heads(t: torch.Tensor, n: int, what: str):
+    """Address and row stride of token rows [n][heads][128] whose heads lie one after another."""
+    if not isinstance(t, torch.Tensor) or t.dim() != 3:
+        raise ValueError(f"{what}: expected a tensor [n][heads][128]")
+    p = _strided(t, (torch.bfloat16,), (n, t.shape[1], 128), what)
+    if t.shape[1] > 1 and t.stride(1) != 128:
+        raise ValueError(f"{what}: expected a token's heads one after another")
+    return p, _outer(t, 0)
+
+
+def rotate(q: torch.Tensor | None, k: torch.Tensor | None, positions: torch.Tensor, table: torch.Tensor,
+           pairs: bool = False, q_out: torch.Tensor | None = None, k_out: torch.Tensor | None = None, stream=None):
+    """gambit_rotate: (q_out, k_out), queries and keys [n][heads][128] bf16 turned by the table's rows [n_pos][rot]
+    (rot / 2 cosines, rot / 2 sines, fp32) of their positions (int32 [n], on the device)."""
+    if table.dim() != 2:
+        raise ValueError("table: expected [n_pos][rot]")
+    if q is None and k is None:
+        raise ValueError("q, k: nothing to turn")
+    n = (k if q is None else q).shape[0]
+    tp = _dev(table, torch.float32, None, "table")
+    pp = _dev(positions, torch.int32, (n,), "positions")
+    side = []
+    for x, out, what in ((q, q_out, "q"), (k, k_out, "k")):
+        if x is None:
+            if out is not None:
+                raise ValueError(f"{what}_out: there is no {what}")
+            side.append((0, None, 0, None, None))
+            continue
+        xp, stride = _heads(x, n, what)
+        if out is None:
+            out = torch.empty(x.shape, dtype=torch.bfloat16, device=x.device)
+        side.append((x.shape[1], xp, stride, out, _dev(out, torch.bfloat16, x.shape, what + "_out")))
+    (hq, qp, qs, q_out, qop), (hk, kp, ks, k_out, kop) = side
+    _here(table, q, k, positions, q_out, k_out)
+    st = lib().gambit_rotate(n, hq, hk, qp, qs, kp, ks, pp, tp, table.shape[0], table.shape[1], pairs, qop, kop,
+                             _stream(stream))
+    if st != OK:
+        raise GambitError(st, "rotate")
+    return q_out, k_out
+
+
+def sample(logits: torch.Tensor, u: torch.Tensor, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0,
+           out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """gambit_sample: one token id (int32) a row of logits [n][vocab] (bf16 or fp32) from the random numbers u [n]
+    (fp32, in [0, 1)); each parameter is a number, or a device tensor [n] (fp32; top_k int32)."""
+    if logits.dim() != 2:
+        raise ValueError("logits: expected [n][vocab]")
+    n, vocab = logits.shape
+    zp = _strided(logits, FLOAT_CODES, None, "logits")
+    up = _dev(u, torch.float32, (n,), "u")
+    args, given = [], []
+    for x, dt, what in ((temperature, torch.float32, "temperature"), (top_k, torch.int32, "top_k"),
+                        (top_p, torch.float32, "top_p"), (min_p, torch.float32, "min_p")):
+        if isinstance(x, torch.Tensor):
+            args += [_dev(x, dt, (n,), what), 0]
+            given.append(x)
+        else:
+            args += [None, x]
+    if out is None:
+        out = torch.empty(n, dtype=torch.int32, device=logits.device)
+    op = _dev(out, torch.int32, (n,), "out")
+    _here(logits, u, out, *given)
+    st = lib().gambit_sample(n, vocab, zp, FLOAT_CODES[logits.dtype], _outer(logits, 0), up, *args, op, _stream(stream))
+    if st != OK:
+        raise GambitError(st, "sample")
+    return out
 
 
 class Pool:
@@ -464,6 +661,45 @@ class Pool:
         self._check(lib().gambit_kv_write_layer(self._h, layer, ids.size, _in(ids), _in(p0), _in(nt),
                                                 None if rows is None else _in(rows), n_rows, kp, vp,
                                                 _stream(stream)), "kv_write_layer")
+
+    def kv_write_rotated(self, layer: int, ids, pos0, n_tokens, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor,
+                         q: torch.Tensor | None = None, q_out: torch.Tensor | None = None, rows=None,
+                         pairs: bool = False, stream=None) -> torch.Tensor | None:
+        """gambit_kv_write_rotated: kv_write_layer with keys, and queries q [n_rows][Hq][D], turned by the table
+        [n_pos][rot] (fp32) on the way; k, v and q may be parts of packed rows.  Returns q_out [total][Hq][D]."""
+        ids, nt, total = self._packed(ids, n_tokens, "n_tokens")
+        p0 = _host_i32(pos0)
+        if p0.shape != ids.shape:
+            raise ValueError("pos0: expected one per trace")
+        n_rows = total
+        if rows is not None:
+            rows = _host_i32(rows)
+            if rows.shape != (total,):
+                raise ValueError(f"rows: expected {total}, got {rows.shape}")
+            n_rows = k.shape[0]
+        if table.dim() != 2:
+            raise ValueError("table: expected [n_pos][rot]")
+        tp = _dev(table, torch.float32, None, "table")
+        (kp, ks), (vp, vs) = _heads(k, n_rows, "k"), _heads(v, n_rows, "v")
+        if k.shape[1] != self.Hkv or v.shape[1] != self.Hkv:
+            raise ValueError(f"k, v: expected {self.Hkv} heads, got {k.shape[1]} and {v.shape[1]}")
+        qp = qop = None
+        qs = 0
+        if q is not None:
+            qp, qs = _heads(q, n_rows, "q")
+            if q.shape[1] != self.Hq:
+                raise ValueError(f"q: expected {self.Hq} heads, got {q.shape[1]}")
+            shape = (total, self.Hq, self.D)
+            if q_out is None:
+                q_out = torch.empty(shape, dtype=torch.bfloat16, device=q.device)
+            qop = _dev(q_out, torch.bfloat16, shape, "q_out")
+        elif q_out is not None:
+            raise ValueError("q_out: there are no queries")
+        self._check(lib().gambit_kv_write_rotated(self._h, layer, ids.size, _in(ids), _in(p0), _in(nt),
+                                                  None if rows is None else _in(rows), n_rows, kp, ks, vp, vs, qp, qs, qop,
+                                                  tp, table.shape[0], table.shape[1], pairs, _stream(stream)),
+                    "kv_write_rotated")
+        return q_out
 
     def _attn_io(self, total: int, q: torch.Tensor, out, out_dtype):
         """The queries' address, the output and its code."""

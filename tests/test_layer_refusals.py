@@ -1,0 +1,105 @@
+"""Refused calls of the layer operators: decided on the host before any device work, so they run without a GPU."""
+import math
+import os
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import layer
+from paper_2608_08020_amd import gambit as g
+
+pytestmark = pytest.mark.skipif(not os.path.exists(g.LIB_PATH), reason="libgambit.so not built")
+P = 1 << 20  # stands for an aligned device address that is never touched
+BAD, TOO_BIG = g.ERR_INVALID, g.ERR_UNSUPPORTED
+
+
+def _call(name, good, status, **change):
+    args = dict(good, **change)
+    assert getattr(g.lib(), name)(*args.values()) == status, change
+
+
+NORM = dict(n=4, heads=1, dim=128, x=P, xd=0, rs=128, hs=0, w=P, wd=0, eps=1e-6, r=P, ro=P, rd=0, out=P, od=2, sc=P, stream=None)
+
+
+@pytest.mark.parametrize("change", [dict(n=-1), dict(heads=0), dict(dim=0), dict(dim=12, od=0), dict(dim=136), dict(xd=2), dict(wd=7), dict(od=3), dict(rd=2),
+                                    dict(eps=0.0), dict(eps=-1.0), dict(eps=math.nan), dict(eps=math.inf), dict(eps=1e-30), dict(x=None), dict(w=None), dict(out=None), dict(sc=None),
+                                    dict(ro=None), dict(x=P + 8), dict(w=P + 2), dict(out=P + 4), dict(r=P + 8), dict(ro=P + 8), dict(rs=130), dict(hs=4), dict(rs=-128),
+                                    dict(xd=1, rs=130)])
+def test_rms_norm(change):
+    _call("gambit_rms_norm", NORM, BAD, **change)
+
+
+def test_sizes_beyond_the_kernels():
+    _call("gambit_rms_norm", NORM, TOO_BIG, dim=32784, rs=32784)
+    _call("gambit_rms_norm", NORM, TOO_BIG, n=1 << 20, heads=1 << 12)
+    _call("gambit_quantize", QUANT, TOO_BIG, n=1 << 30, dim=1024)
+    _call("gambit_linear_fp8", LINEAR, TOO_BIG, m=(1 << 24) + 1)
+    _call("gambit_linear_fp8", LINEAR, TOO_BIG, n=(1 << 24) + 1)
+    _call("gambit_rotate", ROTATE, TOO_BIG, hq=5000)
+    _call("gambit_rotate", ROTATE, TOO_BIG, n=1 << 30)
+    _call("gambit_sample", SAMPLE, TOO_BIG, vocab=(1 << 18) + 1)
+
+
+def test_nothing_to_do():
+    for name, good in (("gambit_rms_norm", NORM), ("gambit_quantize", QUANT), ("gambit_rotate", ROTATE), ("gambit_sample", SAMPLE)):
+        _call(name, good, g.OK, n=0)
+    _call("gambit_linear_fp8", LINEAR, g.OK, m=0)
+
+
+QUANT = dict(n=4, dim=128, x=P, xd=0, rs=128, gated=0, out=P, sc=P, stream=None)
+
+
+@pytest.mark.parametrize("change", [dict(n=-1), dict(dim=0), dict(dim=24), dict(xd=2), dict(x=None), dict(out=None), dict(sc=None), dict(x=P + 2), dict(out=P + 8),
+                                    dict(rs=129), dict(rs=-8), dict(xd=1, rs=130)])
+def test_quantize(change):
+    _call("gambit_quantize", QUANT, BAD, **change)
+
+
+LINEAR = dict(m=4, n=8, k=128, x=P, xs=P, w=P, ws=P, out=P, od=0, stream=None)
+
+
+@pytest.mark.parametrize("change", [dict(m=-1), dict(n=0), dict(k=0), dict(k=120), dict(od=2), dict(x=None), dict(xs=None), dict(w=None), dict(ws=None), dict(out=None),
+                                    dict(x=P + 8), dict(w=P + 4), dict(out=P + 2), dict(xs=P + 2), dict(ws=P + 1)])
+def test_linear_fp8(change):
+    _call("gambit_linear_fp8", LINEAR, BAD, **change)
+
+
+ROTATE = dict(n=4, hq=8, hk=2, q=P, qs=1024, k=P, ks=256, pos=P, table=P, n_pos=9, rot=128, pairs=0, qo=P, ko=P, stream=None)
+
+
+@pytest.mark.parametrize("change", [dict(n=-1), dict(hq=-1), dict(hk=-2), dict(rot=0), dict(rot=24), dict(rot=144), dict(n_pos=0), dict(q=None), dict(k=None), dict(qo=None),
+                                    dict(ko=None), dict(pos=None), dict(table=None), dict(table=P + 4), dict(q=P + 8), dict(ko=P + 2), dict(qs=1020), dict(ks=-256),
+                                    dict(pos=P + 2)])
+def test_rotate(change):
+    _call("gambit_rotate", ROTATE, BAD, **change)
+
+
+SAMPLE = dict(n=4, vocab=100, z=P, zd=0, rs=100, u=P, t=None, t1=1.0, k=None, k1=0, p=None, p1=1.0, m=None, m1=0.0, out=P, stream=None)
+
+
+@pytest.mark.parametrize("change", [dict(n=-1), dict(vocab=0), dict(zd=2), dict(rs=-1), dict(z=None), dict(u=None), dict(out=None), dict(z=P + 1), dict(zd=1, z=P + 2),
+                                    dict(u=P + 2), dict(out=P + 1), dict(t=P + 1), dict(k=P + 2), dict(p=P + 2), dict(m=P + 3)])
+def test_sample(change):
+    _call("gambit_sample", SAMPLE, BAD, **change)
+
+
+def test_binding_refuses_tensors_of_another_kind():
+    x = torch.zeros(4, 128, dtype=torch.bfloat16)
+    f = torch.zeros(1, 4)
+    for call in (lambda: g.rms_norm(x, x[0]), lambda: g.quantize(x), lambda: g.linear_fp8(x, f, x, f), lambda: g.sample(x, f[0]),
+                 lambda: g.rotate(x.view(4, 1, 128), None, f[0], f), lambda: g.rms_norm(x.half(), x[0]), lambda: g.rms_norm(x[0], x[0]), lambda: g.quantize(x[:, :127], gated=True),
+                 lambda: g.sample(x[0], f[0]), lambda: g.rotate(None, None, f[0], f), lambda: g.rms_norm(x.T, x[0])):
+        with pytest.raises(ValueError):
+            call()
+
+
+def test_the_oracle_draws_as_described():
+    z = [0.0, 1.0, 1.0, -math.inf, 2.0]
+    w = np.exp([0.0, 1.0, 1.0, -math.inf, 2.0])
+    for u in np.linspace(0, 0.999, 50):
+        assert layer.draw(z, u) == int(np.flatnonzero(np.cumsum(w) > u * w.sum())[0])
+    assert layer.draw(z, 0.99, top_k=2) == 4 and layer.draw(z, 0.01, top_k=2) == 1   # of the equal ones the lower index
+    assert layer.draw(z, 0.5, top_p=0.3) == 4 and layer.draw(z, 0.0, top_p=w[4] / w.sum() + 1e-9) == 1
+    assert layer.draw(z, 0.0, min_p=0.9) == 4 and layer.draw(z, 0.0, temperature=0.0) == 4
+    assert layer.draw([math.nan, -math.inf], 0.3) == -1
