@@ -581,8 +581,8 @@ const char* gambit_scorer_last_error(const gambit_scorer* scorer);
 
 /*
  * What a model's layer does between its attention calls, on rows of tokens.
- * These calls hold no state and take no workspace: they may run on several
- * streams at once and be captured into a graph.  Device buffers are those of
+ * These calls hold no state: they may run on several streams at once and be
+ * captured into a graph.  Device buffers are those of
  * the current device, 16-byte aligned unless a line says otherwise; n (or m)
  * = 0 does nothing.  GAMBIT_ERR_INVALID for a bad argument, GAMBIT_ERR_
  * UNSUPPORTED for a size beyond the kernels', GAMBIT_ERR_DEVICE when the launch
@@ -661,19 +661,23 @@ gambit_status gambit_rotate(int32_t n, int32_t q_heads, int32_t k_heads, const v
  * lower index).  In logits NaN counts as -inf (which is never drawn), +inf as
  * the largest finite value; a row that holds nothing else gives -1.  u below 0
  * or NaN counts as 0; from 1 on, the last kept index.
- * Weights are rounded to 2^-S, S = 62 - ceil(log2(vocab)), at most 50; sums
- * are exact.
+ * Weights are rounded to 2^-44 of the largest or finer; their sums are exact.
  *   logits    device, GAMBIT_BF16 or GAMBIT_F32, rows row_stride values
  *             apart, aligned to their type
  *   u         device fp32 [n], in [0, 1)
  *   temperature, top_k, top_p, min_p  device [n] (fp32, int32, fp32, fp32); NULL:
  *             the call's *_all for every row
  *   ids_out   device int32 [n]
- *   vocab     at most 2^18 */
+ *   vocab     at most 2^18;  n at most 2^20
+ *   workspace device, 16-byte aligned, >= gambit_sample_workspace_size(n, vocab,
+ *             dtype) bytes (0 for short rows: NULL will do); its contents do
+ *             not matter, and calls that may overlap have one each */
+size_t gambit_sample_workspace_size(int32_t n, int32_t vocab, int32_t dtype);
 gambit_status gambit_sample(int32_t n, int32_t vocab, const void* logits, int32_t dtype, int64_t row_stride,
                             const float* u, const float* temperature, float temperature_all,
                             const int32_t* top_k, int32_t top_k_all, const float* top_p, float top_p_all,
-                            const float* min_p, float min_p_all, int32_t* ids_out, void* stream);
+                            const float* min_p, float min_p_all, int32_t* ids_out, void* workspace,
+                            size_t workspace_bytes, void* stream);
 
 /* Measurement, not a step of the method: the device's streaming-read rate,
  * the practical ceiling beside the published HBM peak for the attention

@@ -1,5 +1,5 @@
 // One token a row of logits from a given random number (gambit_sample),
-// kernel and host entry point.
+// kernels and host entry point.
 //
 //     w_i = 2^((z_i - max z) log2(e) / T)
 //     kept: the top_k largest (of equal ones the lower index); of those the
@@ -8,581 +8,679 @@
 //     token: the first kept one, by index, up to which the kept weights' sum
 //            exceeds u times their whole sum
 //
-// Weights are whole numbers, round(2^S w_i) with S = 62 - log2 of the row's
-// length (44 for the longest rows): sums are exact whatever their order, so a
-// row's token depends on its inputs alone, and the atomics below change
-// nothing.  w is computed in fp64 to 2^-50 (a table of 64 powers and a
-// polynomial of degree 5), because a token is one of many neighbours on the
-// line from 0 to 1, and an error of fp32's size there would give another one
-// in every few thousand draws.
+// Weights are whole numbers, in units of 2^-44 of the power of two at or above
+// the row's largest: sums are exact whatever their order, so a row's token
+// depends on its inputs alone, and the atomics below change nothing.  A weight
+// is computed in fp64 to 2^-44 (a table of 64 powers and a polynomial), because
+// a token is one of many neighbours on the line from 0 to 1, and an error of
+// fp32's size there would give another one in every few thousand draws.
 //
-// One workgroup a row goes over it as often as the filters ask: the maximum;
-// with a filter, a histogram of the weights by 64ths of an octave, sixteen
-// octaves at a time from the maximum down, and the row's whole weight; the
-// values of the bin where the filter's border falls, listed and sorted in LDS,
-// together with the kept weight of every 64 loads of the row; then the 64
-// loads that the token is among.
-#include <hip/hip_runtime.h>
-
-#include <cfloat>
-#include <cmath>
-#include <cstdint>
+// Four launches.  sample_chunks_kernel reads the rows once, in chunks: each
+// leaves the maximum of every segment of 64 loads, and, from its own maximum
+// down, a histogram by eighths of an octave - of counts for top_k, of weights
+// for top_p alone - or its whole weight.  sample_border_kernel, one workgroup a
+// row, adds the histograms up and finds the bin where the filter's border
+// falls.  sample_gather_kernel reads the segments again that reach the bin: the
+// weights above it are summed by segment, the bin's values listed (with both
+// filters all values down to top_k's bin).  sample_rows_kernel, one workgroup a
+// row, sorts the list, cuts it, and finds the segment and then the value that
+// the token is.  Rows that
+// this does not hold (more values than a list; a border below the histogram;
+// logits over the temperature beyond 2^10 octaves, where their product with
+// log2(e) / T keeps too few bits) it draws as short rows are, the way of
+// sampling_any.h.
+#include <algorithm>
 
 #include "../../include/gambit.h"
-#include "fp8_codes.h"
 #include "kernels.h"
+#include "sampling.h"
+#include "sampling_any.h"
 
 namespace gambit {
 namespace {
 
-constexpr int kMaxVocab = 1 << 18;
-constexpr int kThreads = 1024;
-constexpr int kBins = 1024, kBinsPerOctave = 64;  // a histogram's window: 16 octaves
-constexpr int kList = 4096;                       // listed values of one bin
-constexpr int kSegs = kMaxVocab / 4 / 64 + 1;     // 64 loads (a wave's) of 16 bytes each; rows may start inside one
+constexpr int kThreads = 512, kWaves = kThreads / 64;
+static_assert(kThreads == kAnyThreads, "one kernel holds both ways");
+constexpr int kOctaveBins = 8, kBins = 24 * kOctaveBins;  // a histogram's; smaller weights are not told apart
+constexpr int kNoBin = 1 << 20;                           // below every value's
+constexpr int kList = 8192;
+constexpr int kMaxChunks = (kMaxVocab / 4 + 1 + kThreads - 1) / kThreads;
+constexpr double kMostOctaves = 1024.;
+constexpr int kShortLoads = 2048;  // rows of no more are drawn by sample_any_kernel
 
-struct SampleArgs {
-  const void* z;
-  int64_t stride;  // values between rows
-  int32_t vocab;
-  int32_t scale_bits;  // S
-  const float* u;
-  const float* temperature;  // [n], or null: t_all for every row; the others alike
-  const int32_t* top_k;
-  const float* top_p;
-  const float* min_p;
-  float t_all, p_all, m_all;
-  int32_t k_all;
-  int32_t* out;
+// Where a row's border falls.
+struct Border {
+  float top;         // the row's maximum
+  int32_t bin;       // -1: nowhere in the histogram, or the row is out of range
+  float from;        // the least value of bins up to `bin`, or a little less
+  uint32_t listed;   // values in the list (beyond kList: not all are there)
+  u64 above, total;  // top_k: values above the bin; top_p: their weight, and that of all
 };
 
-__device__ inline uint32_t key_of(float z) {  // ordered as the values are
-  const uint32_t b = __float_as_uint(z);
-  return b & 0x80000000u ? ~b : b | 0x80000000u;
+// What a call's kernels leave for the next, for each row.
+struct Left {
+  int32_t chunks, segs, chunk_segs;
+  float* most;      // [n][chunks] maximum
+  u64* weight;      // [n][chunks]
+  u64* bins;        // [n][chunks][kBins] counts or weights
+  float* seg_most;  // [n][segs]
+  u64* seg_sum;     // [n][segs]
+  Border* border;   // [n]
+  u64* list;        // [n][kList]
+};
+
+// Weights below the octave e that holds a maximum.
+struct Scale {
+  double slope;  // log2(e) / temperature
+  int e64;       // 64 e
+  float floor;   // 60 octaves below e: smaller values count as it (a weight of zero)
+  __device__ Scale(double slope_, float most) : slope(slope_) {
+    const double e = fmin(fmax(ceil((double)most * slope), -0x1p20), 0x1p20);
+    e64 = 64 * (int)e;
+    floor = fmaxf((float)((e - 60.) / slope), -FLT_MAX);
+  }
+  // 64 log2 of a weight, rounded (<= 0), and what the rounding left of log2
+  __device__ int at(float z, double* r) const {
+    const double x = (double)fmaxf(z, floor), y = fma(x, slope, kTo64ths);
+    *r = fma(x, slope, kTo64ths - y);
+    return (int)__double_as_longlong(y) - e64;
+  }
+  __device__ int at(float z) const { return (int)__double_as_longlong(fma((double)fmaxf(z, floor), slope, kTo64ths)) - e64; }
+};
+__device__ inline int bin_of(int q) { return -q >> 3; }
+static_assert(kOctaveBins == 8, "64ths of an octave to bins");
+
+
+// How a row is drawn.
+enum Way { kGreedy, kAll, kMinP, kTopK, kTopP, kBoth };
+__device__ inline Way way_of(const Filter& F) {
+  if (F.greedy) return kGreedy;
+  if (F.use_k) return F.use_p ? kBoth : kTopK;
+  return F.use_p ? kTopP : F.min_p > 0.f ? kMinP : kAll;
 }
-__device__ inline float value_of(uint32_t key) {
-  return __uint_as_float(key & 0x80000000u ? key & 0x7fffffffu : ~key);
+__device__ inline bool in_range(float most, double slope) {
+  return fabs((double)most * slope) <= kMostOctaves && slope > 1e-30;
+}
+__device__ inline u64 entry_of(float z, int index) { return (u64)~key_of(z) << 32 | (uint32_t)index; }
+__device__ inline float entry_value(u64 entry) { return value_of(~(uint32_t)(entry >> 32)); }
+__device__ inline u64 weight_at(float z, const Scale& S, const double* powers) {
+  double r;
+  const int q = S.at(z, &r);
+  return weight_of(q, r, powers);
 }
 
-template <bool kF32>
-struct Row {
-  static constexpr int kPer = kF32 ? 4 : 8;  // values of a 16-byte load
-  const uint8_t* base;                       // of load 0, 16-byte aligned: `lead` values before the row
-  int lead, vocab, loads;
-
-  __device__ Row(const void* z, int64_t at, int vocab_) : vocab(vocab_) {
-    const uint8_t* p = static_cast<const uint8_t*>(z) + at * (kF32 ? 4 : 2);
-    lead = (int)(reinterpret_cast<uintptr_t>(p) & 15) / (kF32 ? 4 : 2);
-    base = p - (reinterpret_cast<uintptr_t>(p) & 15);
-    loads = (lead + vocab + kPer - 1) / kPer;
-  }
-  // NaN counts as -inf, +inf as the largest finite value, -0 as 0.
-  __device__ static float clean(float x) { return x == x ? fminf(x, FLT_MAX) + 0.f : -INFINITY; }
-  __device__ int index(int load, int i) const { return load * kPer + i - lead; }
-  // The values of a load; places outside the row are not read and count as -inf.
-  __device__ void get(int load, float* z) const {
-    const uint8_t* p = base + (size_t)load * 16;
-    const int first = index(load, 0);
-    if (first >= 0 && first + kPer <= vocab) {
-      const uint4 a = *reinterpret_cast<const uint4*>(p);
-      const uint32_t w[4] = {a.x, a.y, a.z, a.w};
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        if constexpr (kF32) {
-          z[i] = clean(__uint_as_float(w[i]));
-        } else {
-          z[2 * i] = clean(bf16_lo(w[i]));
-          z[2 * i + 1] = clean(bf16_hi(w[i]));
-        }
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < kPer; ++i) {
-        z[i] = -INFINITY;
-        if (first + i < 0 || first + i >= vocab) continue;
-        if constexpr (kF32)
-          z[i] = clean(reinterpret_cast<const float*>(p)[i]);
-        else
-          z[i] = clean(__uint_as_float((uint32_t)reinterpret_cast<const uint16_t*>(p)[i] << 16));
-      }
-    }
-  }
-};
-
-struct Shared {
-  unsigned long long mass[kBins];
-  uint32_t count[kBins];
-  unsigned long long list[kList];  // ~key, index: ascending is likeliest first
-  unsigned long long segs[kSegs + 1];
-  double power[64];
-  unsigned long long wave_sum[kThreads / 64];
-  unsigned long long found_mass, rest;
-  uint32_t wave_max[kThreads / 64];
-  uint32_t found, found_count, listed, key_lo, key_hi, token;
-};
-
-// What the kept values have at least: a key, and of equal ones an index at most.
-struct Cut {
-  uint32_t key, index;
-};
-
-template <bool kF32>
-struct Sampler {
-  Shared& L;
-  const Row<kF32> row;
-  static constexpr int kPer = Row<kF32>::kPer;
-  const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
-  float top = 0.f;         // the row's maximum
-  double slope = 0.;       // log2(e) / T
-  float bin_slope = 0.f;
-  double least = -INFINITY;  // log2 of min_p
-  int bits;                // S
-  unsigned long long total = 0;  // weight of all values
-  int window = -1;         // the histogram's
-
-  // log2 of a weight
-  __device__ double octaves(float z) const { return ((double)z - (double)top) * slope; }
-  // round(2^S w); 0 below half a unit (NaN: of -inf at an infinite temperature)
-  __device__ unsigned long long weight(double x) const {
-    if (!(x >= -(double)(bits + 1))) return 0;
-    constexpr double kShift = 0x1.8p46;  // its last bit is 1/64
-    const double y = x + kShift, r = x - (y - kShift);
-    const int q = (int)__double_as_longlong(y);
-    double p = fma(r, 1.3333558146428443e-3, 9.6181291076284772e-3);  // ln(2)^n / n!
-    p = fma(r, p, 5.5504108664821580e-2);
-    p = fma(r, p, 2.4022650695910071e-1);
-    p = fma(r, p, 6.9314718055994531e-1);
-    p = fma(r, p, 1.0);
-    p = ldexp(p * L.power[q & 63], (q >> 6) + bits) + 0x1p52;
-    return (unsigned long long)__double_as_longlong(p) - 0x4330000000000000ull;
-  }
-  // Bin of a value, from the maximum down; a huge one for -inf.
-  __device__ int bin(float z) const {
-    return z > -INFINITY ? (int)fminf(fminf(top - z, FLT_MAX) * bin_slope, 0x1p30f) : 0x7fffffff;
-  }
-  __device__ bool in(const Cut& c, float z, int index) const {
-    const uint32_t k = key_of(z);
-    return k > c.key || (k == c.key && (uint32_t)index <= c.index);
-  }
-
-  // f(load, values) for every load of the row; a wave's are its segment's.
+// A thread's loads of its chunk: load i of wave w is segment 8 i + w of the chunk.
+template <bool kF32, int kLoads>
+struct Chunk {
+  typedef Row<kF32> R;
+  const R row;
+  const int j0;
+  float z[kLoads][R::kPer];
+  __device__ Chunk(const SampleArgs& A, int r, int c)
+      : row(A.z, r * A.stride, A.vocab), j0(c * kThreads * kLoads + threadIdx.x) {}
+  __device__ int load(int i) const { return j0 + i * kThreads; }
+  __device__ int seg(int i) const { return load(i) >> 6; }
   template <class F>
-  __device__ void each(F&& f) {
-    for (int j = t; j < (row.loads + 63) / 64 * 64; j += kThreads) {
-      float z[kPer];
-      if (j < row.loads) {
-        row.get(j, z);
-      } else {
+  __device__ void read(F&& wanted) {  // all of a wave's lanes want a load, or none
+    uint4 a[kLoads];
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) z[i] = -INFINITY;
+    for (int i = 0; i < kLoads; ++i)
+      if (wanted(i) && row.whole(load(i))) a[i] = row.raw(load(i));
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      if (!wanted(i)) continue;
+      if (row.whole(load(i)))
+        R::unpack(a[i], z[i]);
+      else
+        row.edge(load(i), z[i]);
+    }
+  }
+};
+
+struct ChunkShared {
+  u64 bins[kBins];
+  u64 sums[kWaves];
+  double powers[64];
+  float most[kWaves];
+};
+
+template <bool kF32, int kLoads>
+__global__ __launch_bounds__(kThreads) void sample_chunks_kernel(SampleArgs A, Left W) {
+  __shared__ ChunkShared L;
+  typedef Row<kF32> R;
+  const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+  const int r = blockIdx.x / W.chunks, c = blockIdx.x % W.chunks;
+  Chunk<kF32, kLoads> C(A, r, c);
+  C.read([](int) { return true; });
+  if (t < 64) L.powers[t] = exp2(t / 64.);
+  if (t < kBins) L.bins[t] = 0;
+  float most = -INFINITY;
+#pragma unroll
+  for (int i = 0; i < kLoads; ++i) {
+    float m = C.z[i][0];
+#pragma unroll
+    for (int e = 1; e < R::kPer; ++e) m = fmaxf(m, C.z[i][e]);
+    m = wave_max(m);
+    if (lane == 0 && C.seg(i) < W.segs) W.seg_most[(size_t)r * W.segs + C.seg(i)] = m;
+    most = fmaxf(most, m);
+  }
+  if (lane == 0) L.most[wave] = most;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) most = fmaxf(most, L.most[w]);
+  const size_t at = (size_t)r * W.chunks + c;
+  if (t == 0) W.most[at] = most;
+  const Filter F(A, r);
+  const Way way = way_of(F);
+  if (most == -INFINITY || way == kGreedy || way == kMinP) return;
+  const Scale S(F.slope, most);
+  u64 sum = 0;
+  if (way == kAll || way == kTopP) {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i)
+#pragma unroll
+      for (int k = 0; k < R::kPer; ++k) {
+        double rest;
+        const int q = S.at(C.z[i][k], &rest);
+        const u64 w = weight_of(q, rest, L.powers);
+        sum += w;
+        const uint32_t b = bin_of(q);
+        if (way == kTopP && b < (uint32_t)kBins) atomicAdd(&L.bins[b], w);
       }
-      f(j, z);
-    }
-  }
-
-  __device__ static unsigned long long wave_total(unsigned long long x) {
+    sum = wave_total(sum);
+    if (lane == 0) L.sums[wave] = sum;
+  } else {
 #pragma unroll
-    for (int o = 32; o; o >>= 1) x += __shfl_xor(x, o);
-    return x;
-  }
-  // Sum of x over the threads before this one; *all: over all of them.
-  __device__ unsigned long long scan(unsigned long long x, unsigned long long* all) {
-    unsigned long long y = x;
+    for (int i = 0; i < kLoads; ++i)
 #pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const unsigned long long z = __shfl_up(y, o);
-      if (lane >= o) y += z;
-    }
-    __syncthreads();  // an earlier scan has been read
-    if (lane == 63) L.wave_sum[wave] = y;
-    __syncthreads();
-    unsigned long long before = 0, sum = 0;
-#pragma unroll
-    for (int w = 0; w < kThreads / 64; ++w) {
-      const unsigned long long z = L.wave_sum[w];
-      if (w < wave) before += z;
-      sum += z;
-    }
-    *all = sum;
-    return before + y - x;
-  }
-
-  __device__ void clear_bins() {
-    __syncthreads();
-    L.mass[t] = 0;
-    L.count[t] = 0;
-    __syncthreads();
-  }
-  // The histogram's bin that takes the running count (or mass) from `above` to
-  // `want` or more; false if none does.  *above then stands before that bin.
-  __device__ bool crossing(bool by_mass, unsigned long long want, unsigned long long* above_count,
-                           unsigned long long* above_mass, uint32_t* at, uint32_t* here) {
-    static_assert(kBins == kThreads, "a bin a thread");
-    const unsigned long long c = L.count[t], m = L.mass[t];
-    unsigned long long all_c, all_m;
-    const unsigned long long bc = *above_count + scan(c, &all_c), bm = *above_mass + scan(m, &all_m);
-    if (t == 0) L.found = ~0u;
-    __syncthreads();
-    if (by_mass ? bm < want && bm + m >= want : bc < want && bc + c >= want) {
-      L.found = t;
-      L.found_count = (uint32_t)bc;
-      L.found_mass = bm;
-    }
-    __syncthreads();
-    if (L.found == ~0u) {
-      *above_count += all_c;
-      *above_mass += all_m;
-      return false;
-    }
-    *at = L.found;
-    *here = L.count[*at];
-    *above_count = L.found_count;
-    *above_mass = L.found_mass;
-    return true;
-  }
-
-  // The histogram of one window; the first time also the weight of all values.
-  __device__ void histogram(int w, bool masses) {
-    clear_bins();
-    unsigned long long sum = 0;
-    each([&](int, const float* z) {
-#pragma unroll
-      for (int i = 0; i < kPer; ++i) {
-        const int b = bin(z[i]) - w * kBins;
-        const unsigned long long m = masses ? weight(octaves(z[i])) : 0;
-        sum += m;
-        if (b >= 0 && b < kBins) {
-          atomicAdd(&L.count[b], 1u);
-          if (masses) atomicAdd(&L.mass[b], m);
-        }
+      for (int k = 0; k < R::kPer; ++k) {
+        const uint32_t b = bin_of(S.at(C.z[i][k]));
+        if (b < (uint32_t)kBins) atomicAdd(&L.bins[b], 1ull);
       }
-    });
-    if (masses) {
-      unsigned long long all;
-      scan(sum, &all);
-      total = all;
-    }
-    window = w;
-    __syncthreads();
   }
+  __syncthreads();
+  if (t == 0 && (way == kAll || way == kTopP)) {
+    sum = 0;
+    for (int w = 0; w < kWaves; ++w) sum += L.sums[w];
+    W.weight[at] = sum;
+  }
+  if (way != kAll && t < kBins) W.bins[at * kBins + t] = L.bins[t];
+}
 
-  __device__ void append(uint32_t key, int index) {
-    const uint32_t at = atomicAdd(&L.listed, 1u);
-    if (at < (uint32_t)kList) L.list[at] = (unsigned long long)~key << 32 | (uint32_t)index;
+constexpr int kBorderThreads = 256;
+static_assert(kBins <= kBorderThreads && kMaxChunks <= kBorderThreads, "a thread each");
+
+__global__ __launch_bounds__(kBorderThreads) void sample_border_kernel(SampleArgs A, Left W) {
+  __shared__ u64 sums[kBorderThreads / 64];
+  __shared__ float most[kBorderThreads / 64];
+  __shared__ int32_t below[kMaxChunks];  // octaves of a chunk below the row's; 64: nothing there counts
+  const int t = threadIdx.x, lane = t & 63, wave = t >> 6, r = blockIdx.x;
+  const size_t first = (size_t)r * W.chunks;
+  const float mine = t < W.chunks ? W.most[first + t] : -INFINITY;
+  const Filter F(A, r);
+  const Way way = way_of(F);
+  const u64 weight = t < W.chunks && way == kTopP ? W.weight[first + t] : 0;
+  float top = wave_max(mine);
+  if (lane == 0) most[wave] = top;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kBorderThreads / 64; ++w) top = fmaxf(top, most[w]);
+  Border B{top, kNoBin, -FLT_MAX, 0, 0, 0};
+  const bool drawn = top > -INFINITY && way != kGreedy;
+  if (drawn && !in_range(top, F.slope)) B.bin = -1;
+  if (!drawn || B.bin < 0 || way == kAll || way == kMinP) {
+    if (t == 0) W.border[r] = B;
+    return;
   }
-  // Ascending sort of the list, padded to a power of two.
-  __device__ void sort(int n) {
-    int m = 64;
-    while (m < n) m <<= 1;
-    for (int i = n + t; i < m; i += kThreads) L.list[i] = ~0ull;
-    for (int k = 2; k <= m; k <<= 1)
-      for (int j = k >> 1; j; j >>= 1) {
-        __syncthreads();
-        for (int i = t; i < m / 2; i += kThreads) {
-          const int a = 2 * i - (i & (j - 1)), b = a + j;
-          const unsigned long long x = L.list[a], y = L.list[b];
-          if ((x > y) == ((a & k) == 0)) {
-            L.list[a] = y;
-            L.list[b] = x;
-          }
-        }
+  const Scale S(F.slope, top);
+  const int sh = mine == -INFINITY ? 64 : min(64, (S.e64 - Scale(F.slope, mine).e64) / 64);
+  if (t < W.chunks) below[t] = sh;
+  // (the scan's barriers also stand behind `below`)
+  block_before<kBorderThreads>(way == kTopP && t < W.chunks && sh < 64 ? weight >> sh : 0, sums, &B.total);
+  u64 x = 0, all;
+  if (t < kBins) {
+    constexpr int kAhead = 16;
+    for (int c0 = 0; c0 < W.chunks; c0 += kAhead) {
+      u64 y[kAhead];
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) {
+        const int c = min(c0 + i, W.chunks - 1), from = t - kOctaveBins * below[c];
+        y[i] = c0 + i < W.chunks && from >= 0 ? W.bins[(first + c) * kBins + from] : 0;
       }
-    __syncthreads();
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) x += way == kTopP ? y[i] >> min(63, below[min(c0 + i, W.chunks - 1)]) : y[i];
+    }
   }
+  const u64 want = way == kTopP ? max((u64)ceil((double)F.p * (double)B.total), (u64)1) : (u64)F.k;
+  const u64 before = block_before<kBorderThreads>(x, sums, &all);
+  if (all < want) {
+    B.bin = -1;
+    if (t == 0) W.border[r] = B;
+  } else if (before < want && before + x >= want) {
+    B.bin = t;
+    B.above = before;
+    const float low = (float)(((double)S.e64 - 8. * (t + 1) - 1.) / 64. / F.slope);
+    B.from = low - fabsf(low) * 0x1p-20f;
+    W.border[r] = B;
+  }
+}
 
-  // The cut after the listed values that take the running count or mass from
-  // `above` to `want`; *mass: of all values in the cut.
-  __device__ Cut cut_list(int n, bool by_mass, unsigned long long want, unsigned long long above_count,
-                          unsigned long long above_mass, unsigned long long* mass) {
-    sort(n);
+template <bool kF32, int kLoads>
+__global__ __launch_bounds__(kThreads) void sample_gather_kernel(SampleArgs A, Left W) {
+  __shared__ double powers[64];
+  __shared__ float seg_most[8 * kLoads];
+  __shared__ uint32_t listed[kWaves], base;
+  typedef Row<kF32> R;
+  const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+  const int r = blockIdx.x / W.chunks, c = blockIdx.x % W.chunks;
+  Chunk<kF32, kLoads> C(A, r, c);
+  const Border B = W.border[r];
+  const Filter F(A, r);
+  const Way way = way_of(F);
+  if (way == kGreedy || way == kAll || B.bin < 0 || B.top == -INFINITY) return;
+  if (t < 8 * kLoads && c * 8 * kLoads + t < W.segs) seg_most[t] = W.seg_most[(size_t)r * W.segs + c * 8 * kLoads + t];
+  if (t < 64) powers[t] = exp2(t / 64.);
+  __syncthreads();
+  const Scale S(F.slope, B.top);
+  const double least = F.least();
+  auto likely = [&](float z) { return ((double)z - (double)B.top) * F.slope >= least; };
+  const int b = B.bin;
+  const float from = B.from;
+  auto wanted = [&](int i) {
+    const float m = C.seg(i) < W.segs ? seg_most[8 * i + wave] : -INFINITY;
+    return m >= from && (b < kNoBin || likely(m));
+  };
+  C.read(wanted);
+  u64 flags = 0;  // of the thread's values: listed
+#pragma unroll
+  for (int i = 0; i < kLoads; ++i) {
+    if (C.seg(i) >= W.segs) continue;
+    u64 sum = 0;
+    if (wanted(i)) {
+#pragma unroll
+      for (int k = 0; k < R::kPer; ++k) {
+        const float z = C.z[i][k];
+        if (!(z >= from)) continue;
+        double rest;
+        const int q = S.at(z, &rest), at = bin_of(q);
+        if (at > b) continue;
+        if (at == b || way == kBoth)
+          flags |= 1ull << (i * R::kPer + k);
+        else if (likely(z))
+          sum += weight_of(q, rest, powers);
+      }
+      sum = wave_total(sum);
+    }
+    if (lane == 0) W.seg_sum[(size_t)r * W.segs + C.seg(i)] = sum;
+  }
+  if (b == kNoBin) return;
+  // the values' places in the row's list: one claim a workgroup
+  uint32_t n = __popcll(flags), at = (uint32_t)wave_before(n, lane);
+  if (lane == 63) listed[wave] = at + n;
+  __syncthreads();
+  if (t == 0) {
+    uint32_t all = 0;
+    for (int w = 0; w < kWaves; ++w) {
+      const uint32_t x = listed[w];
+      listed[w] = all;
+      all += x;
+    }
+    base = all ? atomicAdd(&W.border[r].listed, all) : 0;
+  }
+  __syncthreads();
+  at += base + listed[wave];
+#pragma unroll
+  for (int i = 0; i < kLoads; ++i)
+#pragma unroll
+    for (int k = 0; k < R::kPer; ++k)
+      if (flags >> (i * R::kPer + k) & 1) {
+        if (at < (uint32_t)kList) W.list[(size_t)r * kList + at] = entry_of(C.z[i][k], C.row.index(C.load(i), k));
+        ++at;
+      }
+}
+
+struct RowShared {
+  u64 list[kList];  // ~key, index: ascending is likeliest first
+  u64 segs[kSegs + 1];
+  double powers[64];
+  u64 sums[kWaves];
+  u64 rest;
+  uint32_t found, token;
+};
+#define L lds_as<RowShared>()
+
+// Ascending sort of the list: by counting the smaller ones, a few of which
+// every thread reads at once, or in many steps.
+__device__ __forceinline__ void sort_list(int n) {
+  constexpr int kEach = 2, kAhead = 8;
+  if (n > kEach * kThreads) return block_sort<kThreads>(L.list, n);
+  const int m = (n + kAhead - 1) / kAhead * kAhead;
+  if (n + (int)threadIdx.x < m) L.list[n + threadIdx.x] = ~0ull;
+  __syncthreads();
+  u64 x[kEach];
+  int rank[kEach] = {};
+#pragma unroll
+  for (int e = 0; e < kEach; ++e) x[e] = L.list[min((int)threadIdx.x + e * kThreads, n - 1)];
+  for (int i = 0; i < m; i += kAhead)
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      const u64 y = L.list[i + j];
+#pragma unroll
+      for (int e = 0; e < kEach; ++e) rank[e] += y < x[e];
+    }
+  __syncthreads();
+#pragma unroll
+  for (int e = 0; e < kEach; ++e)
+    if ((int)threadIdx.x + e * kThreads < n) L.list[rank[e]] = x[e];
+  __syncthreads();
+}
+
+template <bool kF32>
+struct RowDraw {
+  typedef Row<kF32> R;
+  static constexpr int kPer = R::kPer, kSegsEach = (kSegs + kThreads - 1) / kThreads;
+  const R row;
+  const Scale S;
+  const float top;
+  const double least;  // log2 of what a kept weight has at least
+  const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+
+  __device__ u64 scan(u64 x, u64* all) const { return block_before<kThreads>(x, L.sums, all); }
+  __device__ u64 weight(float z) const { return weight_at(z, S, L.powers); }
+  __device__ bool likely(float z) const { return ((double)z - (double)top) * S.slope >= least; }
+
+  // The cut in the sorted list: by count its value k - above; by mass the one that
+  // takes the weight from `above` to `want`; with both, the weight of the first k
+  // is what p is a share of.
+  __device__ __forceinline__ Cut cut_list(int n, const Filter& F, Way way, u64 above, u64 total) {
     constexpr int kEach = kList / kThreads;
-    unsigned long long m[kEach], sum = 0, all;
-#pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-      const int a = t * kEach + i;
-      m[i] = a < n ? weight(octaves(value_of(~(uint32_t)(L.list[a] >> 32)))) : 0;
-      sum += m[i];
+    const int each = (n + kThreads - 1) / kThreads;
+    if (way == kTopK) {
+      const u64 x = L.list[min((int)(F.k - above), n) - 1];
+      return {~(uint32_t)(x >> 32), (uint32_t)x};
     }
-    unsigned long long before = above_mass + scan(sum, &all);
+    u64 w[kEach], sum = 0, all;
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
-      const int a = t * kEach + i;
-      if (a < n && (by_mass ? before < want && before + m[i] >= want : above_count + a + 1 == want)) {
-        L.found = a;
-        L.found_mass = before + m[i];
+      w[i] = 0;
+      if (i >= each) continue;  // uniform
+      const int a = t * each + i;
+      if (a < n) w[i] = weight(entry_value(L.list[a]));
+      sum += w[i];
+    }
+    const u64 first = (way == kBoth ? 0 : above) + scan(sum, &all);
+    int last = n - 1;
+    if (way == kBoth) {
+      last = min(F.k, n) - 1;
+      u64 before = first;
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) {
+        if (i >= each) continue;
+        before += w[i];
+        if (t * each + i == last) L.rest = before;
       }
-      before += m[i];
+      __syncthreads();
+      total = L.rest;
+    }
+    const u64 want = max((u64)ceil((double)F.p * (double)total), (u64)1);
+    if (t == 0) L.found = last;  // (a bin's weight, shifted as a whole, may be a few units off its values')
+    __syncthreads();
+    u64 before = first;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      if (i >= each) continue;
+      const int a = t * each + i;
+      if (a < last && (before < want || a == 0) && before + w[i] >= want) L.found = a;
+      before += w[i];
     }
     __syncthreads();
-    const unsigned long long x = L.list[L.found];
-    *mass = L.found_mass;
+    const u64 x = L.list[L.found];
     return {~(uint32_t)(x >> 32), (uint32_t)x};
   }
 
-  // Too many values in a bin for the list: the bin's range of keys is cut
-  // finer, down to a list, or to equal values, of which the first by index count.
-  __device__ Cut cut_finer(int b, bool by_mass, bool masses, unsigned long long want, unsigned long long above_count,
-                           unsigned long long above_mass, unsigned long long* mass) {
-    if (t == 0) {
-      L.key_lo = ~0u;
-      L.key_hi = 0;
+  // The token: the first that `cut` keeps up to which the segments' sum exceeds
+  // `target`, or u times their sum where that is not known.  -2: they hold nothing.
+  __device__ __forceinline__ int pick(u64 target, double u, const Cut& cut) {
+    u64 w[kSegsEach], x = 0, all;
+#pragma unroll
+    for (int i = 0; i < kSegsEach; ++i) {
+      w[i] = t * kSegsEach + i < kSegs ? L.segs[t * kSegsEach + i] : 0;
+      x += w[i];
     }
-    __syncthreads();
-    uint32_t lo = ~0u, hi = 0;
-    each([&](int, const float* z) {
+    u64 before = scan(x, &all);
+    if (all == 0) return -2;
+    if (target == ~0ull) target = (u64)fmin(u * (double)all, 0x1p63);
+    target = target < all ? target : all - 1;  // (u of 1; and shifted sums may be a few units off)
 #pragma unroll
-      for (int i = 0; i < kPer; ++i)
-        if (bin(z[i]) == b) {
-          lo = min(lo, key_of(z[i]));
-          hi = max(hi, key_of(z[i]));
-        }
-    });
-    atomicMin(&L.key_lo, lo);
-    atomicMax(&L.key_hi, hi);
-    __syncthreads();
-    lo = L.key_lo;
-    hi = L.key_hi;
-    uint32_t here = ~0u;
-    while (here > (uint32_t)kList && lo < hi) {
-      int shift = 0;
-      while ((hi - lo) >> shift >= (uint32_t)kBins) ++shift;
-      clear_bins();
-      each([&](int, const float* z) {
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-          const uint32_t k = key_of(z[i]);
-          if (k < lo || k > hi) continue;
-          atomicAdd(&L.count[(hi - k) >> shift], 1u);
-          if (masses) atomicAdd(&L.mass[(hi - k) >> shift], weight(octaves(z[i])));
-        }
-      });
-      __syncthreads();
-      uint32_t at;
-      if (!crossing(by_mass, want, &above_count, &above_mass, &at, &here)) break;  // never: the bin's sums are these
-      hi -= at << shift;
-      const uint32_t width = (1u << shift) - 1;
-      lo = hi - lo > width ? hi - width : lo;
-    }
-    window = -1;
-    if (here <= (uint32_t)kList) {
-      if (t == 0) L.listed = 0;
-      __syncthreads();
-      each([&](int j, const float* z) {
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-          const uint32_t k = key_of(z[i]);
-          if (k >= lo && k <= hi) append(k, row.index(j, i));
-        }
-      });
-      __syncthreads();
-      return cut_list((int)here, by_mass, want, above_count, above_mass, mass);
-    }
-    // equal values: `need` of them, the first by index
-    const unsigned long long w = weight(octaves(value_of(lo)));
-    const unsigned long long need = by_mass ? (want - above_mass + w - 1) / (w ? w : 1) : want - above_count;
-    *mass = above_mass + need * w;
-    seg_sums([&](float z, int) { return key_of(z) == lo; }, [](float) { return 1ull; });
-    const uint32_t index = pick(need - 1, [&](float z, int) { return key_of(z) == lo; }, [](float) { return 1ull; });
-    return {lo, index};
-  }
-
-  // segs[s] = sum of g over the values of segment s that f keeps
-  template <class F, class G>
-  __device__ void seg_sums(F&& f, G&& g) {
-    __syncthreads();
-    each([&](int j, const float* z) {
-      unsigned long long sum = 0;
-#pragma unroll
-      for (int i = 0; i < kPer; ++i)
-        if (f(z[i], row.index(j, i))) sum += g(z[i]);
-      if (__any(sum != 0)) sum = wave_total(sum);
-      if (lane == 0) L.segs[j >> 6] = sum;
-    });
-    __syncthreads();
-  }
-
-  // The index, among what f keeps, of the first value up to which the sum of g exceeds `target` (segs hold the sums).
-  template <class F, class G>
-  __device__ uint32_t pick(unsigned long long target, F&& f, G&& g) {
-    const int n = (row.loads + 63) / 64;
-    static_assert(kSegs + 1 <= 2 * kThreads, "two segments a thread");
-    const unsigned long long a = 2 * t < n ? L.segs[2 * t] : 0, b = 2 * t + 1 < n ? L.segs[2 * t + 1] : 0;
-    unsigned long long all;
-    const unsigned long long before = scan(a + b, &all);
-    if (before <= target && target < before + a + b) {
-      const bool second = target >= before + a;
-      L.found = 2 * t + second;
-      L.rest = target - before - (second ? a : 0);
+    for (int i = 0; i < kSegsEach; ++i) {
+      if (before <= target && target < before + w[i]) {
+        L.found = t * kSegsEach + i;
+        L.rest = target - before;
+      }
+      before += w[i];
     }
     __syncthreads();
     if (wave == 0) {
       const int j = (int)L.found * 64 + lane;
-      const unsigned long long rest = L.rest;
       float z[kPer];
-      unsigned long long m[kPer], sum = 0;
-      if (j < row.loads) row.get(j, z);
+      u64 v[kPer], sum = 0;
+      row.get(j, z);
 #pragma unroll
       for (int i = 0; i < kPer; ++i) {
-        m[i] = j < row.loads && f(z[i], row.index(j, i)) ? g(z[i]) : 0;
-        sum += m[i];
+        v[i] = z[i] > -INFINITY && cut.holds(z[i], row.index(j, i)) && likely(z[i]) ? weight(z[i]) : 0;
+        sum += v[i];
       }
-      unsigned long long y = sum;
-#pragma unroll
-      for (int o = 1; o < 64; o <<= 1) {
-        const unsigned long long x = __shfl_up(y, o);
-        if (lane >= o) y += x;
-      }
-      y -= sum;
+      u64 y = wave_before(sum, lane);
+      const u64 rest = L.rest;
 #pragma unroll
       for (int i = 0; i < kPer; ++i) {
-        if (y <= rest && rest < y + m[i]) L.token = row.index(j, i);
-        y += m[i];
+        if (y <= rest && rest < y + v[i]) L.token = row.index(j, i);
+        y += v[i];
       }
     }
     __syncthreads();
-    return L.token;
+    return (int)L.token;
   }
 
-  __device__ int run(const SampleArgs& A, int r) {
-    const float T = A.temperature ? A.temperature[r] : A.t_all, p = A.top_p ? A.top_p[r] : A.p_all;
-    const float mp = A.min_p ? A.min_p[r] : A.m_all;
-    const int k = A.top_k ? A.top_k[r] : A.k_all;
-    if (t < 64) L.power[t] = exp2(t / 64.);
-    uint32_t best = 0;
-    each([&](int, const float* z) {
-#pragma unroll
-      for (int i = 0; i < kPer; ++i) best = max(best, key_of(z[i]));
-    });
-#pragma unroll
-    for (int o = 32; o; o >>= 1) best = max(best, (uint32_t)__shfl_xor((int)best, o));
-    if (lane == 0) L.wave_max[wave] = best;
-    if (t == 0) L.token = ~0u;
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < kThreads / 64; ++w) best = max(best, L.wave_max[w]);
-    top = value_of(best);
-    if (top == -INFINITY) return -1;
-    const bool use_k = k > 0 && k < row.vocab, use_p = p < 1.f;
-    if (!(T > 0.f) || k == 1 || (use_p && p <= 0.f)) {
-      uint32_t first = ~0u;
-      each([&](int j, const float* z) {
-#pragma unroll
-        for (int i = 0; i < kPer; ++i)
-          if (z[i] == top) first = min(first, (uint32_t)row.index(j, i));
-      });
-      if (first != ~0u) atomicMin(&L.token, first);
-      __syncthreads();
-      return (int)L.token;
-    }
-    slope = 1.4426950408889634 / (double)T;
-    bin_slope = fminf((float)(slope * kBinsPerOctave), FLT_MAX);
-    if (mp > 0.f) least = log2((double)fminf(mp, 1.f));
+  // The row's token; -2: to be drawn the other way.
+  __device__ __forceinline__ int run(const Filter& F, double u, const Left& W, const Border& B, int r) {
+    const Way way = way_of(F);
     Cut cut{0, ~0u};
-    bool summed = false;  // segs hold the kept weights
-    auto weigh = [&](float z) { return weight(octaves(z)); };
-    auto likely = [&](float z) { return octaves(z) >= least; };
-    for (int by_mass = use_k ? 0 : 1; by_mass <= (use_p ? 1 : 0); ++by_mass) {
-      const bool last = by_mass == (use_p ? 1 : 0);
-      unsigned long long want = k, above_count = 0, above_mass = 0, mass = 0;
-      uint32_t at = 0, here = 0;
-      if (by_mass) {
-        if (window != 0) histogram(0, true);
-        want = (unsigned long long)ceil((double)p * (double)total_kept(use_k));
-        want = want ? want : 1;
+    u64 target = ~0ull;
+    for (int s = t; s < kSegs + 1; s += kThreads)
+      L.segs[s] = s < W.segs && way != kAll && way != kBoth ? W.seg_sum[(size_t)r * W.segs + s] : 0;
+    if (way == kAll) {  // the chunk that the token is in, then its segments
+      u64 weight_c = 0, total;
+      if (t < W.chunks) {
+        const size_t at = (size_t)r * W.chunks + t;
+        const float most = W.most[at];
+        if (most > -INFINITY) weight_c = W.weight[at] >> min(63, (S.e64 - Scale(S.slope, most).e64) / 64);
       }
-      const int windows = ((bits + 1) * kBinsPerOctave + kBins - 1) / kBins;
-      bool found = false;
-      int w = 0;
-      for (; w < windows; ++w) {
-        if (window != w) histogram(w, use_p);
-        if ((found = crossing(by_mass, want, &above_count, &above_mass, &at, &here))) break;
+      const u64 before = scan(weight_c, &total);
+      if (total == 0) return -2;
+      target = (u64)fmin(u * (double)total, 0x1p63);
+      target = target < total ? target : total - 1;
+      if (before <= target && target < before + weight_c) {
+        L.found = t;
+        L.rest = target - before;
       }
-      if (!found) {  // the border lies among values of weight zero
-        kept_mass = total;
-        continue;
-      }
-      const int b = w * kBins + (int)at;
-      if (here <= (uint32_t)kList) {
-        if (t == 0) L.listed = 0;
-        __syncthreads();
-        each([&](int j, const float* z) {
-          unsigned long long sum = 0;
+      __syncthreads();
+      target = L.rest;
+      const int s0 = (int)L.found * W.chunk_segs, s1 = min(W.segs, s0 + W.chunk_segs);
+#pragma unroll 2
+      for (int s = s0 + wave; s < s1; s += kWaves) {
+        float z[kPer];
+        row.get(s * 64 + lane, z);
+        u64 sum = 0;
 #pragma unroll
-          for (int i = 0; i < kPer; ++i) {
-            const int zb = bin(z[i]);
-            if (zb == b)
-              append(key_of(z[i]), row.index(j, i));
-            else if (last && zb < b && likely(z[i]))
-              sum += weigh(z[i]);
-          }
-          if (last) {
-            if (__any(sum != 0)) sum = wave_total(sum);
-            if (lane == 0) L.segs[j >> 6] = sum;
-          }
-        });
-        __syncthreads();
-        cut = cut_list((int)here, by_mass, want, above_count, above_mass, &mass);
-        if (last) {
-          for (int i = t; i < (int)here; i += kThreads) {
-            const unsigned long long x = L.list[i];
-            const float z = value_of(~(uint32_t)(x >> 32));
-            const int load = ((int)(uint32_t)x + row.lead) / kPer;
-            if (in(cut, z, (int)(uint32_t)x) && likely(z)) atomicAdd(&L.segs[load >> 6], weigh(z));
-          }
-          summed = true;
-          __syncthreads();
-        }
-      } else {
-        cut = cut_finer(b, by_mass, use_p, want, above_count, above_mass, &mass);
+        for (int k = 0; k < kPer; ++k) sum += weight(z[k]);
+        sum = wave_total(sum);
+        if (lane == 0) L.segs[s] = sum;
       }
-      kept_mass = mass;
+    } else if (way != kMinP) {
+      if (B.listed > (uint32_t)kList) return -2;
+      const int n = (int)B.listed;
+      for (int i = t; i < n; i += kThreads) L.list[i] = W.list[(size_t)r * kList + i];
+      __syncthreads();
+      sort_list(n);
+      cut = cut_list(n, F, way, B.above, B.total);
+      for (int i = t; i < n; i += kThreads) {
+        const u64 x = L.list[i];
+        const float z = entry_value(x);
+        const int index = (int)(uint32_t)x;
+        if (cut.holds(z, index) && likely(z)) atomicAdd(&L.segs[((index + row.lead) / kPer) >> 6], weight(z));
+      }
     }
-    auto kept = [&](float z, int index) { return z > -INFINITY && in(cut, z, index) && likely(z); };
-    if (!summed) seg_sums(kept, weigh);
-    const int n = (row.loads + 63) / 64;
-    unsigned long long all;
-    scan((2 * t < n ? L.segs[2 * t] : 0) + (2 * t + 1 < n ? L.segs[2 * t + 1] : 0), &all);
-    const double u = fmax((double)A.u[r], 0.);
-    unsigned long long target = (unsigned long long)fmin(u * (double)all, 0x1p63);
-    target = target < all ? target : all - 1;
-    return (int)pick(target, kept, weigh);
+    __syncthreads();
+    return pick(target, u, cut);
   }
-
-  unsigned long long kept_mass = 0;  // of the values that top_k keeps
-  __device__ unsigned long long total_kept(bool use_k) const { return use_k ? kept_mass : total; }
 };
 
 template <bool kF32>
-__global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs A) {
-  __shared__ Shared lds;
+__global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleArgs A, Left W) {
+  typedef Row<kF32> R;
+  const int r = blockIdx.x, t = threadIdx.x, lane = t & 63;
+  const R row(A.z, r * A.stride, A.vocab);
+  const Filter F(A, r);
+  const Border B = W.border[r];
+  const float m = B.top;
+  if (t < 64) L.powers[t] = exp2(t / 64.);
+  if (t == 0) L.token = ~0u;
+  __syncthreads();
+  int token = -1;
+  if (m > -INFINITY && F.greedy) {  // the first segment of that maximum, the first value there
+    uint32_t s = ~0u;
+    for (int i = t; i < W.segs; i += kThreads)
+      if (W.seg_most[(size_t)r * W.segs + i] == m) s = min(s, (uint32_t)i);
+    if (s != ~0u) atomicMin(&L.token, s);
+    __syncthreads();
+    const int j = (int)L.token * 64 + lane;
+    float z[R::kPer];
+    row.get(j, z);
+    s = ~0u;
+#pragma unroll
+    for (int i = 0; i < R::kPer; ++i)
+      if (z[i] == m) s = min(s, (uint32_t)row.index(j, i));
+#pragma unroll
+    for (int o = 32; o; o >>= 1) s = min(s, (uint32_t)__shfl_xor((int)s, o));
+    token = (int)s;
+  } else if (m > -INFINITY) {
+    token = -2;
+    if (B.bin >= 0) {
+      RowDraw<kF32> d{row, Scale(F.slope, m), m, F.least()};
+      token = d.run(F, fmax((double)A.u[r], 0.), W, B, r);
+    }
+    if (token == -2) {
+      __syncthreads();
+      Sampler<kF32> s{row};
+      token = s.run(A, r);
+    }
+  }
+  if (t == 0) A.out[r] = token;
+}
+#undef L
+
+template <bool kF32>
+__global__ __launch_bounds__(kThreads) void sample_any_kernel(SampleArgs A) {
   const int r = blockIdx.x;
-  Sampler<kF32> s{lds, Row<kF32>(A.z, r * A.stride, A.vocab)};
-  s.bits = A.scale_bits;
+  Sampler<kF32> s{Row<kF32>(A.z, r * A.stride, A.vocab)};
   const int token = s.run(A, r);
   if (threadIdx.x == 0) A.out[r] = token;
 }
 
+// How a call's rows are cut, and what its workspace holds.
+struct Cuts {
+  int loads = 0;  // of a chunk's thread; 0: no chunks
+  int chunks = 0, segs = 0;
+  size_t weight, bins, seg_most, seg_sum, border, list, bytes = 0;
+  Cuts(int64_t n, int vocab, bool f32) {
+    const int per = f32 ? 4 : 8, most = (vocab + 2 * (per - 1)) / per;  // a row's loads, wherever it begins
+    if (most <= kShortLoads) return;
+    segs = (most + 63) / 64;
+    // the largest chunks of which there is one for every other compute unit
+    for (loads = 4; loads > 1 && n * ((most + kThreads * loads - 1) / (kThreads * loads)) < 128;) loads /= 2;
+    chunks = (most + kThreads * loads - 1) / (kThreads * loads);
+    auto take = [&](size_t size) {
+      const size_t o = bytes;
+      bytes = (o + size + 255) / 256 * 256;
+      return o;
+    };
+    const size_t parts = (size_t)n * chunks;
+    take(4 * parts);
+    weight = take(8 * parts);
+    bins = take(8 * parts * kBins);
+    seg_most = take(4 * (size_t)n * segs);
+    seg_sum = take(8 * (size_t)n * segs);
+    border = take(sizeof(Border) * (size_t)n);
+    list = take(8 * (size_t)n * kList);
+  }
+};
+
+template <bool kF32, int kLoads>
+hipError_t launch_chunks(const SampleArgs& A, const Left& W, int n, hipStream_t s) {
+  const dim3 grid((unsigned)n * W.chunks);
+  hipLaunchKernelGGL((sample_chunks_kernel<kF32, kLoads>), grid, dim3(kThreads), 0, s, A, W);
+  if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  hipLaunchKernelGGL(sample_border_kernel, dim3(n), dim3(kBorderThreads), 0, s, A, W);
+  if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  hipLaunchKernelGGL((sample_gather_kernel<kF32, kLoads>), grid, dim3(kThreads), 0, s, A, W);
+  if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  hipLaunchKernelGGL(sample_rows_kernel<kF32>, dim3(n), dim3(kThreads), 0, s, A, W);
+  return hipGetLastError();
+}
+
+template <bool kF32>
+hipError_t launch(const SampleArgs& A, const Cuts& C, uint8_t* ws, int n, hipStream_t s) {
+  if (!C.loads) {
+    hipLaunchKernelGGL(sample_any_kernel<kF32>, dim3(n), dim3(kThreads), 0, s, A);
+    return hipGetLastError();
+  }
+  const Left W{C.chunks, C.segs, C.loads * kWaves, reinterpret_cast<float*>(ws), reinterpret_cast<u64*>(ws + C.weight),
+               reinterpret_cast<u64*>(ws + C.bins), reinterpret_cast<float*>(ws + C.seg_most),
+               reinterpret_cast<u64*>(ws + C.seg_sum), reinterpret_cast<Border*>(ws + C.border),
+               reinterpret_cast<u64*>(ws + C.list)};
+  switch (C.loads) {
+    case 8: return launch_chunks<kF32, 8>(A, W, n, s);
+    case 4: return launch_chunks<kF32, 4>(A, W, n, s);
+    case 2: return launch_chunks<kF32, 2>(A, W, n, s);
+    default: return launch_chunks<kF32, 1>(A, W, n, s);
+  }
+}
+
+bool sizes_ok(int32_t n, int32_t vocab, int32_t dtype) {
+  return n >= 0 && vocab >= 1 && (dtype == GAMBIT_BF16 || dtype == GAMBIT_F32);
+}
+constexpr int kMaxRows = 1 << 20;
+
 }  // namespace
 }  // namespace gambit
 
-extern "C" gambit_status gambit_sample(int32_t n, int32_t vocab, const void* logits, int32_t dtype, int64_t row_stride,
-                                       const float* u, const float* temperature, float temperature_all,
-                                       const int32_t* top_k, int32_t top_k_all, const float* top_p, float top_p_all,
-                                       const float* min_p, float min_p_all, int32_t* ids_out, void* stream) {
+extern "C" {
+
+size_t gambit_sample_workspace_size(int32_t n, int32_t vocab, int32_t dtype) {
   using namespace gambit;
-  if (n < 0 || vocab < 1 || (dtype != GAMBIT_BF16 && dtype != GAMBIT_F32) || row_stride < 0) return GAMBIT_ERR_INVALID;
-  if (vocab > kMaxVocab) return GAMBIT_ERR_UNSUPPORTED;
+  if (!sizes_ok(n, vocab, dtype) || vocab > kMaxVocab || n > kMaxRows || n == 0) return 0;
+  return Cuts(n, vocab, dtype == GAMBIT_F32).bytes;
+}
+
+gambit_status gambit_sample(int32_t n, int32_t vocab, const void* logits, int32_t dtype, int64_t row_stride,
+                            const float* u, const float* temperature, float temperature_all, const int32_t* top_k,
+                            int32_t top_k_all, const float* top_p, float top_p_all, const float* min_p,
+                            float min_p_all, int32_t* ids_out, void* workspace, size_t workspace_bytes, void* stream) {
+  using namespace gambit;
+  if (!sizes_ok(n, vocab, dtype) || row_stride < 0) return GAMBIT_ERR_INVALID;
+  if (vocab > kMaxVocab || n > kMaxRows) return GAMBIT_ERR_UNSUPPORTED;
   if (n == 0) return GAMBIT_OK;
   if (!logits || !u || !ids_out || reinterpret_cast<uintptr_t>(logits) % (dtype == GAMBIT_F32 ? 4 : 2)) return GAMBIT_ERR_INVALID;
   for (const void* p : {(const void*)u, (const void*)temperature, (const void*)top_k, (const void*)top_p, (const void*)min_p, (const void*)ids_out})
     if (reinterpret_cast<uintptr_t>(p) % 4) return GAMBIT_ERR_INVALID;
+  const Cuts C(n, vocab, dtype == GAMBIT_F32);
+  if (C.bytes && reinterpret_cast<uintptr_t>(workspace) % 16) return GAMBIT_ERR_INVALID;
+  if (C.bytes && (!workspace || workspace_bytes < C.bytes)) return GAMBIT_ERR_WORKSPACE;
   SampleArgs A{};
   A.z = logits;
   A.stride = row_stride;
   A.vocab = vocab;
-  int log2v = 0;
-  while ((1 << log2v) < vocab) ++log2v;
-  A.scale_bits = 62 - log2v < 50 ? 62 - log2v : 50;
   A.u = u;
   A.temperature = temperature;
   A.top_k = top_k;
@@ -593,10 +691,10 @@ extern "C" gambit_status gambit_sample(int32_t n, int32_t vocab, const void* log
   A.p_all = top_p_all;
   A.m_all = min_p_all;
   A.out = ids_out;
+  uint8_t* ws = static_cast<uint8_t*>(workspace);
   hipStream_t s = static_cast<hipStream_t>(stream);
-  if (dtype == GAMBIT_F32)
-    hipLaunchKernelGGL(sample_kernel<true>, dim3(n), dim3(kThreads), 0, s, A);
-  else
-    hipLaunchKernelGGL(sample_kernel<false>, dim3(n), dim3(kThreads), 0, s, A);
-  return hipGetLastError() == hipSuccess ? GAMBIT_OK : GAMBIT_ERR_DEVICE;
+  const hipError_t e = dtype == GAMBIT_F32 ? launch<true>(A, C, ws, n, s) : launch<false>(A, C, ws, n, s);
+  return e == hipSuccess ? GAMBIT_OK : GAMBIT_ERR_DEVICE;
 }
+
+}  // extern "C"

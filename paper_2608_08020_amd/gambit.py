@@ -96,7 +96,7 @@ EXPORTS = ["gambit_workspace_size", "gambit_pool_create", "gambit_pool_destroy",
            "gambit_scorer_steps", "gambit_scorer_check", "gambit_scorer_last_error", "gambit_stream_read",
            "gambit_plan_kinds", "gambit_mlp_score_static", "gambit_kv_write_layer", "gambit_prompt_attn",
            "gambit_tree_attn", "gambit_kv_write_rotated", "gambit_rms_norm", "gambit_quantize", "gambit_linear_fp8",
-           "gambit_rotate", "gambit_sample"]
+           "gambit_rotate", "gambit_sample", "gambit_sample_workspace_size"]
 
 
 def lib() -> ctypes.CDLL:
@@ -155,7 +155,9 @@ def lib() -> ctypes.CDLL:
         "gambit_quantize": (i32, [i32, i32, vp, i32, i64, i32, vp, vp, vp]),
         "gambit_linear_fp8": (i32, [i32, i32, i32, vp, vp, vp, vp, vp, i32, vp]),
         "gambit_rotate": (i32, [i32, i32, i32, vp, i64, vp, i64, vp, vp, i32, i32, i32, vp, vp, vp]),
-        "gambit_sample": (i32, [i32, i32, vp, i32, i64, vp, vp, f32, vp, i32, vp, f32, vp, f32, vp, vp]),
+        "gambit_sample": (i32, [i32, i32, vp, i32, i64, vp, vp, f32, vp, i32, vp, f32, vp, f32, vp, vp, ctypes.c_size_t,
+                                vp]),
+        "gambit_sample_workspace_size": (ctypes.c_size_t, [i32, i32, i32]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(L, name)
@@ -488,7 +490,10 @@ def sample(logits: torch.Tensor, u: torch.Tensor, temperature=1.0, top_k=0, top_
         out = torch.empty(n, dtype=torch.int32, device=logits.device)
     op = _dev(out, torch.int32, (n,), "out")
     _here(logits, u, out, *given)
-    st = lib().gambit_sample(n, vocab, zp, FLOAT_CODES[logits.dtype], _outer(logits, 0), up, *args, op, _stream(stream))
+    dt = FLOAT_CODES[logits.dtype]
+    size = lib().gambit_sample_workspace_size(n, vocab, dt)
+    ws = torch.empty(size, dtype=torch.uint8, device=logits.device).data_ptr() if size else None
+    st = lib().gambit_sample(n, vocab, zp, dt, _outer(logits, 0), up, *args, op, ws, size, _stream(stream))
     if st != OK:
         raise GambitError(st, "sample")
     return out

@@ -75,13 +75,24 @@ def test_rotate(change):
     _call("gambit_rotate", ROTATE, BAD, **change)
 
 
-SAMPLE = dict(n=4, vocab=100, z=P, zd=0, rs=100, u=P, t=None, t1=1.0, k=None, k1=0, p=None, p1=1.0, m=None, m1=0.0, out=P, stream=None)
+SAMPLE = dict(n=4, vocab=100, z=P, zd=0, rs=100, u=P, t=None, t1=1.0, k=None, k1=0, p=None, p1=1.0, m=None, m1=0.0, out=P, ws=P, size=1 << 30, stream=None)
 
 
 @pytest.mark.parametrize("change", [dict(n=-1), dict(vocab=0), dict(zd=2), dict(rs=-1), dict(z=None), dict(u=None), dict(out=None), dict(z=P + 1), dict(zd=1, z=P + 2),
                                     dict(u=P + 2), dict(out=P + 1), dict(t=P + 1), dict(k=P + 2), dict(p=P + 2), dict(m=P + 3)])
 def test_sample(change):
     _call("gambit_sample", SAMPLE, BAD, **change)
+
+
+def test_sample_workspace():
+    size = g.lib().gambit_sample_workspace_size
+    need = size(8, 100000, 0)
+    assert need > 0 and size(8, 100, 0) == 0 and size(0, 100000, 0) == 0 and size(8, 1 << 19, 0) == 0 and size(8, 100000, 2) == 0
+    big = dict(SAMPLE, n=8, vocab=100000, rs=100000, size=need)
+    _call("gambit_sample", big, g.ERR_WORKSPACE, size=need - 1)
+    _call("gambit_sample", big, g.ERR_WORKSPACE, ws=None)
+    _call("gambit_sample", big, BAD, ws=P + 8)
+    _call("gambit_sample", big, TOO_BIG, n=(1 << 20) + 1)
 
 
 def test_binding_refuses_tensors_of_another_kind():
