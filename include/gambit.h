@@ -629,7 +629,7 @@ gambit_status gambit_quantize(int32_t n, int32_t dim, const void* x, int32_t x_d
  *   w         device [n][k] codes, w_scale fp32 [ceil(n / 128)][ceil(k / 128)]
  *             (4-byte aligned)
  *   out       device [m][n], GAMBIT_BF16 or GAMBIT_F32
- *   k         a multiple of 16; m, n at most 2^24 */
+ *   k         a multiple of 16, at most 2^22; m, n at most 2^24 */
 gambit_status gambit_linear_fp8(int32_t m, int32_t n, int32_t k, const void* x, const float* x_scale,
                                 const void* w, const float* w_scale, void* out, int32_t out_dtype, void* stream);
 

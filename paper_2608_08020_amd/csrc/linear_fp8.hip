@@ -195,21 +195,64 @@ __global__ __launch_bounds__(64 * kSkinnyWaves) void linear_skinny_kernel(Linear
 }
 
 // ---- many tokens ---------------------------------------------------------------
+// kLoads times 64 x 16 bytes from global memory straight into LDS, 1 KiB after
+// another from `lds` on: lane i's from base + at[d].  (One block, so that M0 is
+// set once a load; it is restored, as the compiler does not track it here.)
+template <int kLoads>
+__device__ inline void dma_rows(const uint8_t* base, const uint32_t* at, uint32_t lds) {
+  static_assert(kLoads == 2 || kLoads == 4 || kLoads == 8, "");
+  uint32_t save;
+#define DMA_NEXT(v) "s_add_u32 m0, m0, 0x400\n\ts_nop 0\n\tglobal_load_lds_dwordx4 " v ", %2\n\t"
+  if constexpr (kLoads == 8)
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %3, %2\n\t"
+                 DMA_NEXT("%4") DMA_NEXT("%5") DMA_NEXT("%6") DMA_NEXT("%7") DMA_NEXT("%8") DMA_NEXT("%9") DMA_NEXT("%10")
+                 "s_mov_b32 m0, %0"
+                 : "=&s"(save)
+                 : "s"(lds), "s"(base), "v"(at[0]), "v"(at[1]), "v"(at[2]), "v"(at[3]), "v"(at[4]), "v"(at[5]), "v"(at[6]), "v"(at[7])
+                 : "memory", "scc");
+  else if constexpr (kLoads == 4)
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %3, %2\n\t"
+                 DMA_NEXT("%4") DMA_NEXT("%5") DMA_NEXT("%6")
+                 "s_mov_b32 m0, %0"
+                 : "=&s"(save)
+                 : "s"(lds), "s"(base), "v"(at[0]), "v"(at[1]), "v"(at[2]), "v"(at[3])
+                 : "memory", "scc");
+  else
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %3, %2\n\t"
+                 DMA_NEXT("%4")
+                 "s_mov_b32 m0, %0"
+                 : "=&s"(save)
+                 : "s"(lds), "s"(base), "v"(at[0]), "v"(at[1])
+                 : "memory", "scc");
+#undef DMA_NEXT
+}
+__device__ inline void dma_dword(const void* base, uint32_t at, uint32_t lds) {
+  uint32_t save;
+  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %3, %2\n\ts_mov_b32 m0, %0"
+               : "=&s"(save)
+               : "s"(lds), "s"(base), "v"(at)
+               : "memory");
+}
+
 // Tiles of kTF features x kTT tokens, kWF x kWT waves.  A block of k of both
 // operands and of the tokens' scales goes from global memory straight into an
 // LDS stage while the block before it is multiplied.  Row r's 16-byte chunk c
 // sits at chunk position c ^ ((r >> 1) & 7) of its 128-byte row, so that the sixteen
 // rows of one operand read fall on sixteen different 16-byte bank groups.
+//
+// The matrix unit is fed without a pause: a row of products (one block of
+// features, all of a wave's tokens) is issued while the row before it is
+// scaled and added, four fused additions in the shadow of each, and the next
+// features are read from LDS.
 template <bool kExact, int kTF, int kTT, int kWF, int kWT>
 __global__ __launch_bounds__(64 * kWF * kWT) void linear_tile_kernel(LinearArgs A) {
   constexpr int kWaves = kWF * kWT, kRows = kTF + kTT, kLoads = kRows / 8 / kWaves;
   constexpr int kA = kTF / kWF / 16, kB = kTT / kWT / 16, kSlices = kTT / 64;
   constexpr int kStage = kRows * kKB + kWaves * 256;
   static_assert(kRows % (8 * kWaves) == 0 && kTF % (8 * kLoads) == 0, "a wave's rows are of one operand");
-  static_assert(128 % (kTF / kWF) == 0 || (kTF / kWF) % 128 == 0, "a wave's features share their scale");
-  static_assert(kTF / kWF <= 128 && kWaves >= kSlices, "");
+  static_assert(128 % (kTF / kWF) == 0 && kWaves >= kSlices, "a wave's features share their scale");
   __shared__ __attribute__((aligned(1024))) uint8_t lds[2 * kStage];
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, i = lane & 15, q = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, i = lane & 15, q = lane >> 4;
   // Tiles in groups of four token tiles; consecutive ones go to the same XCD
   // (workgroup b runs on XCD b % 8) where the grid divides, so that what an
   // XCD's L2 holds serves several tiles.
@@ -218,20 +261,25 @@ __global__ __launch_bounds__(64 * kWF * kWT) void linear_tile_kernel(LinearArgs 
   const int group = item / (4 * A.tiles_f), gt = min(4, A.tiles_t - 4 * group), in = item - group * 4 * A.tiles_f;
   const int f0 = in / gt * kTF, t0 = (4 * group + in % gt) * kTT;
 
-  // this lane's load sources: rows past the end re-read the last one (never stored)
-  const uint8_t* src[kLoads];
+  // this lane's load sources, relative to its operand's first row of the tile:
+  // rows past the end re-read the last one (never stored)
+  const bool of_w = kLoads * 8 * wave < kTF;
+  const uint8_t* src = of_w ? A.w + (size_t)f0 * A.k : A.x + (size_t)t0 * A.k;
+  uint32_t at[kLoads];
 #pragma unroll
   for (int d = 0; d < kLoads; ++d) {
     const int r = 8 * (kLoads * wave + d) + (lane >> 3), c = (lane & 7) ^ ((r >> 1) & 7);
-    src[d] = (r < kTF ? A.w + (size_t)min(f0 + r, A.n - 1) * A.k : A.x + (size_t)min(t0 + r - kTF, A.m - 1) * A.k) + 16 * c;
+    at[d] = (uint32_t)(of_w ? min(r, A.n - 1 - f0) : min(r - kTF, A.m - 1 - t0)) * A.k + 16 * c;
   }
-  const int slice = wave % kSlices;
-  const float* ssrc = A.xs + min(t0 + 64 * slice + lane, A.m - 1);
-  auto issue = [&](int b) {
-    uint8_t* st = lds + (b & 1) * kStage;
-#pragma unroll
-    for (int d = 0; d < kLoads; ++d) dma16(src[d] + (size_t)b * kKB, st + 8 * (kLoads * wave + d) * kKB);
-    dma4(ssrc + (size_t)b * A.m, st + kRows * kKB + 256 * wave);
+  const float* ssrc = A.xs;
+  const uint32_t sat = 4 * (uint32_t)min(t0 + 64 * (wave % kSlices) + lane, A.m - 1);
+  const uint32_t lds0 = lds_addr(lds);
+  const uint32_t dst = lds0 + 8 * kLoads * wave * kKB, sdst = lds0 + kRows * kKB + 256 * wave;
+  auto issue = [&](int b) {  // blocks in order: the sources move along
+    dma_rows<kLoads>(src, at, dst + (b & 1) * kStage);
+    dma_dword(ssrc, sat, sdst + (b & 1) * kStage);
+    src += kKB;
+    ssrc += A.m;
   };
 
   const int wf = wave / kWT, wt = wave % kWT, swz = (i >> 1) & 7;
@@ -241,36 +289,45 @@ __global__ __launch_bounds__(64 * kWF * kWT) void linear_tile_kernel(LinearArgs 
   const float* ws = A.ws + (size_t)min((f0 + kTF / kWF * wf) / kKB, (A.n - 1) / kKB) * A.blocks;
   f32x4 acc[kA][kB] = {};
   auto multiply = [&](const uint8_t* st, float s) {
+    auto codes = [&](int off) {
+      return join(*reinterpret_cast<const i32x4*>(st + off + pos0), *reinterpret_cast<const i32x4*>(st + off + pos1));
+    };
     Operand<kExact> x[kB], w;
+    i32x8 next = codes(offa);
     float c[kB];
 #pragma unroll
     for (int b = 0; b < kB; ++b) {
-      const uint8_t* p = st + offb + b * 16 * kKB;
-      x[b].set(join(*reinterpret_cast<const i32x4*>(p + pos0), *reinterpret_cast<const i32x4*>(p + pos1)));
+      x[b].set(codes(offb + b * 16 * kKB));
       c[b] = *reinterpret_cast<const float*>(st + offs + 64 * b) * s;
     }
+    f32x4 part[2][kB];
 #pragma unroll
-    for (int a = 0; a < kA; ++a) {
-      const uint8_t* p = st + offa + a * 16 * kKB;
-      w.set(join(*reinterpret_cast<const i32x4*>(p + pos0), *reinterpret_cast<const i32x4*>(p + pos1)));
+    for (int a = 0; a <= kA; ++a) {
+      if (a < kA) w.set(next);
+      if (a + 1 < kA) next = codes(offa + (a + 1) * 16 * kKB);
 #pragma unroll
       for (int b = 0; b < kB; ++b) {
-        const f32x4 y = block_sum(w, x[b]);
+        __builtin_amdgcn_sched_barrier(0);
+        if (a < kA) part[a & 1][b] = block_sum(w, x[b]);
+        if (a > 0)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) acc[a][b][e] = fmaf(y[e], c[b], acc[a][b][e]);
+          for (int e = 0; e < 4; ++e) acc[a - 1][b][e] = fmaf(part[(a - 1) & 1][b][e], c[b], acc[a - 1][b][e]);
       }
     }
+    __builtin_amdgcn_sched_barrier(0);
   };
 
   const int whole = A.k / kKB;
+  float s = ws[0];
   if (whole > 0) issue(0);
   for (int b = 0; b < whole; ++b) {
-    const float s = ws[b];
     wait_vmcnt<0>();
-    __builtin_amdgcn_s_waitcnt(0xC07F);  // this wave's LDS reads
-    barrier_no_fence();                  // block b is in LDS; every wave is done with block b - 1
+    barrier_no_fence();  // block b is in LDS; every wave is done with block b - 1
     if (b + 1 < whole) issue(b + 1);
-    multiply(lds + (b & 1) * kStage, s);
+    const float now = s;
+    s = ws[min(b + 1, A.blocks - 1)];
+    multiply(lds + (b & 1) * kStage, now);
+    __builtin_amdgcn_s_waitcnt(0xC07F);  // this wave's LDS reads
   }
   if (whole < A.blocks) {  // the last block: its values behind k are zero
     __syncthreads();
@@ -280,10 +337,10 @@ __global__ __launch_bounds__(64 * kWF * kWT) void linear_tile_kernel(LinearArgs 
     for (int d = 0; d < kLoads; ++d) {
       const int r = 8 * (kLoads * wave + d) + (lane >> 3), c = (lane & 7) ^ ((r >> 1) & 7);
       i32x4 v{};
-      if (c < chunks) v = *reinterpret_cast<const i32x4*>(src[d] + (size_t)whole * kKB);
+      if (c < chunks) v = *reinterpret_cast<const i32x4*>(src + at[d]);
       *reinterpret_cast<i32x4*>(st + r * kKB + (lane & 7) * 16) = v;
     }
-    *reinterpret_cast<float*>(st + kRows * kKB + 256 * wave + 4 * lane) = ssrc[(size_t)whole * A.m];
+    *reinterpret_cast<float*>(st + kRows * kKB + 256 * wave + 4 * lane) = ssrc[sat / 4];
     __syncthreads();
     multiply(st, ws[whole]);
   }
@@ -302,7 +359,7 @@ extern "C" gambit_status gambit_linear_fp8(int32_t m, int32_t n, int32_t k, cons
                                            void* stream) {
   using namespace gambit;
   if (m < 0 || n < 1 || k < 16 || k % 16 || (out_dtype != GAMBIT_BF16 && out_dtype != GAMBIT_F32)) return GAMBIT_ERR_INVALID;
-  if (m > 1 << 24 || n > 1 << 24) return GAMBIT_ERR_UNSUPPORTED;
+  if (m > 1 << 24 || n > 1 << 24 || k > 1 << 22) return GAMBIT_ERR_UNSUPPORTED;
   if (m == 0) return GAMBIT_OK;
   if (!x || !x_scale || !w || !w_scale || !out) return GAMBIT_ERR_INVALID;
   for (const void* p : {x, w, static_cast<const void*>(out)})

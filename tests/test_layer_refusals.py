@@ -36,6 +36,7 @@ def test_sizes_beyond_the_kernels():
     _call("gambit_quantize", QUANT, TOO_BIG, n=1 << 30, dim=1024)
     _call("gambit_linear_fp8", LINEAR, TOO_BIG, m=(1 << 24) + 1)
     _call("gambit_linear_fp8", LINEAR, TOO_BIG, n=(1 << 24) + 1)
+    _call("gambit_linear_fp8", LINEAR, TOO_BIG, k=(1 << 22) + 16)
     _call("gambit_rotate", ROTATE, TOO_BIG, hq=5000)
     _call("gambit_rotate", ROTATE, TOO_BIG, n=1 << 30)
     _call("gambit_sample", SAMPLE, TOO_BIG, vocab=(1 << 18) + 1)
