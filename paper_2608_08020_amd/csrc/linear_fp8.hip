@@ -234,25 +234,34 @@ __device__ inline void dma_dword(const void* base, uint32_t at, uint32_t lds) {
                : "memory");
 }
 
+// Keeps the computation of v above what follows.
+template <class V>
+__device__ inline void pin(V& v) {
+  asm volatile("" : "+v"(v));
+}
+
 // Tiles of kTF features x kTT tokens, kWF x kWT waves.  A block of k of both
 // operands and of the tokens' scales goes from global memory straight into an
 // LDS stage while the block before it is multiplied.  Row r's 16-byte chunk c
 // sits at chunk position c ^ ((r >> 1) & 7) of its 128-byte row, so that the sixteen
 // rows of one operand read fall on sixteen different 16-byte bank groups.
 //
-// The matrix unit is fed without a pause: a row of products (one block of
-// features, all of a wave's tokens) is issued while the row before it is
-// scaled and added, four fused additions in the shadow of each, and the next
-// features are read from LDS.
-template <bool kExact, int kTF, int kTT, int kWF, int kWT>
+// The matrix unit is fed without a pause.  Products are issued in rows (one
+// block of sixteen features, all of a wave's tokens); the one two before the last is
+// scaled and added meanwhile, and the next features are read from LDS.  Before a
+// block's last row its stage has been read, the next one waited for, and the one
+// kStages later sent for; during the last row the next block's tokens take the
+// places of this one's.
+template <bool kExact, int kTF, int kTT, int kWF, int kWT, int kStages>
 __global__ __launch_bounds__(64 * kWF * kWT) void linear_tile_kernel(LinearArgs A) {
   constexpr int kWaves = kWF * kWT, kRows = kTF + kTT, kLoads = kRows / 8 / kWaves;
-  constexpr int kA = kTF / kWF / 16, kB = kTT / kWT / 16, kSlices = kTT / 64;
+  constexpr int kF = kTF / kWF, kT = kTT / kWT, kA = kF / 16, kB = kT / 16, kProducts = kA * kB, kSlices = kTT / 64, kSlicesF = (kTF + 127) / 128;
   constexpr int kStage = kRows * kKB + kWaves * 256;
   static_assert(kRows % (8 * kWaves) == 0 && kTF % (8 * kLoads) == 0, "a wave's rows are of one operand");
-  static_assert(128 % (kTF / kWF) == 0 && kWaves >= kSlices, "a wave's features share their scale");
-  __shared__ __attribute__((aligned(1024))) uint8_t lds[2 * kStage];
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, i = lane & 15, q = lane >> 4;
+  static_assert(128 % kF == 0 && kWaves >= kSlices + kSlicesF, "a wave's features share their scale");
+  static_assert(kWaves * kF * kT * 2 <= kStages * kStage, "the outputs in bf16 go through LDS");
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[kStages * kStage];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   // Tiles in groups of four token tiles; consecutive ones go to the same XCD
   // (workgroup b runs on XCD b % 8) where the grid divides, so that what an
   // XCD's L2 holds serves several tiles.
@@ -271,84 +280,143 @@ __global__ __launch_bounds__(64 * kWF * kWT) void linear_tile_kernel(LinearArgs 
     const int r = 8 * (kLoads * wave + d) + (lane >> 3), c = (lane & 7) ^ ((r >> 1) & 7);
     at[d] = (uint32_t)(of_w ? min(r, A.n - 1 - f0) : min(r - kTF, A.m - 1 - t0)) * A.k + 16 * c;
   }
-  const float* ssrc = A.xs;
-  const uint32_t sat = 4 * (uint32_t)min(t0 + 64 * (wave % kSlices) + lane, A.m - 1);
+  // scales: 64 tokens a wave, then 128 features a wave
+  const bool s_of_x = wave < kSlices;
+  const int srow = min(f0 / kKB + (wave - kSlices) % kSlicesF, (A.n - 1) / kKB);
+  const float* ssrc = s_of_x ? A.xs : A.ws + (size_t)srow * A.blocks;
+  const int snext = s_of_x ? A.m : 1;
+  const uint32_t sat = s_of_x ? 4 * (uint32_t)min(t0 + 64 * wave + lane, A.m - 1) : 0;
   const uint32_t lds0 = lds_addr(lds);
   const uint32_t dst = lds0 + 8 * kLoads * wave * kKB, sdst = lds0 + kRows * kKB + 256 * wave;
-  auto issue = [&](int b) {  // blocks in order: the sources move along
-    dma_rows<kLoads>(src, at, dst + (b & 1) * kStage);
-    dma_dword(ssrc, sat, sdst + (b & 1) * kStage);
+  const int whole = A.k / kKB;
+  auto issue = [&](int b, int stage) {  // blocks in order: the sources move along
+    if (b < whole) {
+      dma_rows<kLoads>(src, at, dst + stage * kStage);
+    } else {  // the last block: its values behind k are zero
+      const int chunks = (A.k - whole * kKB) / 16;
+#pragma unroll
+      for (int d = 0; d < kLoads; ++d) {
+        const int r = 8 * (kLoads * wave + d) + (lane >> 3), cc = (lane & 7) ^ ((r >> 1) & 7);
+        i32x4 v{};
+        if (cc < chunks) v = *reinterpret_cast<const i32x4*>(src + at[d]);
+        *reinterpret_cast<i32x4*>(lds + stage * kStage + r * kKB + (lane & 7) * 16) = v;
+      }
+    }
+    dma_dword(ssrc, sat, sdst + stage * kStage);
     src += kKB;
-    ssrc += A.m;
+    ssrc += snext;
   };
 
-  const int wf = wave / kWT, wt = wave % kWT, swz = (i >> 1) & 7;
-  const int offa = (kTF / kWF * wf + i) * kKB, offb = (kTF + kTT / kWT * wt + i) * kKB;
-  const int pos0 = (q ^ swz) * 16, pos1 = ((q | 4) ^ swz) * 16;
-  const int offs = kRows * kKB + 4 * (kTT / kWT * wt + i);
-  const float* ws = A.ws + (size_t)min((f0 + kTF / kWF * wf) / kKB, (A.n - 1) / kKB) * A.blocks;
+  const int wf = wave / kWT, wt = wave % kWT, i = lane & 15, q = lane >> 4, swz = (i >> 1) & 7;
+  const int pos0 = i * kKB + (q ^ swz) * 16, pos1 = i * kKB + ((q | 4) ^ swz) * 16;
+  const int offs = kRows * kKB + 4 * (kT * wt + i), offw = kRows * kKB + 256 * (kSlices + kF * wf / kKB);
+  auto codes = [&](const uint8_t* st, int row) {  // of rows row + i, row uniform
+    return join(*reinterpret_cast<const i32x4*>(st + row * kKB + pos0), *reinterpret_cast<const i32x4*>(st + row * kKB + pos1));
+  };
   f32x4 acc[kA][kB] = {};
-  auto multiply = [&](const uint8_t* st, float s) {
-    auto codes = [&](int off) {
-      return join(*reinterpret_cast<const i32x4*>(st + off + pos0), *reinterpret_cast<const i32x4*>(st + off + pos1));
-    };
-    Operand<kExact> x[kB], w;
-    i32x8 next = codes(offa);
+  f32x4 part[2] = {};   // products on their way
+  float factor[2] = {}; // theirs
+  i32x8 x[kB], w;       // the block's tokens, and its next features
+  float xs[kB], s;      // the tokens' scales, the features'
+  auto read_token = [&](const uint8_t* st, int b) {
+    x[b] = codes(st, kTF + kT * wt + 16 * b);
+    xs[b] = *reinterpret_cast<const float*>(st + offs + 64 * b);
+  };
+  auto add = [&](int j) {  // the oldest of them, product j of its block
+    f32x4& to = acc[j / kB][j % kB];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) to[e] = fmaf(part[0][e], factor[0], to[e]);
+    __builtin_amdgcn_sched_barrier(0);
+    pin(to);
+    part[0] = part[1];
+    factor[0] = factor[1];
+  };
+#pragma unroll
+  for (int b = 0; b < kStages - 1; ++b)
+    if (b < A.blocks) issue(b, b);
+  if (kStages > 2 && kStages - 1 <= whole)
+    wait_vmcnt<(kStages - 2) * (kLoads + 1)>();
+  else
+    wait_vmcnt<0>();
+  __builtin_amdgcn_s_waitcnt(0xC07F);  // LDS
+  barrier_no_fence();
+  if (kStages - 1 < A.blocks) issue(kStages - 1, kStages - 1);
+  w = codes(lds, kF * wf);
+#pragma unroll
+  for (int b = 0; b < kB; ++b) read_token(lds, b);
+  s = *reinterpret_cast<const float*>(lds + offw);
+  for (int k = 0, stage = 0; k < A.blocks; ++k) {
+    const int next = stage + 1 < kStages ? stage + 1 : 0;
+    const uint8_t *st = lds + stage * kStage, *nst = lds + next * kStage;
+    Operand<kExact> xo[kB], wo;
     float c[kB];
 #pragma unroll
-    for (int b = 0; b < kB; ++b) {
-      x[b].set(codes(offb + b * 16 * kKB));
-      c[b] = *reinterpret_cast<const float*>(st + offs + 64 * b) * s;
-    }
-    f32x4 part[2][kB];
+    for (int b = 0; b < kB; ++b) xo[b].set(x[b]);
 #pragma unroll
-    for (int a = 0; a <= kA; ++a) {
-      if (a < kA) w.set(next);
-      if (a + 1 < kA) next = codes(offa + (a + 1) * 16 * kKB);
+    for (int a = 0; a < kA; ++a) {
+      wo.set(w);
+      if (a + 1 < kA) {
+        w = codes(st, kF * wf + (a + 1) * 16);
+      } else {
+        __builtin_amdgcn_s_waitcnt(0xC07F);  // this wave's LDS reads (and writes)
+        if (kStages > 2 && k + kStages <= whole)  // (of the blocks behind k + 1, all whole ones, every load may be on its way)
+          wait_vmcnt<(kStages - 2) * (kLoads + 1)>();
+        else
+          wait_vmcnt<0>();
+        barrier_no_fence();  // block k + 1 is in LDS; every wave has read block k
+        if (k + kStages < A.blocks) issue(k + kStages, stage);
+        w = codes(nst, kF * wf);  // (after the last block: what is there, and not used)
+      }
 #pragma unroll
       for (int b = 0; b < kB; ++b) {
         __builtin_amdgcn_sched_barrier(0);
-        if (a < kA) part[a & 1][b] = block_sum(w, x[b]);
-        if (a > 0)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) acc[a - 1][b][e] = fmaf(part[(a - 1) & 1][b][e], c[b], acc[a - 1][b][e]);
+        const f32x4 y = block_sum(wo, xo[b]);
+        __builtin_amdgcn_sched_barrier(0);
+        if (a == 0) c[b] = xs[b] * s;
+        pin(part[0]);
+        add((a * kB + b + kProducts - 2) % kProducts);  // (at a block's first products: of the block before)
+        part[1] = y;
+        factor[1] = c[b];
+        if (a == kA - 1) {
+          if (b == 0) s = *reinterpret_cast<const float*>(nst + offw);
+          read_token(nst, b);
+        }
       }
     }
     __builtin_amdgcn_sched_barrier(0);
-  };
+    stage = next;
+  }
+  add(kProducts - 2);
+  add(kProducts - 1);
 
-  const int whole = A.k / kKB;
-  float s = ws[0];
-  if (whole > 0) issue(0);
-  for (int b = 0; b < whole; ++b) {
-    wait_vmcnt<0>();
-    barrier_no_fence();  // block b is in LDS; every wave is done with block b - 1
-    if (b + 1 < whole) issue(b + 1);
-    const float now = s;
-    s = ws[min(b + 1, A.blocks - 1)];
-    multiply(lds + (b & 1) * kStage, now);
-    __builtin_amdgcn_s_waitcnt(0xC07F);  // this wave's LDS reads
-  }
-  if (whole < A.blocks) {  // the last block: its values behind k are zero
-    __syncthreads();
-    const int chunks = (A.k - whole * kKB) / 16;
-    uint8_t* st = lds + (whole & 1) * kStage;
+  const int tw = t0 + kT * wt, fw = f0 + kF * wf;
+  if (kExact || A.n % 8 != 0) {
 #pragma unroll
-    for (int d = 0; d < kLoads; ++d) {
-      const int r = 8 * (kLoads * wave + d) + (lane >> 3), c = (lane & 7) ^ ((r >> 1) & 7);
-      i32x4 v{};
-      if (c < chunks) v = *reinterpret_cast<const i32x4*>(src + at[d]);
-      *reinterpret_cast<i32x4*>(st + r * kKB + (lane & 7) * 16) = v;
-    }
-    *reinterpret_cast<float*>(st + kRows * kKB + 256 * wave + 4 * lane) = ssrc[sat / 4];
-    __syncthreads();
-    multiply(st, ws[whole]);
+    for (int a = 0; a < kA; ++a)
+#pragma unroll
+      for (int b = 0; b < kB; ++b) store4(A, tw + 16 * b + i, fw + 16 * a + 4 * q, acc[a][b]);
+    return;
   }
+  // Whole rows of kF features leave together: a wave lays its outputs out in LDS (token t's
+  // chunk c of eight features at position c ^ t) and reads them back in rows.
+  constexpr int kC = kF / 8;
+  __syncthreads();  // every wave is done with the stages
+  uint8_t* own = lds + wave * (kF * kT * 2);
 #pragma unroll
   for (int a = 0; a < kA; ++a)
 #pragma unroll
-    for (int b = 0; b < kB; ++b)
-      store4(A, t0 + kTT / kWT * wt + 16 * b + i, f0 + kTF / kWF * wf + 16 * a + 4 * q, acc[a][b]);
+    for (int b = 0; b < kB; ++b) {
+      const f32x4& y = acc[a][b];
+      const int c = 2 * a + q / 2, t = 16 * b + i;
+      *reinterpret_cast<uint2*>(own + t * (2 * kF) + (c ^ (t % kC)) * 16 + q % 2 * 8) = make_uint2(bf16_pair(y[0], y[1]), bf16_pair(y[2], y[3]));
+    }
+  uint16_t* out = static_cast<uint16_t*>(A.out);
+#pragma unroll
+  for (int d = 0; d < kT * kC / 64; ++d) {
+    const int t = (64 * d + lane) / kC, cc = lane % kC, f = fw + 8 * cc;
+    const uint4 v = *reinterpret_cast<const uint4*>(own + t * (2 * kF) + (cc ^ (t % kC)) * 16);
+    if (tw + t < A.m && f < A.n) *reinterpret_cast<uint4*>(out + (size_t)(tw + t) * A.n + f) = v;
+  }
 }
 
 }  // namespace
@@ -397,10 +465,12 @@ extern "C" gambit_status gambit_linear_fp8(int32_t m, int32_t n, int32_t k, cons
       wide ? skinny(linear_skinny_kernel<kExact, 4, 2>, 64, 32) : skinny(linear_skinny_kernel<kExact, 4, 1>, 64, 16);
     else if (m <= 128 && !wide)
       skinny(linear_skinny_kernel<kExact, 8, 1>, 128, 16);
+    else if constexpr (kExact)
+      tile(linear_tile_kernel<true, 128, 128, 2, 4, 2>, 128, 128, 512);
     else if ((int64_t)((n + 255) / 256) * ((m + 255) / 256) >= 256)
-      tile(linear_tile_kernel<kExact, 256, 256, 2, 4>, 256, 256, 512);
+      tile(linear_tile_kernel<false, 256, 256, 2, 4, 2>, 256, 256, 512);
     else
-      tile(linear_tile_kernel<kExact, 128, 128, 2, 4>, 128, 128, 512);
+      tile(linear_tile_kernel<false, 128, 128, 2, 4, 4>, 128, 128, 512);
   };
   A.f32 ? choose(std::true_type{}) : choose(std::false_type{});
   return hipGetLastError() == hipSuccess ? GAMBIT_OK : GAMBIT_ERR_DEVICE;
