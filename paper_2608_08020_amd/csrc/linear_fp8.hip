@@ -454,6 +454,7 @@ extern "C" gambit_status gambit_linear_fp8(int32_t m, int32_t n, int32_t k, cons
     A.tiles_t = (m + tokens - 1) / tokens;
     hipLaunchKernelGGL(kernel, dim3(A.tiles_f * A.tiles_t), dim3(threads), 0, s, A);
   };
+  auto tiles = [&](int side) { return (int64_t)((n + side - 1) / side) * ((m + side - 1) / side); };
   auto choose = [&](auto exact) {
     constexpr bool kExact = decltype(exact)::value;
     const bool wide = n >= 32 * 512;
@@ -467,10 +468,16 @@ extern "C" gambit_status gambit_linear_fp8(int32_t m, int32_t n, int32_t k, cons
       skinny(linear_skinny_kernel<kExact, 8, 1>, 128, 16);
     else if constexpr (kExact)
       tile(linear_tile_kernel<true, 128, 128, 2, 4, 2>, 128, 128, 512);
-    else if ((int64_t)((n + 255) / 256) * ((m + 255) / 256) >= 256)
+    // Tiles of 256 x 256 re-read least, but need one for each of the 256 CUs.  Of the
+    // small ones two workgroups share a CU (two stages each) or, where there is one a
+    // CU at most, a third stage hides the loads (us, two / three stages: 224 tiles
+    // 64 / 57, 768 tiles 55 / 65).
+    else if (tiles(256) >= 256)
       tile(linear_tile_kernel<false, 256, 256, 2, 4, 2>, 256, 256, 512);
+    else if (tiles(128) > 256)
+      tile(linear_tile_kernel<false, 128, 128, 2, 4, 2>, 128, 128, 512);
     else
-      tile(linear_tile_kernel<false, 128, 128, 2, 4, 4>, 128, 128, 512);
+      tile(linear_tile_kernel<false, 128, 128, 2, 4, 3>, 128, 128, 512);
   };
   A.f32 ? choose(std::true_type{}) : choose(std::false_type{});
   return hipGetLastError() == hipSuccess ? GAMBIT_OK : GAMBIT_ERR_DEVICE;
