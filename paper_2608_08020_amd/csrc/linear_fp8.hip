@@ -111,90 +111,23 @@ __device__ inline void store4(const LinearArgs& A, int t, int f, f32x4 y) {
   }
 }
 
-// ---- few tokens --------------------------------------------------------------
-// Bound by the weights' bytes.  A workgroup takes 16 kF features and up to
-// 16 kT tokens; its eight waves take every eighth block of k each, weights and
-// tokens straight into registers, and add up through LDS.
-constexpr int kSkinnyWaves = 8;
-
-template <bool kExact, int kT, int kF>
-__global__ __launch_bounds__(64 * kSkinnyWaves) void linear_skinny_kernel(LinearArgs A) {
-  __shared__ f32x4 sums[kSkinnyWaves][kT * kF][64];
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, i = lane & 15, q = lane >> 4;
-  const int f0 = blockIdx.x * 16 * kF, t0 = blockIdx.y * 16 * kT;
-  const uint8_t *wp[kF], *xp[kT];
-  const float* sp[kT];
-#pragma unroll
-  for (int f = 0; f < kF; ++f) wp[f] = A.w + (size_t)min(f0 + 16 * f + i, A.n - 1) * A.k + 32 * q;
-#pragma unroll
-  for (int t = 0; t < kT; ++t) {
-    const int tok = min(t0 + 16 * t + i, A.m - 1);  // tokens past the end repeat the last one (never stored)
-    xp[t] = A.x + (size_t)tok * A.k + 32 * q;
-    sp[t] = A.xs + tok;
-  }
-  const float* ws = A.ws + (size_t)(f0 / kKB) * A.blocks;
-  f32x4 acc[kF][kT] = {};
-  auto add = [&](const i32x8* w, const i32x8* x, int b) {
-    const float s = ws[b];
-    Operand<kExact> wo[kF], xo;
-#pragma unroll
-    for (int f = 0; f < kF; ++f) wo[f].set(w[f]);
-#pragma unroll
-    for (int t = 0; t < kT; ++t) {
-      const float c = sp[t][(size_t)b * A.m] * s;
-      xo.set(x[t]);
-#pragma unroll
-      for (int f = 0; f < kF; ++f) {
-        const f32x4 y = block_sum(wo[f], xo);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) acc[f][t][e] = fmaf(y[e], c, acc[f][t][e]);
-      }
-    }
-  };
-  const int whole = A.k / kKB;
-#pragma unroll 2
-  for (int b = wave; b < whole; b += kSkinnyWaves) {
-    i32x8 w[kF], x[kT];
-#pragma unroll
-    for (int f = 0; f < kF; ++f) {
-      const i32x4* p = reinterpret_cast<const i32x4*>(wp[f] + (size_t)b * kKB);
-      w[f] = join(__builtin_nontemporal_load(p), __builtin_nontemporal_load(p + 1));
-    }
-#pragma unroll
-    for (int t = 0; t < kT; ++t) {
-      const i32x4* p = reinterpret_cast<const i32x4*>(xp[t] + (size_t)b * kKB);
-      x[t] = join(p[0], p[1]);
-    }
-    add(w, x, b);
-  }
-  if (whole < A.blocks && wave == whole % kSkinnyWaves) {  // the last block's values behind k are zero
-    const int left = A.k - whole * kKB - 32 * q;
-    auto get = [&](const uint8_t* base) {
-      const i32x4* p = reinterpret_cast<const i32x4*>(base + (size_t)whole * kKB);
-      return join(left > 0 ? p[0] : i32x4{}, left > 16 ? p[1] : i32x4{});
-    };
-    i32x8 w[kF], x[kT];
-#pragma unroll
-    for (int f = 0; f < kF; ++f) w[f] = get(wp[f]);
-#pragma unroll
-    for (int t = 0; t < kT; ++t) x[t] = get(xp[t]);
-    add(w, x, whole);
-  }
-#pragma unroll
-  for (int f = 0; f < kF; ++f)
-#pragma unroll
-    for (int t = 0; t < kT; ++t) sums[wave][f * kT + t][lane] = acc[f][t];
-  __syncthreads();
-  for (int s = threadIdx.x; s < kT * kF * 64; s += 64 * kSkinnyWaves) {
-    const int tile = s >> 6, l = s & 63;
-    f32x4 y = sums[0][tile][l];
-#pragma unroll
-    for (int v = 1; v < kSkinnyWaves; ++v) y += sums[v][tile][l];
-    store4(A, t0 + 16 * (tile % kT) + (l & 15), f0 + 16 * (tile / kT) + 4 * (l >> 4), y);
-  }
+// ---- from global memory into LDS ------------------------------------------------
+// 64 x 16 (4) bytes from global memory straight into LDS at `lds`, lane i's from
+// base + at.  (M0 is restored, as the compiler does not track it here.)
+__device__ inline void dma_16(const uint8_t* base, uint32_t at, uint32_t lds) {
+  uint32_t save;
+  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %3, %2\n\ts_mov_b32 m0, %0"
+               : "=&s"(save)
+               : "s"(lds), "s"(base), "v"(at)
+               : "memory");
 }
-
-// ---- many tokens ---------------------------------------------------------------
+__device__ inline void dma_dword(const void* base, uint32_t at, uint32_t lds) {
+  uint32_t save;
+  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %3, %2\n\ts_mov_b32 m0, %0"
+               : "=&s"(save)
+               : "s"(lds), "s"(base), "v"(at)
+               : "memory");
+}
 // kLoads times 64 x 16 bytes from global memory straight into LDS, 1 KiB after
 // another from `lds` on: lane i's from base + at[d].  (One block, so that M0 is
 // set once a load; it is restored, as the compiler does not track it here.)
@@ -226,14 +159,94 @@ __device__ inline void dma_rows(const uint8_t* base, const uint32_t* at, uint32_
                  : "memory", "scc");
 #undef DMA_NEXT
 }
-__device__ inline void dma_dword(const void* base, uint32_t at, uint32_t lds) {
-  uint32_t save;
-  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %3, %2\n\ts_mov_b32 m0, %0"
-               : "=&s"(save)
-               : "s"(lds), "s"(base), "v"(at)
-               : "memory");
+// ---- few tokens, few features ---------------------------------------------------
+// Bound by the weights' bytes and by how soon they are asked for.  A workgroup
+// takes sixteen features and kTT (16 or 32) tokens, 512 values of k at a time
+// through LDS; of these each wave takes one block of 128 and sixteen tokens, and the
+// waves' sums meet in LDS.  Row r's 16-byte chunk c of a stage sits at chunk position
+// c ^ (r % 16) of its 512 bytes: an operand read's sixteen rows on sixteen bank groups.
+template <bool kExact, int kTT, int kStages>
+__global__ __launch_bounds__(kTT == 32 ? 512 : 256) void linear_split_kernel(LinearArgs A) {
+  constexpr int kWaves = kTT == 32 ? 8 : 4, kRows = 16 + kTT;
+  constexpr int kBlocks = 4, kBytes = kBlocks * kKB, kLoads = kRows / 2 / kWaves, kScales = 2 * kBlocks / kWaves;
+  constexpr int kStage = kRows * kBytes + 2 * kBlocks * 256;
+  static_assert(kRows / 2 % kWaves == 0 && kWaves * 1024 <= kStages * kStage, "");
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[kStages * kStage];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, i = lane & 15, q = lane >> 4;
+  const int f0 = blockIdx.x * 16, t0 = blockIdx.y * kTT;
+  // load d of this wave: rows 2 l and 2 l + 1, l = kLoads wave + d; rows past the end re-read the last one (never stored)
+  const uint8_t *wsrc = A.w + (size_t)f0 * A.k, *xsrc = A.x + (size_t)t0 * A.k;
+  auto row = [&](int d) { return 2 * (kLoads * wave + d) + (lane >> 5); };
+  auto of_w = [&](int d) { return kLoads * wave + d < 8; };
+  uint32_t at[kLoads];
+#pragma unroll
+  for (int d = 0; d < kLoads; ++d)
+    at[d] = (uint32_t)(of_w(d) ? min(row(d), A.n - 1 - f0) : min(row(d) - 16, A.m - 1 - t0)) * A.k + 16 * ((lane & 31) ^ (row(d) & 15));
+  const uint32_t lds0 = lds_addr(lds), sat = 4 * (uint32_t)min(t0 + lane, A.m - 1);
+  const float* ws = A.ws + (size_t)(f0 / kKB) * A.blocks;
+  const int whole = A.k / kBytes, stages = (A.blocks + kBlocks - 1) / kBlocks;
+  auto issue = [&](int s, int stage) {
+    const size_t k0 = (size_t)s * kBytes;
+#pragma unroll
+    for (int d = 0; d < kLoads; ++d) {
+      const uint8_t* src = (of_w(d) ? wsrc : xsrc) + k0;
+      if (s < whole) {
+        dma_16(src, at[d], lds0 + stage * kStage + 1024 * (kLoads * wave + d));
+      } else {  // the last stage: its values behind k are zero
+        i32x4 v{};
+        if (k0 + 16 * ((lane & 31) ^ (row(d) & 15)) < (size_t)A.k) v = *reinterpret_cast<const i32x4*>(src + at[d]);
+        *reinterpret_cast<i32x4*>(lds + stage * kStage + 1024 * (kLoads * wave + d) + 16 * lane) = v;
+      }
+    }
+#pragma unroll
+    for (int d = 0; d < kScales; ++d) {  // the blocks' token scales, then their feature scales
+      const int c = kScales * wave + d, b = min(s * kBlocks + c % kBlocks, A.blocks - 1);
+      dma_dword(c < kBlocks ? A.xs + (size_t)b * A.m : ws + b, c < kBlocks ? sat : 0, lds0 + stage * kStage + kRows * kBytes + 256 * c);
+    }
+  };
+  const int blk = wave % kBlocks, tw = wave / kBlocks * 16;
+  const int pos0 = i * kBytes + ((8 * blk + q) ^ i) * 16, pos1 = i * kBytes + ((8 * blk + q + 4) ^ i) * 16;
+  f32x4 acc{};
+#pragma unroll
+  for (int s = 0; s < kStages - 1; ++s)
+    if (s < stages) issue(s, s);
+  for (int s = 0, stage = 0; s < stages; ++s) {
+    __builtin_amdgcn_s_waitcnt(0xC07F);  // this wave's LDS reads (and writes)
+    if (s + kStages - 1 <= whole)        // (of the stages behind s, all whole ones, every load may be on its way)
+      wait_vmcnt<(kStages - 2) * (kLoads + kScales)>();
+    else
+      wait_vmcnt<0>();
+    barrier_no_fence();  // stage s is in LDS; every wave has read the one before
+    if (s + kStages - 1 < stages) issue(s + kStages - 1, stage > 0 ? stage - 1 : kStages - 1);
+    const uint8_t* st = lds + stage * kStage;
+    auto codes = [&](int row) {
+      return join(*reinterpret_cast<const i32x4*>(st + row * kBytes + pos0), *reinterpret_cast<const i32x4*>(st + row * kBytes + pos1));
+    };
+    if (s * kBlocks + blk < A.blocks) {
+      const float* sc = reinterpret_cast<const float*>(st + kRows * kBytes);
+      Operand<kExact> w, x;
+      w.set(codes(0));
+      x.set(codes(16 + tw));
+      const float c = sc[64 * blk + tw + i] * sc[64 * (kBlocks + blk)];
+      const f32x4 y = block_sum(w, x);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[e] = fmaf(y[e], c, acc[e]);
+    }
+    stage = stage + 1 < kStages ? stage + 1 : 0;
+  }
+  __syncthreads();  // every wave is done with the stages
+  f32x4* sums = reinterpret_cast<f32x4*>(lds);
+  sums[wave * 64 + lane] = acc;
+  __syncthreads();
+  if (wave < kTT / 16) {
+    f32x4 y = sums[wave * kBlocks * 64 + lane];
+#pragma unroll
+    for (int c = 1; c < kBlocks; ++c) y += sums[(wave * kBlocks + c) * 64 + lane];
+    store4(A, t0 + 16 * wave + i, f0 + 4 * q, y);
+  }
 }
 
+// ---- many tokens ---------------------------------------------------------------
 // Keeps the computation of v above what follows.
 template <class V>
 __device__ inline void pin(V& v) {
@@ -255,10 +268,10 @@ __device__ inline void pin(V& v) {
 template <bool kExact, int kTF, int kTT, int kWF, int kWT, int kStages>
 __global__ __launch_bounds__(64 * kWF * kWT) void linear_tile_kernel(LinearArgs A) {
   constexpr int kWaves = kWF * kWT, kRows = kTF + kTT, kLoads = kRows / 8 / kWaves;
-  constexpr int kF = kTF / kWF, kT = kTT / kWT, kA = kF / 16, kB = kT / 16, kProducts = kA * kB, kSlices = kTT / 64, kSlicesF = (kTF + 127) / 128;
+  constexpr int kF = kTF / kWF, kT = kTT / kWT, kA = kF / 16, kB = kT / 16, kProducts = kA * kB, kSlices = (kTT + 63) / 64, kSlicesF = (kTF + 127) / 128;
   constexpr int kStage = kRows * kKB + kWaves * 256;
-  static_assert(kRows % (8 * kWaves) == 0 && kTF % (8 * kLoads) == 0, "a wave's rows are of one operand");
-  static_assert(128 % kF == 0 && kWaves >= kSlices + kSlicesF, "a wave's features share their scale");
+  static_assert(kRows % (8 * kWaves) == 0 && kTF % 8 == 0, "a load's rows are of one operand");
+  static_assert(128 % kF == 0 && kA >= 2 && kWaves >= kSlices + kSlicesF, "a wave's features share their scale");
   static_assert(kWaves * kF * kT * 2 <= kStages * kStage, "the outputs in bf16 go through LDS");
   __shared__ __attribute__((aligned(1024))) uint8_t lds[kStages * kStage];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
@@ -272,13 +285,13 @@ __global__ __launch_bounds__(64 * kWF * kWT) void linear_tile_kernel(LinearArgs 
 
   // this lane's load sources, relative to its operand's first row of the tile:
   // rows past the end re-read the last one (never stored)
-  const bool of_w = kLoads * 8 * wave < kTF;
-  const uint8_t* src = of_w ? A.w + (size_t)f0 * A.k : A.x + (size_t)t0 * A.k;
+  const uint8_t *wsrc = A.w + (size_t)f0 * A.k, *xsrc = A.x + (size_t)t0 * A.k;
+  auto of_w = [&](int d) { return 8 * (kLoads * wave + d) < kTF; };  // (8 rows a load)
   uint32_t at[kLoads];
 #pragma unroll
   for (int d = 0; d < kLoads; ++d) {
     const int r = 8 * (kLoads * wave + d) + (lane >> 3), c = (lane & 7) ^ ((r >> 1) & 7);
-    at[d] = (uint32_t)(of_w ? min(r, A.n - 1 - f0) : min(r - kTF, A.m - 1 - t0)) * A.k + 16 * c;
+    at[d] = (uint32_t)(of_w(d) ? min(r, A.n - 1 - f0) : min(r - kTF, A.m - 1 - t0)) * A.k + 16 * c;
   }
   // scales: 64 tokens a wave, then 128 features a wave
   const bool s_of_x = wave < kSlices;
@@ -291,19 +304,25 @@ __global__ __launch_bounds__(64 * kWF * kWT) void linear_tile_kernel(LinearArgs 
   const int whole = A.k / kKB;
   auto issue = [&](int b, int stage) {  // blocks in order: the sources move along
     if (b < whole) {
-      dma_rows<kLoads>(src, at, dst + stage * kStage);
+      if constexpr (kTF % (8 * kLoads) == 0) {
+        dma_rows<kLoads>(of_w(0) ? wsrc : xsrc, at, dst + stage * kStage);
+      } else {
+#pragma unroll
+        for (int d = 0; d < kLoads; ++d) dma_16(of_w(d) ? wsrc : xsrc, at[d], dst + stage * kStage + 1024 * d);
+      }
     } else {  // the last block: its values behind k are zero
       const int chunks = (A.k - whole * kKB) / 16;
 #pragma unroll
       for (int d = 0; d < kLoads; ++d) {
         const int r = 8 * (kLoads * wave + d) + (lane >> 3), cc = (lane & 7) ^ ((r >> 1) & 7);
         i32x4 v{};
-        if (cc < chunks) v = *reinterpret_cast<const i32x4*>(src + at[d]);
+        if (cc < chunks) v = *reinterpret_cast<const i32x4*>((of_w(d) ? wsrc : xsrc) + at[d]);
         *reinterpret_cast<i32x4*>(lds + stage * kStage + r * kKB + (lane & 7) * 16) = v;
       }
     }
     dma_dword(ssrc, sat, sdst + stage * kStage);
-    src += kKB;
+    wsrc += kKB;
+    xsrc += kKB;
     ssrc += snext;
   };
 
@@ -446,8 +465,8 @@ extern "C" gambit_status gambit_linear_fp8(int32_t m, int32_t n, int32_t k, cons
   A.blocks = (k + kKB - 1) / kKB;
   A.f32 = out_dtype == GAMBIT_F32;
   hipStream_t s = static_cast<hipStream_t>(stream);
-  auto skinny = [&](auto kernel, int tokens, int features) {
-    hipLaunchKernelGGL(kernel, dim3((n + features - 1) / features, (m + tokens - 1) / tokens), dim3(64 * kSkinnyWaves), 0, s, A);
+  auto split = [&](auto kernel, int tokens) {
+    hipLaunchKernelGGL(kernel, dim3((n + 15) / 16, (m + tokens - 1) / tokens), dim3(tokens == 32 ? 512 : 256), 0, s, A);
   };
   auto tile = [&](auto kernel, int features, int tokens, int threads) {
     A.tiles_f = (n + features - 1) / features;
@@ -457,15 +476,20 @@ extern "C" gambit_status gambit_linear_fp8(int32_t m, int32_t n, int32_t k, cons
   auto tiles = [&](int side) { return (int64_t)((n + side - 1) / side) * ((m + side - 1) / side); };
   auto choose = [&](auto exact) {
     constexpr bool kExact = decltype(exact)::value;
-    const bool wide = n >= 32 * 512;
-    if (m <= 16)
-      wide ? skinny(linear_skinny_kernel<kExact, 1, 2>, 16, 32) : skinny(linear_skinny_kernel<kExact, 1, 1>, 16, 16);
-    else if (m <= 32)
-      wide ? skinny(linear_skinny_kernel<kExact, 2, 2>, 32, 32) : skinny(linear_skinny_kernel<kExact, 2, 1>, 32, 16);
+    const int64_t groups = (n + 15) / 16;
+    // Few tokens: sixteen features a workgroup while 128 of them would leave CUs without
+    // one (k 4096, us, sixteen / 128: 64 tokens, 6144 features 10.7 / 15.2, 12288 20.1 /
+    // 15.7; 32 tokens, 12288 11.7 / 15.6, 24576 20.9 / 16.7; 8 tokens, fp32, 151936
+    // 123 / 140).  Up to sixteen tokens, two stages let four workgroups share a CU, four
+    // stages two (us, two / four: 768 workgroups 8.2 / 11.8, 256 of k 12288 14.8 / 12.3).
+    if (m <= 16 && groups > 512)
+      split(linear_split_kernel<kExact, 16, 2>, 16);
+    else if (m <= 16)
+      split(linear_split_kernel<kExact, 16, 4>, 16);
+    else if (m <= 128 && n < (m <= 32 ? 16384 : 8192))
+      split(linear_split_kernel<kExact, 32, 3>, 32);
     else if (m <= 64)
-      wide ? skinny(linear_skinny_kernel<kExact, 4, 2>, 64, 32) : skinny(linear_skinny_kernel<kExact, 4, 1>, 64, 16);
-    else if (m <= 128 && !wide)
-      skinny(linear_skinny_kernel<kExact, 8, 1>, 128, 16);
+      tile(linear_tile_kernel<kExact, 128, 64, 4, 2, 3>, 128, 64, 512);
     else if constexpr (kExact)
       tile(linear_tile_kernel<true, 128, 128, 2, 4, 2>, 128, 128, 512);
     // Tiles of 256 x 256 re-read least, but need one for each of the 256 CUs.  Of the
