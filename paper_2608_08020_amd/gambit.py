@@ -209,6 +209,8 @@ def _spec(t: torch.Tensor, dtype=None, shape=None, what: str = "tensor"):
 
 def _dev(t: torch.Tensor, dtype=None, shape=None, what: str = "tensor"):
     """Pointer of a contiguous device tensor (checked as by _spec)."""
+    if type(t) is torch.Tensor and t.is_cuda and t.dtype is dtype and t.shape == shape and t.is_contiguous():
+        return t.data_ptr()  # (the common argument, sooner)
     _spec(t, dtype, shape, what)
     if not t.is_cuda:
         raise ValueError(f"{what}: expected a device tensor")
@@ -332,14 +334,31 @@ def _outer(t: torch.Tensor, i: int) -> int:
     return t.stride(i) if t.shape[i] > 1 else 0
 
 
-def _here(t: torch.Tensor, *others):
-    """All of a call's tensors are the current device's."""
-    d = t.get_device()
-    if d != torch.cuda.current_device():
-        raise ValueError(f"the tensors are on device {d}, device {torch.cuda.current_device()} is current")
+def _here(stream, t: torch.Tensor, *others):
+    """The stream's handle for a call whose tensors are all the current device's."""
+    d, current = t.get_device(), torch.cuda.current_device()
+    if d != current:
+        raise ValueError(f"the tensors are on device {d}, device {current} is current")
     for o in others:
         if o is not None and o.get_device() != d:
             raise ValueError(f"tensors on devices {d} and {o.get_device()}")
+    return torch._C._cuda_getCurrentRawStream(d) if stream is None else stream.cuda_stream
+
+
+def _rows(t: torch.Tensor, shape, what: str):
+    """Address and type code of a dense bf16 or fp32 tensor."""
+    if isinstance(t, torch.Tensor) and t.dtype is torch.float32:
+        return _dev(t, torch.float32, shape, what), 1
+    return _dev(t, torch.bfloat16, shape, what), 0
+
+
+def _scales(out_scale, dim: int, n: int, device):
+    """The scales of E4M3 rows, one for 128 values: given ones or new ones, and their address."""
+    shape = (-(-dim // 128), n)
+    if out_scale is None:
+        out_scale = torch.empty(shape, dtype=torch.float32, device=device)
+        return out_scale, out_scale.data_ptr()
+    return out_scale, _dev(out_scale, torch.float32, shape, "out_scale")
 
 
 def rms_norm(x: torch.Tensor, weight: torch.Tensor, eps: float = 1e-6, residual: torch.Tensor | None = None,
@@ -353,17 +372,19 @@ def rms_norm(x: torch.Tensor, weight: torch.Tensor, eps: float = 1e-6, residual:
     shape, dim = x.shape, x.shape[-1]
     n, heads = shape[0], shape[1] if len(shape) == 3 else 1
     xp = _strided(x, FLOAT_CODES, None, "x")
+    if out is not None:
+        out_dtype = out.dtype
+    if out_dtype not in ROW_CODES:
+        raise ValueError(f"out: expected dtype {tuple(ROW_CODES)}, got {out_dtype}")
     if out is None:
         out = torch.empty(shape, dtype=out_dtype, device=x.device)
-    if out.dtype not in ROW_CODES:
-        raise ValueError(f"out: expected dtype {tuple(ROW_CODES)}, got {out.dtype}")
-    op = _dev(out, None, shape, "out")
-    wp = _dev(weight, (torch.bfloat16, torch.float32), (dim,), "weight")
-    fp8, sp = out.dtype is E4M3, None
+        op = out.data_ptr()
+    else:
+        op = _dev(out, out_dtype, shape, "out")
+    wp, wd = _rows(weight, (dim,), "weight")
+    fp8, sp = out_dtype is E4M3, None
     if fp8:
-        if out_scale is None:
-            out_scale = torch.empty((-(-dim // 128), n * heads), dtype=torch.float32, device=x.device)
-        sp = _dev(out_scale, torch.float32, (-(-dim // 128), n * heads), "out_scale")
+        out_scale, sp = _scales(out_scale, dim, n * heads, x.device)
     elif out_scale is not None:
         raise ValueError("out_scale: only E4M3 rows have scales")
     rp = rop = None
@@ -371,13 +392,13 @@ def rms_norm(x: torch.Tensor, weight: torch.Tensor, eps: float = 1e-6, residual:
     if residual is not None:
         if residual_out is None:
             residual_out = residual
-        rp, rd = _dev(residual, (torch.bfloat16, torch.float32), shape, "residual"), FLOAT_CODES[residual.dtype]
-        rop = _dev(residual_out, residual.dtype, shape, "residual_out")
+        rp, rd = _rows(residual, shape, "residual")
+        rop = rp if residual_out is residual else _dev(residual_out, residual.dtype, shape, "residual_out")
     elif residual_out is not None:
         raise ValueError("residual_out: there is no residual")
-    _here(x, weight, out, out_scale, residual, residual_out)
-    st = lib().gambit_rms_norm(n, heads, dim, xp, FLOAT_CODES[x.dtype], _outer(x, 0), _outer(x, 1) if len(shape) == 3 else 0,
-                               wp, FLOAT_CODES[weight.dtype], eps, rp, rop, rd, op, ROW_CODES[out.dtype], sp, _stream(stream))
+    s = _here(stream, x, weight, out, out_scale, residual, residual_out)
+    st = lib().gambit_rms_norm(n, heads, dim, xp, FLOAT_CODES[x.dtype], _outer(x, 0), _outer(x, 1) if heads > 1 else 0,
+                               wp, wd, eps, rp, rop, rd, op, ROW_CODES[out_dtype], sp, s)
     if st != OK:
         raise GambitError(st, "rms_norm")
     return (out, out_scale) if fp8 else out
@@ -393,12 +414,12 @@ def quantize(x: torch.Tensor, gated: bool = False, out: torch.Tensor | None = No
     xp = _strided(x, FLOAT_CODES, None, "x")
     if out is None:
         out = torch.empty((n, dim), dtype=E4M3, device=x.device)
-    if out_scale is None:
-        out_scale = torch.empty((-(-dim // 128), n), dtype=torch.float32, device=x.device)
-    op = _dev(out, E4M3, (n, dim), "out")
-    sp = _dev(out_scale, torch.float32, (-(-dim // 128), n), "out_scale")
-    _here(x, out, out_scale)
-    st = lib().gambit_quantize(n, dim, xp, FLOAT_CODES[x.dtype], _outer(x, 0), gated, op, sp, _stream(stream))
+        op = out.data_ptr()
+    else:
+        op = _dev(out, E4M3, (n, dim), "out")
+    out_scale, sp = _scales(out_scale, dim, n, x.device)
+    s = _here(stream, x, out, out_scale)
+    st = lib().gambit_quantize(n, dim, xp, FLOAT_CODES[x.dtype], _outer(x, 0), gated, op, sp, s)
     if st != OK:
         raise GambitError(st, "quantize")
     return out, out_scale
@@ -413,16 +434,20 @@ def linear_fp8(x: torch.Tensor, x_scale: torch.Tensor, w: torch.Tensor, w_scale:
     m, k = x.shape
     n = w.shape[0]
     blocks = -(-k // 128)
-    xp, wp = _dev(x, E4M3, None, "x"), _dev(w, E4M3, (n, k), "w")
+    xp, wp = _dev(x, E4M3, x.shape, "x"), _dev(w, E4M3, (n, k), "w")
     xsp = _dev(x_scale, torch.float32, (blocks, m), "x_scale")
     wsp = _dev(w_scale, torch.float32, (-(-n // 128), blocks), "w_scale")
+    if out is not None:
+        out_dtype = out.dtype
+    if out_dtype not in OUT_CODES:
+        raise ValueError(f"out: expected dtype {tuple(OUT_CODES)}, got {out_dtype}")
     if out is None:
         out = torch.empty((m, n), dtype=out_dtype, device=x.device)
-    if out.dtype not in OUT_CODES:
-        raise ValueError(f"out: expected dtype {tuple(OUT_CODES)}, got {out.dtype}")
-    op = _dev(out, None, (m, n), "out")
-    _here(x, x_scale, w, w_scale, out)
-    st = lib().gambit_linear_fp8(m, n, k, xp, xsp, wp, wsp, op, OUT_CODES[out.dtype], _stream(stream))
+        op = out.data_ptr()
+    else:
+        op = _dev(out, out_dtype, (m, n), "out")
+    s = _here(stream, x, x_scale, w, w_scale, out)
+    st = lib().gambit_linear_fp8(m, n, k, xp, xsp, wp, wsp, op, OUT_CODES[out_dtype], s)
     if st != OK:
         raise GambitError(st, "linear_fp8")
     return out
@@ -447,7 +472,7 @@ def rotate(q: torch.Tensor | None, k: torch.Tensor | None, positions: torch.Tens
     if q is None and k is None:
         raise ValueError("q, k: nothing to turn")
     n = (k if q is None else q).shape[0]
-    tp = _dev(table, torch.float32, None, "table")
+    tp = _dev(table, torch.float32, table.shape, "table")
     pp = _dev(positions, torch.int32, (n,), "positions")
     side = []
     for x, out, what in ((q, q_out, "q"), (k, k_out, "k")):
@@ -459,11 +484,13 @@ def rotate(q: torch.Tensor | None, k: torch.Tensor | None, positions: torch.Tens
         xp, stride = _heads(x, n, what)
         if out is None:
             out = torch.empty(x.shape, dtype=torch.bfloat16, device=x.device)
-        side.append((x.shape[1], xp, stride, out, _dev(out, torch.bfloat16, x.shape, what + "_out")))
+            op = out.data_ptr()
+        else:
+            op = _dev(out, torch.bfloat16, x.shape, what + "_out")
+        side.append((x.shape[1], xp, stride, out, op))
     (hq, qp, qs, q_out, qop), (hk, kp, ks, k_out, kop) = side
-    _here(table, q, k, positions, q_out, k_out)
-    st = lib().gambit_rotate(n, hq, hk, qp, qs, kp, ks, pp, tp, table.shape[0], table.shape[1], pairs, qop, kop,
-                             _stream(stream))
+    s = _here(stream, table, q, k, positions, q_out, k_out)
+    st = lib().gambit_rotate(n, hq, hk, qp, qs, kp, ks, pp, tp, table.shape[0], table.shape[1], pairs, qop, kop, s)
     if st != OK:
         raise GambitError(st, "rotate")
     return q_out, k_out
@@ -488,12 +515,19 @@ def sample(logits: torch.Tensor, u: torch.Tensor, temperature=1.0, top_k=0, top_
             args += [None, x]
     if out is None:
         out = torch.empty(n, dtype=torch.int32, device=logits.device)
-    op = _dev(out, torch.int32, (n,), "out")
-    _here(logits, u, out, *given)
+        op = out.data_ptr()
+    else:
+        op = _dev(out, torch.int32, (n,), "out")
+    s = _here(stream, logits, u, out, *given)
     dt = FLOAT_CODES[logits.dtype]
     size = lib().gambit_sample_workspace_size(n, vocab, dt)
-    ws = torch.empty(size, dtype=torch.uint8, device=logits.device).data_ptr() if size else None
-    st = lib().gambit_sample(n, vocab, zp, dt, _outer(logits, 0), up, *args, op, ws, size, _stream(stream))
+    wp = None
+    if size:
+        ws = torch.empty(size, dtype=torch.uint8, device=logits.device)
+        if stream is not None:  # (not reused before that stream is done with it)
+            ws.record_stream(stream)
+        wp = ws.data_ptr()
+    st = lib().gambit_sample(n, vocab, zp, dt, _outer(logits, 0), up, *args, op, wp, size, s)
     if st != OK:
         raise GambitError(st, "sample")
     return out
@@ -684,7 +718,7 @@ class Pool:
             n_rows = k.shape[0]
         if table.dim() != 2:
             raise ValueError("table: expected [n_pos][rot]")
-        tp = _dev(table, torch.float32, None, "table")
+        tp = _dev(table, torch.float32, table.shape, "table")
         (kp, ks), (vp, vs) = _heads(k, n_rows, "k"), _heads(v, n_rows, "v")
         if k.shape[1] != self.Hkv or v.shape[1] != self.Hkv:
             raise ValueError(f"k, v: expected {self.Hkv} heads, got {k.shape[1]} and {v.shape[1]}")
@@ -697,7 +731,9 @@ class Pool:
             shape = (total, self.Hq, self.D)
             if q_out is None:
                 q_out = torch.empty(shape, dtype=torch.bfloat16, device=q.device)
-            qop = _dev(q_out, torch.bfloat16, shape, "q_out")
+                qop = q_out.data_ptr()
+            else:
+                qop = _dev(q_out, torch.bfloat16, shape, "q_out")
         elif q_out is not None:
             raise ValueError("q_out: there are no queries")
         self._check(lib().gambit_kv_write_rotated(self._h, layer, ids.size, _in(ids), _in(p0), _in(nt),
