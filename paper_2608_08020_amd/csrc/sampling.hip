@@ -52,7 +52,7 @@ constexpr int kShortLoads = 2048;  // rows of no more are drawn by sample_any_ke
 struct Border {
   float top;         // the row's maximum
   int32_t bin;       // -1: nowhere in the histogram, or the row is out of range
-  float from;        // the least value of bins up to `bin`, or a little less
+  float from, to;    // the least value of `bin`, or a little less, and its largest, or a little more
   uint32_t listed;   // values in the list (beyond kList: not all are there)
   u64 above, total;  // top_k: values above the bin; top_p: their weight, and that of all
 };
@@ -61,7 +61,7 @@ struct Border {
 struct Left {
   int32_t chunks, segs, chunk_segs;
   float* most;      // [n][chunks] maximum
-  u64* weight;      // [n][chunks]
+  u64* weight;      // [n][chunks]; top_p alone: then that above the border's bin, in the row's units
   u64* bins;        // [n][chunks][kBins] counts or weights
   float* seg_most;  // [n][segs]
   u64* seg_sum;     // [n][segs]
@@ -92,7 +92,7 @@ static_assert(kOctaveBins == 8, "64ths of an octave to bins");
 
 
 // How a row is drawn.
-enum Way { kGreedy, kAll, kMinP, kTopK, kTopP, kBoth };
+enum Way { kGreedy, kAll, kMinP, kTopK, kTopP, kBoth };  // (kTopP: a min_p besides makes no other way)
 __device__ inline Way way_of(const Filter& F) {
   if (F.greedy) return kGreedy;
   if (F.use_k) return F.use_p ? kBoth : kTopK;
@@ -214,6 +214,7 @@ __global__ __launch_bounds__(kBorderThreads) void sample_border_kernel(SampleArg
   __shared__ u64 sums[kBorderThreads / 64];
   __shared__ float most[kBorderThreads / 64];
   __shared__ int32_t below[kMaxChunks];  // octaves of a chunk below the row's; 64: nothing there counts
+  __shared__ int32_t bin;
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6, r = blockIdx.x;
   const size_t first = (size_t)r * W.chunks;
   const float mine = t < W.chunks ? W.most[first + t] : -INFINITY;
@@ -225,7 +226,7 @@ __global__ __launch_bounds__(kBorderThreads) void sample_border_kernel(SampleArg
   __syncthreads();
 #pragma unroll
   for (int w = 0; w < kBorderThreads / 64; ++w) top = fmaxf(top, most[w]);
-  Border B{top, kNoBin, -FLT_MAX, 0, 0, 0};
+  Border B{top, kNoBin, -FLT_MAX, FLT_MAX, 0, 0, 0};
   const bool drawn = top > -INFINITY && way != kGreedy;
   if (drawn && !in_range(top, F.slope)) B.bin = -1;
   if (!drawn || B.bin < 0 || way == kAll || way == kMinP) {
@@ -256,12 +257,27 @@ __global__ __launch_bounds__(kBorderThreads) void sample_border_kernel(SampleArg
   if (all < want) {
     B.bin = -1;
     if (t == 0) W.border[r] = B;
-  } else if (before < want && before + x >= want) {
-    B.bin = t;
+    return;
+  }
+  if (before < want && before + x >= want) {
+    bin = B.bin = t;
     B.above = before;
     const float low = (float)(((double)S.e64 - 8. * (t + 1) - 1.) / 64. / F.slope);
+    const float high = (float)(((double)S.e64 - 8. * t + 1.) / 64. / F.slope);
     B.from = low - fabsf(low) * 0x1p-20f;
+    B.to = high + fabsf(high) * 0x1p-20f;
     W.border[r] = B;
+  }
+  if (way != kTopP) return;
+  __syncthreads();
+  for (int c = wave; c < W.chunks; c += kBorderThreads / 64) {
+    const int down = below[c], bins = bin - kOctaveBins * down;
+    u64 y = 0;
+#pragma unroll
+    for (int i = 0; i < kBins / 64; ++i)
+      if (64 * i + lane < bins) y += W.bins[(first + c) * kBins + 64 * i + lane];
+    y = wave_total(y);
+    if (lane == 0) W.weight[first + c] = y >> min(63, down);
   }
 }
 
@@ -291,6 +307,7 @@ __global__ __launch_bounds__(kThreads) void sample_gather_kernel(SampleArgs A, L
     return m >= from && (b < kNoBin || likely(m));
   };
   C.read(wanted);
+  const bool sums = way != kTopP || least > -INFINITY;  // (else the chunks' weights are known)
   u64 flags = 0;  // of the thread's values: listed
 #pragma unroll
   for (int i = 0; i < kLoads; ++i) {
@@ -300,18 +317,18 @@ __global__ __launch_bounds__(kThreads) void sample_gather_kernel(SampleArgs A, L
 #pragma unroll
       for (int k = 0; k < R::kPer; ++k) {
         const float z = C.z[i][k];
-        if (!(z >= from)) continue;
+        if (!(z >= from) || (!sums && z > B.to)) continue;
         double rest;
         const int q = S.at(z, &rest), at = bin_of(q);
         if (at > b) continue;
         if (at == b || way == kBoth)
           flags |= 1ull << (i * R::kPer + k);
-        else if (likely(z))
+        else if (sums && likely(z))
           sum += weight_of(q, rest, powers);
       }
-      sum = wave_total(sum);
+      if (sums) sum = wave_total(sum);
     }
-    if (lane == 0) W.seg_sum[(size_t)r * W.segs + C.seg(i)] = sum;
+    if (lane == 0 && sums) W.seg_sum[(size_t)r * W.segs + C.seg(i)] = sum;
   }
   if (b == kNoBin) return;
   // the values' places in the row's list: one claim a workgroup
@@ -343,9 +360,11 @@ struct RowShared {
   u64 list[kList];  // ~key, index: ascending is likeliest first
   u64 segs[kSegs + 1];
   double powers[64];
+  u64 chunks[kMaxChunks];
+  u64 part[kThreads];  // sums of the list's values by key, then the values that one of them counts
   u64 sums[kWaves];
   u64 rest;
-  uint32_t found, token;
+  uint32_t found, token, lo, hi, parted;
 };
 #define L lds_as<RowShared>()
 
@@ -388,6 +407,84 @@ struct RowDraw {
   __device__ u64 scan(u64 x, u64* all) const { return block_before<kThreads>(x, L.sums, all); }
   __device__ u64 weight(float z) const { return weight_at(z, S, L.powers); }
   __device__ bool likely(float z) const { return ((double)z - (double)top) * S.slope >= least; }
+
+  // The cut in the list by one sum: by count its value k - above, by mass the one
+  // that takes the weight from `above` to p of the total.  The list is parted by key
+  // into kThreads ranges; the range that the sum crosses in is ranked.  False: it has
+  // too many values.
+  __device__ __forceinline__ bool cut_part(int n, const Filter& F, Way way, u64 above, u64 total, Cut* cut) {
+    if (t == 0) {
+      L.lo = ~0u;
+      L.hi = 0;
+      L.parted = 0;
+      L.found = ~0u;
+    }
+    L.part[t] = 0;
+    __syncthreads();
+    uint32_t lo = ~0u, hi = 0;
+    for (int i = t; i < n; i += kThreads) {
+      const uint32_t key = (uint32_t)(L.list[i] >> 32);
+      lo = min(lo, key);
+      hi = max(hi, key);
+    }
+#pragma unroll
+    for (int o = 32; o; o >>= 1) {
+      lo = min(lo, (uint32_t)__shfl_xor((int)lo, o));
+      hi = max(hi, (uint32_t)__shfl_xor((int)hi, o));
+    }
+    if (lane == 0) {
+      atomicMin(&L.lo, lo);
+      atomicMax(&L.hi, hi);
+    }
+    __syncthreads();
+    lo = L.lo;
+    hi = L.hi;
+    const int shift = max(0, 32 - __builtin_clz((hi - lo) | 1u) - 9);  // (hi - lo) >> shift < 512
+    static_assert(kThreads == 512, "");
+    auto amount = [&](u64 x) { return way == kTopK ? 1 : weight(entry_value(x)); };
+    for (int i = t; i < n; i += kThreads) {
+      const u64 x = L.list[i];
+      atomicAdd(&L.part[((uint32_t)(x >> 32) - lo) >> shift], amount(x));
+    }
+    __syncthreads();
+    const u64 want = max(way == kTopK ? (u64)F.k : (u64)ceil((double)F.p * (double)total), above + 1);
+    const u64 x = L.part[t];
+    u64 all;
+    const u64 before = above + scan(x, &all);
+    // (a bin's weight, shifted as a whole, may be a few units off its values': then the cut is the last one)
+    if (above + all >= want ? before < want && before + x >= want : t == (int)((hi - lo) >> shift)) {
+      L.found = t;
+      L.rest = before;
+    }
+    __syncthreads();
+    const uint32_t at = L.found;
+    const u64 from = L.rest;
+    for (int i = t; i < n; i += kThreads) {
+      const u64 e = L.list[i];
+      if (((uint32_t)(e >> 32) - lo) >> shift != at) continue;
+      const uint32_t to = atomicAdd(&L.parted, 1u);
+      if (to < (uint32_t)kThreads) L.part[to] = e;
+    }
+    __syncthreads();
+    const int m = (int)L.parted;
+    if (m > kThreads) return false;
+    // by rank, a value a thread: its place among them, and what comes before it
+    const u64 mine = t < m ? L.part[t] : ~0ull;
+    int rank = 0;
+    for (int i = 0; i < m; ++i) rank += L.part[i] < mine;
+    __syncthreads();
+    if (t < m) L.part[rank] = mine;
+    if (t == 0) L.found = m - 1;
+    __syncthreads();
+    const u64 w = t < m ? amount(L.part[t]) : 0;
+    u64 some;
+    const u64 front = from + scan(w, &some);
+    if (t < m && front < want && front + w >= want) L.found = t;
+    __syncthreads();
+    const u64 e = L.part[L.found];
+    *cut = {~(uint32_t)(e >> 32), (uint32_t)e};
+    return true;
+  }
 
   // The cut in the sorted list: by count its value k - above; by mass the one that
   // takes the weight from `above` to `want`; with both, the weight of the first k
@@ -485,22 +582,43 @@ struct RowDraw {
   // The row's token; -2: to be drawn the other way.
   __device__ __forceinline__ int run(const Filter& F, double u, const Left& W, const Border& B, int r) {
     const Way way = way_of(F);
+    const bool by_chunk = way == kAll || (way == kTopP && !(least > -INFINITY));
     Cut cut{0, ~0u};
     u64 target = ~0ull;
     for (int s = t; s < kSegs + 1; s += kThreads)
-      L.segs[s] = s < W.segs && way != kAll && way != kBoth ? W.seg_sum[(size_t)r * W.segs + s] : 0;
-    if (way == kAll) {  // the chunk that the token is in, then its segments
-      u64 weight_c = 0, total;
-      if (t < W.chunks) {
-        const size_t at = (size_t)r * W.chunks + t;
-        const float most = W.most[at];
-        if (most > -INFINITY) weight_c = W.weight[at] >> min(63, (S.e64 - Scale(S.slope, most).e64) / 64);
+      L.segs[s] = s < W.segs && !by_chunk && way != kBoth ? W.seg_sum[(size_t)r * W.segs + s] : 0;
+    if (by_chunk && t < W.chunks) {
+      const size_t at = (size_t)r * W.chunks + t;
+      const float most = W.most[at];
+      u64 x = 0;
+      if (most > -INFINITY) x = way == kTopP ? W.weight[at] : W.weight[at] >> min(63, (S.e64 - Scale(S.slope, most).e64) / 64);
+      L.chunks[t] = x;
+    }
+    if (way == kTopK || way == kTopP || way == kBoth) {
+      if (B.listed > (uint32_t)kList || B.listed == 0) return -2;
+      const int n = (int)B.listed;
+      for (int i = t; i < n; i += kThreads) L.list[i] = W.list[(size_t)r * kList + i];
+      __syncthreads();
+      if (way == kBoth || !cut_part(n, F, way, B.above, B.total, &cut)) {
+        sort_list(n);
+        cut = cut_list(n, F, way, B.above, B.total);
       }
-      const u64 before = scan(weight_c, &total);
+      for (int i = t; i < n; i += kThreads) {
+        const u64 x = L.list[i];
+        const float z = entry_value(x);
+        const int index = (int)(uint32_t)x, seg = ((index + row.lead) / kPer) >> 6;
+        if (cut.holds(z, index) && likely(z)) atomicAdd(by_chunk ? &L.chunks[seg / W.chunk_segs] : &L.segs[seg], weight(z));
+      }
+    }
+    if (by_chunk) {  // the chunk that the token is in, then its segments
+      __syncthreads();
+      const u64 x = t < W.chunks ? L.chunks[t] : 0;
+      u64 total;
+      const u64 before = scan(x, &total);
       if (total == 0) return -2;
       target = (u64)fmin(u * (double)total, 0x1p63);
       target = target < total ? target : total - 1;
-      if (before <= target && target < before + weight_c) {
+      if (before <= target && target < before + x) {
         L.found = t;
         L.rest = target - before;
       }
@@ -513,22 +631,10 @@ struct RowDraw {
         row.get(s * 64 + lane, z);
         u64 sum = 0;
 #pragma unroll
-        for (int k = 0; k < kPer; ++k) sum += weight(z[k]);
+        for (int k = 0; k < kPer; ++k)
+          if (way == kAll || cut.holds(z[k], row.index(s * 64 + lane, k))) sum += weight(z[k]);
         sum = wave_total(sum);
         if (lane == 0) L.segs[s] = sum;
-      }
-    } else if (way != kMinP) {
-      if (B.listed > (uint32_t)kList) return -2;
-      const int n = (int)B.listed;
-      for (int i = t; i < n; i += kThreads) L.list[i] = W.list[(size_t)r * kList + i];
-      __syncthreads();
-      sort_list(n);
-      cut = cut_list(n, F, way, B.above, B.total);
-      for (int i = t; i < n; i += kThreads) {
-        const u64 x = L.list[i];
-        const float z = entry_value(x);
-        const int index = (int)(uint32_t)x;
-        if (cut.holds(z, index) && likely(z)) atomicAdd(&L.segs[((index + row.lead) / kPer) >> 6], weight(z));
       }
     }
     __syncthreads();
@@ -537,7 +643,7 @@ struct RowDraw {
 };
 
 template <bool kF32>
-__global__ __launch_bounds__(kThreads) void sample_rows_kernel(SampleArgs A, Left W) {
+__global__ __launch_bounds__(kThreads, 4) void sample_rows_kernel(SampleArgs A, Left W) {
   typedef Row<kF32> R;
   const int r = blockIdx.x, t = threadIdx.x, lane = t & 63;
   const R row(A.z, r * A.stride, A.vocab);
@@ -640,7 +746,6 @@ hipError_t launch(const SampleArgs& A, const Cuts& C, uint8_t* ws, int n, hipStr
                reinterpret_cast<u64*>(ws + C.seg_sum), reinterpret_cast<Border*>(ws + C.border),
                reinterpret_cast<u64*>(ws + C.list)};
   switch (C.loads) {
-    case 8: return launch_chunks<kF32, 8>(A, W, n, s);
     case 4: return launch_chunks<kF32, 4>(A, W, n, s);
     case 2: return launch_chunks<kF32, 2>(A, W, n, s);
     default: return launch_chunks<kF32, 1>(A, W, n, s);
