@@ -408,11 +408,11 @@ struct RowDraw {
   __device__ u64 weight(float z) const { return weight_at(z, S, L.powers); }
   __device__ bool likely(float z) const { return ((double)z - (double)top) * S.slope >= least; }
 
-  // The cut in the list by one sum: by count its value k - above, by mass the one
-  // that takes the weight from `above` to p of the total.  The list is parted by key
-  // into kThreads ranges; the range that the sum crosses in is ranked.  False: it has
-  // too many values.
-  __device__ __forceinline__ bool cut_part(int n, const Filter& F, Way way, u64 above, u64 total, Cut* cut) {
+  // The entry, of the list's up to `limit`, that takes the count (or the weight) from
+  // `above` to `want`.  The list is parted by key into kThreads ranges; the range that
+  // the sum crosses in is ranked.  False: it has too many values.
+  __device__ __forceinline__ bool cut_part(int n, u64 limit, bool count, u64 above, u64 want, u64* cut) {
+    __syncthreads();  // (a cut before this one has been read)
     if (t == 0) {
       L.lo = ~0u;
       L.hi = 0;
@@ -423,6 +423,7 @@ struct RowDraw {
     __syncthreads();
     uint32_t lo = ~0u, hi = 0;
     for (int i = t; i < n; i += kThreads) {
+      if (L.list[i] > limit) continue;
       const uint32_t key = (uint32_t)(L.list[i] >> 32);
       lo = min(lo, key);
       hi = max(hi, key);
@@ -441,13 +442,13 @@ struct RowDraw {
     hi = L.hi;
     const int shift = max(0, 32 - __builtin_clz((hi - lo) | 1u) - 9);  // (hi - lo) >> shift < 512
     static_assert(kThreads == 512, "");
-    auto amount = [&](u64 x) { return way == kTopK ? 1 : weight(entry_value(x)); };
+    auto amount = [&](u64 x) { return count ? 1 : weight(entry_value(x)); };
     for (int i = t; i < n; i += kThreads) {
       const u64 x = L.list[i];
-      atomicAdd(&L.part[((uint32_t)(x >> 32) - lo) >> shift], amount(x));
+      if (x <= limit) atomicAdd(&L.part[((uint32_t)(x >> 32) - lo) >> shift], amount(x));
     }
     __syncthreads();
-    const u64 want = max(way == kTopK ? (u64)F.k : (u64)ceil((double)F.p * (double)total), above + 1);
+    want = max(want, above + 1);
     const u64 x = L.part[t];
     u64 all;
     const u64 before = above + scan(x, &all);
@@ -461,7 +462,7 @@ struct RowDraw {
     const u64 from = L.rest;
     for (int i = t; i < n; i += kThreads) {
       const u64 e = L.list[i];
-      if (((uint32_t)(e >> 32) - lo) >> shift != at) continue;
+      if (e > limit || ((uint32_t)(e >> 32) - lo) >> shift != at) continue;
       const uint32_t to = atomicAdd(&L.parted, 1u);
       if (to < (uint32_t)kThreads) L.part[to] = e;
     }
@@ -481,7 +482,21 @@ struct RowDraw {
     const u64 front = from + scan(w, &some);
     if (t < m && front < want && front + w >= want) L.found = t;
     __syncthreads();
-    const u64 e = L.part[L.found];
+    *cut = L.part[L.found];
+    return true;
+  }
+  // The row's cut.  (A weight reaches p of a whole at one unit at least.)
+  __device__ __forceinline__ bool cut_parts(int n, const Filter& F, Way way, u64 above, u64 total, Cut* cut) {
+    u64 e = ~0ull;
+    if (way != kTopP && !cut_part(n, ~0ull, true, way == kBoth ? 0 : above, F.k, &e)) return false;
+    if (way == kBoth) {  // the weight of the first k is what p is a share of
+      u64 x = 0;
+      for (int i = t; i < n; i += kThreads)
+        if (L.list[i] <= e) x += weight(entry_value(L.list[i]));
+      scan(x, &total);
+      above = 0;
+    }
+    if (way != kTopK && !cut_part(n, e, false, above, max((u64)ceil((double)F.p * (double)total), (u64)1), &e)) return false;
     *cut = {~(uint32_t)(e >> 32), (uint32_t)e};
     return true;
   }
@@ -599,7 +614,7 @@ struct RowDraw {
       const int n = (int)B.listed;
       for (int i = t; i < n; i += kThreads) L.list[i] = W.list[(size_t)r * kList + i];
       __syncthreads();
-      if (way == kBoth || !cut_part(n, F, way, B.above, B.total, &cut)) {
+      if (!cut_parts(n, F, way, B.above, B.total, &cut)) {
         sort_list(n);
         cut = cut_list(n, F, way, B.above, B.total);
       }
@@ -694,12 +709,15 @@ __global__ __launch_bounds__(kThreads) void sample_any_kernel(SampleArgs A) {
   if (threadIdx.x == 0) A.out[r] = token;
 }
 
+constexpr int kRowsAtOnce = 4096;  // rows of one set of launches: the workspace has room for these
+
 // How a call's rows are cut, and what its workspace holds.
 struct Cuts {
   int loads = 0;  // of a chunk's thread; 0: no chunks
   int chunks = 0, segs = 0;
   size_t weight, bins, seg_most, seg_sum, border, list, bytes = 0;
   Cuts(int64_t n, int vocab, bool f32) {
+    n = std::min<int64_t>(n, kRowsAtOnce);
     const int per = f32 ? 4 : 8, most = (vocab + 2 * (per - 1)) / per;  // a row's loads, wherever it begins
     if (most <= kShortLoads) return;
     segs = (most + 63) / 64;
@@ -745,11 +763,26 @@ hipError_t launch(const SampleArgs& A, const Cuts& C, uint8_t* ws, int n, hipStr
                reinterpret_cast<u64*>(ws + C.bins), reinterpret_cast<float*>(ws + C.seg_most),
                reinterpret_cast<u64*>(ws + C.seg_sum), reinterpret_cast<Border*>(ws + C.border),
                reinterpret_cast<u64*>(ws + C.list)};
-  switch (C.loads) {
-    case 4: return launch_chunks<kF32, 4>(A, W, n, s);
-    case 2: return launch_chunks<kF32, 2>(A, W, n, s);
-    default: return launch_chunks<kF32, 1>(A, W, n, s);
+  auto some = [&](const SampleArgs& B, int rows) {
+    switch (C.loads) {
+      case 4: return launch_chunks<kF32, 4>(B, W, rows, s);
+      case 2: return launch_chunks<kF32, 2>(B, W, rows, s);
+      default: return launch_chunks<kF32, 1>(B, W, rows, s);
+    }
+  };
+  for (int r = 0; r < n; r += kRowsAtOnce) {
+    SampleArgs B = A;
+    B.z = static_cast<const uint8_t*>(A.z) + (size_t)r * A.stride * (kF32 ? 4 : 2);
+    auto later = [&](auto*& p) { p = p ? p + r : p; };
+    later(B.u);
+    later(B.temperature);
+    later(B.top_k);
+    later(B.top_p);
+    later(B.min_p);
+    later(B.out);
+    if (hipError_t e = some(B, std::min(n - r, kRowsAtOnce)); e != hipSuccess) return e;
   }
+  return hipSuccess;
 }
 
 bool sizes_ok(int32_t n, int32_t vocab, int32_t dtype) {
