@@ -1,7 +1,7 @@
-// Host side of the packed-token calls: layer writes (gambit_kv_write_layer),
-// prompt attention (gambit_prompt_attn) and draft-tree attention
-// (gambit_tree_attn), rotated writes (gambit_kv_write_rotated) - validation against the host mirror and the plans that
-// their kernels read.
+// Host side of the packed-token calls: layer writes (gambit_kv_write_layer, and
+// gambit_kv_write_rotated with rotated keys), prompt attention
+// (gambit_prompt_attn) and draft-tree attention (gambit_tree_attn) -
+// validation against the host mirror and the plans that their kernels read.
 //
 // A call's plan depends on what it lists and on the mirror alone, so the
 // layers of a step, which list the same, share one: it is made and uploaded

@@ -115,3 +115,21 @@ def test_the_oracle_draws_as_described():
     assert layer.draw(z, 0.5, top_p=0.3) == 4 and layer.draw(z, 0.0, top_p=w[4] / w.sum() + 1e-9) == 1
     assert layer.draw(z, 0.0, min_p=0.9) == 4 and layer.draw(z, 0.0, temperature=0.0) == 4
     assert layer.draw([math.nan, -math.inf], 0.3) == -1
+
+
+def test_tensors_of_another_device_are_refused(monkeypatch):
+    class On:
+        def __init__(self, d):
+            self.d = d
+
+        def get_device(self):
+            return self.d
+
+    class Stream:
+        cuda_stream = 77
+
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    assert g._here(Stream, On(1), None, On(1)) == 77
+    for tensors in ([On(0)], [On(0), On(0)], [On(1), On(0)], [On(1), None, On(-1)]):
+        with pytest.raises(ValueError, match="device"):
+            g._here(Stream, *tensors)
