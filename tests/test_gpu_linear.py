@@ -98,3 +98,38 @@ def test_after_quantize():
     x, xs = g.quantize(v)
     _, _, w, ws = _inputs(1, 200, 400)
     _check(g.linear_fp8(x, xs, w, ws, out_dtype=torch.float32), x, xs, w, ws)
+
+
+@pytest.mark.parametrize("m,n,k", [(8, 8193, 144), (16, 8224, 1040), (17, 16383, 528), (32, 16384, 272), (33, 8191, 656), (64, 8192, 400), (128, 8188, 144), (129, 8191, 272),
+                                   (1300, 4096, 272), (1300, 4099, 400), (4096, 4096, 128), (4100, 4103, 272), (4090, 4104, 656)])
+def test_where_one_kernel_ends_and_the_next_begins(m, n, k):
+    args = _inputs(m, n, k, 3)
+    out = g.linear_fp8(*args)
+    gen = torch.Generator().manual_seed(2)
+    rows = torch.cat([torch.randperm(m, generator=gen)[:40], torch.tensor([0, m - 1])]).to(DEV)
+    x, xs, w, ws = args
+    _check(out[rows], x[rows], xs[:, rows], w, ws)
+    if m > 64:  # every row, in some features
+        at = (n - 1) // 128 * 128
+        _check(out[:, at:], x, xs, w[at:], ws[at // 128:])
+
+
+@pytest.mark.parametrize("m", [1, 9, 16, 40])
+@pytest.mark.parametrize("k", [16, 496, 512, 528, 1536, 2064, 4096, 6160])
+def test_stages_of_k(m, k):
+    for n in (72, 8320):
+        args = _inputs(m, n, k, 5)
+        for dtype in (torch.bfloat16, torch.float32):
+            _check(g.linear_fp8(*args, out_dtype=dtype), *args)
+
+
+@pytest.mark.parametrize("m,n", [(3, 40), (40, 130), (50, 16400), (300, 260), (1300, 4096), (4096, 4104)])
+def test_nothing_behind_the_outputs_is_written(m, n):
+    args = _inputs(m, n, 272, 6)
+    for dtype in (torch.bfloat16, torch.float32):
+        whole = torch.full(((m + 2) * n,), 7.0, dtype=dtype, device=DEV)
+        lead = 16 // whole.element_size()
+        out = whole[lead:lead + m * n].view(m, n)
+        g.linear_fp8(*args, out=out)
+        assert (whole[:lead] == 7).all() and (whole[lead + m * n:] == 7).all()
+        assert torch.equal(out, g.linear_fp8(*args, out_dtype=dtype))

@@ -158,3 +158,36 @@ def test_no_rows_and_given_output():
     out = torch.zeros(3, dtype=torch.int32, device=DEV)
     assert g.sample(z, u, out=out) is out
     assert torch.equal(out, g.sample(z, u))
+
+
+def test_more_rows_than_one_set_of_launches_takes():
+    n, V = 4099, 16500
+    z = 2.5 * torch.randn(n, V, generator=torch.Generator(device=DEV).manual_seed(4), device=DEV).to(torch.bfloat16)
+    u = torch.rand(n, generator=torch.Generator(device=DEV).manual_seed(5), device=DEV)
+    k = torch.randint(0, 300, (n,), generator=torch.Generator(device=DEV).manual_seed(6), device=DEV, dtype=torch.int32)
+    par = dict(temperature=u + 0.3, top_p=1 - 0.5 * u, min_p=0.01 * u)
+    got = g.sample(z, u, top_k=k, **par)
+    for at in (slice(0, 5), slice(4090, 4099)):
+        assert torch.equal(got[at], g.sample(z[at], u[at].clone(), top_k=k[at].clone(), **{a: b[at].clone() for a, b in par.items()}))
+    _check(z[4095:].clone(), u[4095:].clone(), top_k=k[4095:].clone(), **{a: b[4095:].clone() for a, b in par.items()})
+
+
+@pytest.mark.parametrize("V", [8190, 8192, 8200, 16370, 16384, 16400])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_where_rows_begin_to_be_cut_into_chunks(V, dtype):
+    z, u = _rows(3, V, dtype, V)
+    for par in FILTERS:
+        _check(z, u, **par)
+
+
+@pytest.mark.parametrize("many", [500, 700, 3000, 9000])
+def test_many_values_where_the_filter_ends(many):
+    V = 40000
+    z, u = _rows(4, V, torch.float32, many, spread=1.0)
+    z = z.clamp(max=4)
+    at = torch.randperm(V, generator=torch.Generator().manual_seed(many))[:many].to(DEV)
+    z[:, at] = 6 + 0.05 * torch.rand(4, many, generator=torch.Generator().manual_seed(1)).to(DEV)  # one bin
+    z[1, at[::2]] = 6.03125  # half of them equal
+    z[2, at] = 6.0
+    for par in (dict(top_k=many // 3), dict(top_p=0.2), dict(top_k=many // 2, top_p=0.6), dict(top_p=0.4, min_p=0.5), dict(top_k=many - 1)):
+        _check(z, u, **par)
