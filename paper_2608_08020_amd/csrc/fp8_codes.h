@@ -34,6 +34,13 @@ __device__ inline uint32_t fp8_codes(float a, float b, float c, float d) {
   return ((uint32_t)w & ~nan) | (0x7f7f7f7fu & nan);
 }
 
+// Sixteen bytes that no one reads again (the loads' non-temporal hint).
+__device__ inline uint4 load_once(const void* p) {
+  typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+  const u32x4 a = __builtin_nontemporal_load(static_cast<const u32x4*>(p));
+  return make_uint4(a[0], a[1], a[2], a[3]);
+}
+
 __device__ inline float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ inline float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
 

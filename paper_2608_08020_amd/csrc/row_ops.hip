@@ -65,6 +65,17 @@ __device__ inline Eight load8(const void* p, size_t at) {
     return from_bf16(*reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p) + at));
   }
 }
+// Rows, which are read once (8192 x 24576 bf16, gated: 94.6 us, 5.35 TB/s; without the hint 102.5 us).
+template <bool kF32>
+__device__ inline Eight load8_once(const void* p, size_t at) {
+  if constexpr (kF32) {
+    const float* q = static_cast<const float*>(p) + at;
+    const float4 a = __builtin_bit_cast(float4, load_once(q)), b = __builtin_bit_cast(float4, load_once(q + 4));
+    return {{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}};
+  } else {
+    return from_bf16(load_once(static_cast<const uint16_t*>(p) + at));
+  }
+}
 __device__ inline void store8_f32(void* p, size_t at, const Eight& y) {
   float4* q = reinterpret_cast<float4*>(static_cast<float*>(p) + at);
   q[0] = make_float4(y.v[0], y.v[1], y.v[2], y.v[3]);
@@ -134,8 +145,8 @@ __global__ __launch_bounds__(kLanes > 256 ? kLanes : 256) void rms_norm_kernel(R
     const int d = 8 * (i * kLanes + l);
     there[i] = d < A.dim;
     if (there[i]) {
-      h[i] = load8<kX32>(A.x, xat + d);
-      if constexpr (kRes) res[i] = load8<kRes == 2>(A.res, at + d);
+      h[i] = load8_once<kX32>(A.x, xat + d);
+      if constexpr (kRes) res[i] = load8_once<kRes == 2>(A.res, at + d);
     } else {
       h[i] = Eight{};
       res[i] = Eight{};
@@ -225,8 +236,8 @@ __global__ __launch_bounds__(256) void quantize_kernel(RowArgs A, uint32_t group
     a[i] = Eight{};
     b[i] = Eight{};
     if (g < total && d < A.dim) {
-      a[i] = load8<kX32>(A.x, (size_t)row * A.row_stride + d);
-      if constexpr (kGated) b[i] = load8<kX32>(A.x, (size_t)row * A.row_stride + A.dim + d);
+      a[i] = load8_once<kX32>(A.x, (size_t)row * A.row_stride + d);
+      if constexpr (kGated) b[i] = load8_once<kX32>(A.x, (size_t)row * A.row_stride + A.dim + d);
     }
   }
 #pragma unroll
