@@ -736,9 +736,10 @@ class Pool:
                 qop = _dev(q_out, torch.bfloat16, shape, "q_out")
         elif q_out is not None:
             raise ValueError("q_out: there are no queries")
+        here = _here(stream, self.k_cache, k, v, table, q, q_out)
         self._check(lib().gambit_kv_write_rotated(self._h, layer, ids.size, _in(ids), _in(p0), _in(nt),
                                                   None if rows is None else _in(rows), n_rows, kp, ks, vp, vs, qp, qs, qop,
-                                                  tp, table.shape[0], table.shape[1], pairs, _stream(stream)),
+                                                  tp, table.shape[0], table.shape[1], pairs, here),
                     "kv_write_rotated")
         return q_out
 
