@@ -29,6 +29,11 @@
 // logits over the temperature beyond 2^10 octaves, where their product with
 // log2(e) / T keeps too few bits) it draws as short rows are, the way of
 // sampling_any.h.
+//
+// Bound by the weights' arithmetic in fp64 (about 36 instructions a value) and the
+// two reads at many rows, by the launches' chain of dependent reads at few.  512 fp32
+// rows of 151936 values, top_p 0.95: 190 us, chunks 110, border 10, gather 66, rows
+// 20; top_k 50: 130 us; eight bf16 rows with filters of their own 38 us.
 #include <algorithm>
 
 #include "../../include/gambit.h"
@@ -46,7 +51,10 @@ constexpr int kNoBin = 1 << 20;                           // below every value's
 constexpr int kList = 8192;
 constexpr int kMaxChunks = (kMaxVocab / 4 + 1 + kThreads - 1) / kThreads;
 constexpr double kMostOctaves = 1024.;
-constexpr int kShortLoads = 2048;  // rows of no more are drawn by sample_any_kernel
+// Rows of no more are drawn by sample_any_kernel (us, in chunks / by it: 8 bf16 rows of
+// 8192 values, top_p 28 / 29, no filter 19 / 11; of 16384, 28 / 40, 19 / 16; 512 fp32 rows
+// of 8192, 51 / 57, 32 / 21).
+constexpr int kShortLoads = 1024;
 
 // Where a row's border falls.
 struct Border {
@@ -721,8 +729,10 @@ struct Cuts {
     const int per = f32 ? 4 : 8, most = (vocab + 2 * (per - 1)) / per;  // a row's loads, wherever it begins
     if (most <= kShortLoads) return;
     segs = (most + 63) / 64;
-    // the largest chunks of which there is one for every other compute unit
-    for (loads = 4; loads > 1 && n * ((most + kThreads * loads - 1) / (kThreads * loads)) < 128;) loads /= 2;
+    // the largest chunks of which there is one for every other compute unit, of sixteen
+    // values a thread at most (us, top_p, one / two / four loads a thread: 8 fp32 rows of
+    // 151936 values 44 / 38 / 37, 512 of them 356 / 255 / 209, 32 bf16 rows 52 / 47 / 52)
+    for (loads = f32 ? 4 : 2; loads > 1 && n * ((most + kThreads * loads - 1) / (kThreads * loads)) < 128;) loads /= 2;
     chunks = (most + kThreads * loads - 1) / (kThreads * loads);
     auto take = [&](size_t size) {
       const size_t o = bytes;
@@ -764,11 +774,9 @@ hipError_t launch(const SampleArgs& A, const Cuts& C, uint8_t* ws, int n, hipStr
                reinterpret_cast<u64*>(ws + C.seg_sum), reinterpret_cast<Border*>(ws + C.border),
                reinterpret_cast<u64*>(ws + C.list)};
   auto some = [&](const SampleArgs& B, int rows) {
-    switch (C.loads) {
-      case 4: return launch_chunks<kF32, 4>(B, W, rows, s);
-      case 2: return launch_chunks<kF32, 2>(B, W, rows, s);
-      default: return launch_chunks<kF32, 1>(B, W, rows, s);
-    }
+    if constexpr (kF32)
+      if (C.loads == 4) return launch_chunks<kF32, 4>(B, W, rows, s);
+    return C.loads == 2 ? launch_chunks<kF32, 2>(B, W, rows, s) : launch_chunks<kF32, 1>(B, W, rows, s);
   };
   for (int r = 0; r < n; r += kRowsAtOnce) {
     SampleArgs B = A;
