@@ -315,8 +315,10 @@ def stream_read(buf: torch.Tensor, nontemporal: bool, grid: int, sink: torch.Ten
 # -- what a layer does between its attention calls
 
 def _strided(t: torch.Tensor, dtypes, shape, what: str):
-    """Address and outer strides of a device tensor of rows: the last dimension dense, the others of any stride >= 0
+    """Address of a device tensor of rows: the last dimension dense, the others of any stride >= 0
     (that of a dimension of one does not matter)."""
+    if type(t) is torch.Tensor and t.is_cuda and t.dtype in dtypes and shape is None and t.stride(-1) == 1:
+        return t.data_ptr()  # (the common argument, sooner)
     if not isinstance(t, torch.Tensor):
         raise ValueError(f"{what}: expected a tensor, got {type(t).__name__}")
     if t.dtype not in dtypes:
@@ -334,8 +336,16 @@ def _outer(t: torch.Tensor, i: int) -> int:
     return t.stride(i) if t.shape[i] > 1 else 0
 
 
+_one_device = None  # whether the machine has one: then every device tensor is the current one's
+
+
 def _here(stream, t: torch.Tensor, *others):
     """The stream's handle for a call whose tensors are all the current device's."""
+    global _one_device
+    if _one_device is None:
+        _one_device = torch.cuda.device_count() == 1
+    if _one_device:
+        return torch._C._cuda_getCurrentRawStream(0) if stream is None else stream.cuda_stream
     d, current = t.get_device(), torch.cuda.current_device()
     if d != current:
         raise ValueError(f"the tensors are on device {d}, device {current} is current")
@@ -352,11 +362,11 @@ def _rows(t: torch.Tensor, shape, what: str):
     return _dev(t, torch.bfloat16, shape, what), 0
 
 
-def _scales(out_scale, dim: int, n: int, device):
+def _scales(out_scale, dim: int, n: int, x: torch.Tensor):
     """The scales of E4M3 rows, one for 128 values: given ones or new ones, and their address."""
     shape = (-(-dim // 128), n)
     if out_scale is None:
-        out_scale = torch.empty(shape, dtype=torch.float32, device=device)
+        out_scale = x.new_empty(shape, dtype=torch.float32)
         return out_scale, out_scale.data_ptr()
     return out_scale, _dev(out_scale, torch.float32, shape, "out_scale")
 
@@ -377,14 +387,14 @@ def rms_norm(x: torch.Tensor, weight: torch.Tensor, eps: float = 1e-6, residual:
     if out_dtype not in ROW_CODES:
         raise ValueError(f"out: expected dtype {tuple(ROW_CODES)}, got {out_dtype}")
     if out is None:
-        out = torch.empty(shape, dtype=out_dtype, device=x.device)
+        out = x.new_empty(shape, dtype=out_dtype)
         op = out.data_ptr()
     else:
         op = _dev(out, out_dtype, shape, "out")
     wp, wd = _rows(weight, (dim,), "weight")
     fp8, sp = out_dtype is E4M3, None
     if fp8:
-        out_scale, sp = _scales(out_scale, dim, n * heads, x.device)
+        out_scale, sp = _scales(out_scale, dim, n * heads, x)
     elif out_scale is not None:
         raise ValueError("out_scale: only E4M3 rows have scales")
     rp = rop = None
@@ -413,11 +423,11 @@ def quantize(x: torch.Tensor, gated: bool = False, out: torch.Tensor | None = No
     n, dim = x.shape[0], x.shape[1] // 2 if gated else x.shape[1]
     xp = _strided(x, FLOAT_CODES, None, "x")
     if out is None:
-        out = torch.empty((n, dim), dtype=E4M3, device=x.device)
+        out = x.new_empty((n, dim), dtype=E4M3)
         op = out.data_ptr()
     else:
         op = _dev(out, E4M3, (n, dim), "out")
-    out_scale, sp = _scales(out_scale, dim, n, x.device)
+    out_scale, sp = _scales(out_scale, dim, n, x)
     s = _here(stream, x, out, out_scale)
     st = lib().gambit_quantize(n, dim, xp, FLOAT_CODES[x.dtype], _outer(x, 0), gated, op, sp, s)
     if st != OK:
@@ -442,7 +452,7 @@ def linear_fp8(x: torch.Tensor, x_scale: torch.Tensor, w: torch.Tensor, w_scale:
     if out_dtype not in OUT_CODES:
         raise ValueError(f"out: expected dtype {tuple(OUT_CODES)}, got {out_dtype}")
     if out is None:
-        out = torch.empty((m, n), dtype=out_dtype, device=x.device)
+        out = x.new_empty((m, n), dtype=out_dtype)
         op = out.data_ptr()
     else:
         op = _dev(out, out_dtype, (m, n), "out")
@@ -455,6 +465,10 @@ def linear_fp8(x: torch.Tensor, x_scale: torch.Tensor, w: torch.Tensor, w_scale:
 
 def _heads(t: torch.Tensor, n: int, what: str):
     """Address and row stride of token rows [n][heads][128] whose heads lie one after another."""
+    if type(t) is torch.Tensor and t.dtype is torch.bfloat16 and t.is_cuda and t.dim() == 3:  # (the common one, sooner)
+        (a, b, c), (sa, sb, sc) = t.shape, t.stride()
+        if a == n and c == 128 and sc == 1 and (sb == 128 or b == 1):
+            return t.data_ptr(), sa if a > 1 else 0
     if not isinstance(t, torch.Tensor) or t.dim() != 3:
         raise ValueError(f"{what}: expected a tensor [n][heads][128]")
     p = _strided(t, (torch.bfloat16,), (n, t.shape[1], 128), what)
@@ -483,7 +497,7 @@ def rotate(q: torch.Tensor | None, k: torch.Tensor | None, positions: torch.Tens
             continue
         xp, stride = _heads(x, n, what)
         if out is None:
-            out = torch.empty(x.shape, dtype=torch.bfloat16, device=x.device)
+            out = x.new_empty(x.shape)
             op = out.data_ptr()
         else:
             op = _dev(out, torch.bfloat16, x.shape, what + "_out")
@@ -514,7 +528,7 @@ def sample(logits: torch.Tensor, u: torch.Tensor, temperature=1.0, top_k=0, top_
         else:
             args += [None, x]
     if out is None:
-        out = torch.empty(n, dtype=torch.int32, device=logits.device)
+        out = u.new_empty(n, dtype=torch.int32)
         op = out.data_ptr()
     else:
         op = _dev(out, torch.int32, (n,), "out")
@@ -523,7 +537,7 @@ def sample(logits: torch.Tensor, u: torch.Tensor, temperature=1.0, top_k=0, top_
     size = lib().gambit_sample_workspace_size(n, vocab, dt)
     wp = None
     if size:
-        ws = torch.empty(size, dtype=torch.uint8, device=logits.device)
+        ws = u.new_empty(size, dtype=torch.uint8)
         if stream is not None:  # (not reused before that stream is done with it)
             ws.record_stream(stream)
         wp = ws.data_ptr()
@@ -730,7 +744,7 @@ class Pool:
                 raise ValueError(f"q: expected {self.Hq} heads, got {q.shape[1]}")
             shape = (total, self.Hq, self.D)
             if q_out is None:
-                q_out = torch.empty(shape, dtype=torch.bfloat16, device=q.device)
+                q_out = q.new_empty(shape)
                 qop = q_out.data_ptr()
             else:
                 qop = _dev(q_out, torch.bfloat16, shape, "q_out")

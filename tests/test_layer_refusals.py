@@ -129,6 +129,7 @@ def test_tensors_of_another_device_are_refused(monkeypatch):
         cuda_stream = 77
 
     monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    monkeypatch.setattr(g, "_one_device", False)
     assert g._here(Stream, On(1), None, On(1)) == 77
     for tensors in ([On(0)], [On(0), On(0)], [On(1), On(0)], [On(1), None, On(-1)]):
         with pytest.raises(ValueError, match="device"):
