@@ -506,13 +506,17 @@ extern "C" gambit_status gambit_linear_fp8(int32_t m, int32_t n, int32_t k, cons
     // Tiles of 256 x 256 re-read least, but need one for each of the 256 CUs.  Of the
     // small ones two workgroups share a CU (two stages each) or, where there is one a
     // CU at most, a third stage hides the loads (us, two / three stages: 224 tiles
-    // 64 / 57, 768 tiles 55 / 65).
+    // 64 / 57, 768 tiles 55 / 65); halves of them while one round takes those (us, 128 x
+    // 128 / 128 x 64, k 4096: 512 tokens, 4096 features 20.9 / 16.9; 150, 6144 20.8 / 15.8;
+    // two rounds of them: 1024, 4096 23.1 / 25.2).
     else if (tiles(256) >= 256)
       tile(linear_tile_kernel<false, 256, 256, 2, 4, 2>, 256, 256, 512);
     else if (tiles(128) > 256)
       tile(linear_tile_kernel<false, 128, 128, 2, 4, 2>, 128, 128, 512);
-    else
+    else if ((int64_t)((n + 127) / 128) * ((m + 63) / 64) > 256)
       tile(linear_tile_kernel<false, 128, 128, 2, 4, 3>, 128, 128, 512);
+    else
+      tile(linear_tile_kernel<false, 128, 64, 4, 2, 3>, 128, 64, 512);
   };
   A.f32 ? choose(std::true_type{}) : choose(std::false_type{});
   return hipGetLastError() == hipSuccess ? GAMBIT_OK : GAMBIT_ERR_DEVICE;

@@ -133,3 +133,14 @@ def test_nothing_behind_the_outputs_is_written(m, n):
         g.linear_fp8(*args, out=out)
         assert (whole[:lead] == 7).all() and (whole[lead + m * n:] == 7).all()
         assert torch.equal(out, g.linear_fp8(*args, out_dtype=dtype))
+
+
+@pytest.mark.parametrize("m,n,k", [(150, 6144, 272), (1024, 2048, 144), (1025, 2048, 400), (513, 4099, 272), (129, 16, 1040)])
+def test_tiles_of_half_the_tokens(m, n, k):
+    args = _inputs(m, n, k, 7)
+    out = g.linear_fp8(*args)
+    x, xs, w, ws = args
+    at = (n - 1) // 128 * 128
+    _check(out[:, at:], x, xs, w[at:], ws[at // 128:])
+    rows = torch.tensor([0, 63, 64, m // 2, m - 1], device=DEV)
+    _check(out[rows], x[rows], xs[:, rows], w, ws)
