@@ -490,12 +490,16 @@ extern "C" gambit_status gambit_linear_fp8(int32_t m, int32_t n, int32_t k, cons
     const int64_t groups = (n + 15) / 16;
     // Few tokens: sixteen features a workgroup while 128 of them would leave CUs without
     // one (k 4096, us, sixteen / 128: 64 tokens, 6144 features 10.7 / 15.2, 12288 20.1 /
-    // 15.7; 32 tokens, 12288 11.7 / 15.6, 24576 20.9 / 16.7; 8 tokens, fp32, 151936
-    // 123 / 140).  Up to sixteen tokens, two stages let four workgroups share a CU, four
-    // stages two (us, two / four: 768 workgroups 8.2 / 11.8, 256 of k 12288 14.8 / 12.3).
-    if (m <= 16 && groups > 512)
+    // 15.7; 32 tokens, 12288 11.7 / 15.6, 24576 20.9 / 16.7).  Up to sixteen tokens these
+    // take the larger sizes too, but for bf16 output as long as one round holds the tiles
+    // of 128 (8 tokens, 16384 12.8 / 15.9, 24576 20.8 / 16.6, 32768 23.7 / 20.9, 151936 123 /
+    // 133; fp32, 24576 21 / 25, 151936 123 / 140); two stages let four of their workgroups
+    // share a CU, four stages two (us, two / four: 768 workgroups 8.2 / 11.8, 256 of k
+    // 12288 14.8 / 12.3).
+    const bool sixteen = kExact || n <= 16384 || n > 128 * 512;
+    if (m <= 16 && sixteen && groups > 512)
       split(linear_split_kernel<kExact, 16, 2>, 16);
-    else if (m <= 16)
+    else if (m <= 16 && sixteen)
       split(linear_split_kernel<kExact, 16, 4>, 16);
     else if (m <= 128 && n < (m <= 32 ? 16384 : 8192))
       split(linear_split_kernel<kExact, 32, 3>, 32);

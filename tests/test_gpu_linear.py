@@ -144,3 +144,11 @@ def test_tiles_of_half_the_tokens(m, n, k):
     _check(out[:, at:], x, xs, w[at:], ws[at // 128:])
     rows = torch.tensor([0, 63, 64, m // 2, m - 1], device=DEV)
     _check(out[rows], x[rows], xs[:, rows], w, ws)
+
+
+@pytest.mark.parametrize("m", [1, 16])
+@pytest.mark.parametrize("n", [16385, 65536, 65537])
+def test_few_tokens_and_many_features(m, n):
+    args = _inputs(m, n, 400, 8)
+    for dtype in (torch.bfloat16, torch.float32):
+        _check(g.linear_fp8(*args, out_dtype=dtype), *args)
