@@ -77,17 +77,22 @@ struct Row {
   __device__ __forceinline__ bool there(int load) const { return (uint32_t)load < (uint32_t)loads; }
   __device__ __forceinline__ bool whole(int load) const { return there(load) && index(load, 0) >= 0 && index(load, 0) + kPer <= vocab; }
   __device__ __forceinline__ uint4 raw(int load) const { return *reinterpret_cast<const uint4*>(base + (size_t)load * 16); }
-  __device__ __forceinline__ static void unpack(uint4 a, float* z) {
+  __device__ __forceinline__ static void unpack_as_is(uint4 a, float* z) {
     const uint32_t w[4] = {a.x, a.y, a.z, a.w};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       if constexpr (kF32) {
-        z[i] = clean(__uint_as_float(w[i]));
+        z[i] = __uint_as_float(w[i]);
       } else {
-        z[2 * i] = clean(bf16_lo(w[i]));
-        z[2 * i + 1] = clean(bf16_hi(w[i]));
+        z[2 * i] = bf16_lo(w[i]);
+        z[2 * i + 1] = bf16_hi(w[i]);
       }
     }
+  }
+  __device__ __forceinline__ static void unpack(uint4 a, float* z) {
+    unpack_as_is(a, z);
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) z[i] = clean(z[i]);
   }
   // The values of a load that the row holds in part or not at all: places outside it are not read and count as -inf.
   __device__ __forceinline__ void edge(int load, float* z) const {

@@ -49,6 +49,7 @@ static_assert(kThreads == kAnyThreads, "one kernel holds both ways");
 constexpr int kOctaveBins = 8, kBins = 24 * kOctaveBins;  // a histogram's; smaller weights are not told apart
 constexpr int kNoBin = 1 << 20;                           // below every value's
 constexpr int kList = 8192;
+constexpr int kOwn = 1024;  // a chunk's share of it that is gathered in LDS
 constexpr int kMaxChunks = (kMaxVocab / 4 + 1 + kThreads - 1) / kThreads;
 constexpr double kMostOctaves = 1024.;
 // Rows of no more are drawn by sample_any_kernel (us, in chunks / by it: 8 bf16 rows of
@@ -118,6 +119,8 @@ __device__ inline u64 weight_at(float z, const Scale& S, const double* powers) {
 }
 
 // A thread's loads of its chunk: load i of wave w is segment 8 i + w of the chunk.
+// Values as they are: a maximum over them passes quiet NaN by, a row with +inf is out of
+// range, and comparisons with a border leave both out.
 template <bool kF32, int kLoads>
 struct Chunk {
   typedef Row<kF32> R;
@@ -138,7 +141,7 @@ struct Chunk {
     for (int i = 0; i < kLoads; ++i) {
       if (!wanted(i)) continue;
       if (row.whole(load(i)))
-        R::unpack(a[i], z[i]);
+        R::unpack_as_is(a[i], z[i]);
       else
         row.edge(load(i), z[i]);
     }
@@ -165,10 +168,13 @@ __global__ __launch_bounds__(kThreads) void sample_chunks_kernel(SampleArgs A, L
   float most = -INFINITY;
 #pragma unroll
   for (int i = 0; i < kLoads; ++i) {
-    float m = C.z[i][0];
+    float m = -INFINITY;
 #pragma unroll
-    for (int e = 1; e < R::kPer; ++e) m = fmaxf(m, C.z[i][e]);
-    m = wave_max(m);
+    for (int e = 0; e < R::kPer; ++e) {
+      C.z[i][e] = __builtin_canonicalizef(C.z[i][e]);  // (a signalling NaN is the result of a maximum)
+      m = fmaxf(m, C.z[i][e]);
+    }
+    m = fminf(wave_max(m), FLT_MAX);
     if (lane == 0 && C.seg(i) < W.segs) W.seg_most[(size_t)r * W.segs + C.seg(i)] = m;
     most = fmaxf(most, m);
   }
@@ -293,7 +299,8 @@ template <bool kF32, int kLoads>
 __global__ __launch_bounds__(kThreads) void sample_gather_kernel(SampleArgs A, Left W) {
   __shared__ double powers[64];
   __shared__ float seg_most[8 * kLoads];
-  __shared__ uint32_t listed[kWaves], base;
+  __shared__ u64 own[kOwn];  // the list's values of this chunk
+  __shared__ uint32_t listed, base;
   typedef Row<kF32> R;
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
   const int r = blockIdx.x / W.chunks, c = blockIdx.x % W.chunks;
@@ -304,6 +311,7 @@ __global__ __launch_bounds__(kThreads) void sample_gather_kernel(SampleArgs A, L
   if (way == kGreedy || way == kAll || B.bin < 0 || B.top == -INFINITY) return;
   if (t < 8 * kLoads && c * 8 * kLoads + t < W.segs) seg_most[t] = W.seg_most[(size_t)r * W.segs + c * 8 * kLoads + t];
   if (t < 64) powers[t] = exp2(t / 64.);
+  if (t == 0) listed = 0;
   __syncthreads();
   const Scale S(F.slope, B.top);
   const double least = F.least();
@@ -316,7 +324,9 @@ __global__ __launch_bounds__(kThreads) void sample_gather_kernel(SampleArgs A, L
   };
   C.read(wanted);
   const bool sums = way != kTopP || least > -INFINITY;  // (else the chunks' weights are known)
-  u64 flags = 0;  // of the thread's values: listed
+  auto put = [&](uint32_t at, u64 entry) {
+    if (at < (uint32_t)kList) W.list[(size_t)r * kList + at] = entry;
+  };
 #pragma unroll
   for (int i = 0; i < kLoads; ++i) {
     if (C.seg(i) >= W.segs) continue;
@@ -329,9 +339,14 @@ __global__ __launch_bounds__(kThreads) void sample_gather_kernel(SampleArgs A, L
         double rest;
         const int q = S.at(z, &rest), at = bin_of(q);
         if (at > b) continue;
-        if (at == b || way == kBoth)
-          flags |= 1ull << (i * R::kPer + k);
-        else if (sums && likely(z))
+        if (at == b || way == kBoth) {
+          const u64 entry = entry_of(R::clean(z), C.row.index(C.load(i), k));
+          const uint32_t n = atomicAdd(&listed, 1u);
+          if (n < (uint32_t)kOwn)
+            own[n] = entry;
+          else
+            put(atomicAdd(&W.border[r].listed, 1u), entry);
+        } else if (sums && likely(z))
           sum += weight_of(q, rest, powers);
       }
       if (sums) sum = wave_total(sum);
@@ -339,29 +354,12 @@ __global__ __launch_bounds__(kThreads) void sample_gather_kernel(SampleArgs A, L
     if (lane == 0 && sums) W.seg_sum[(size_t)r * W.segs + C.seg(i)] = sum;
   }
   if (b == kNoBin) return;
-  // the values' places in the row's list: one claim a workgroup
-  uint32_t n = __popcll(flags), at = (uint32_t)wave_before(n, lane);
-  if (lane == 63) listed[wave] = at + n;
+  // their places in the row's list: one claim a workgroup
   __syncthreads();
-  if (t == 0) {
-    uint32_t all = 0;
-    for (int w = 0; w < kWaves; ++w) {
-      const uint32_t x = listed[w];
-      listed[w] = all;
-      all += x;
-    }
-    base = all ? atomicAdd(&W.border[r].listed, all) : 0;
-  }
+  const uint32_t n = min(listed, (uint32_t)kOwn);
+  if (t == 0 && n) base = atomicAdd(&W.border[r].listed, n);
   __syncthreads();
-  at += base + listed[wave];
-#pragma unroll
-  for (int i = 0; i < kLoads; ++i)
-#pragma unroll
-    for (int k = 0; k < R::kPer; ++k)
-      if (flags >> (i * R::kPer + k) & 1) {
-        if (at < (uint32_t)kList) W.list[(size_t)r * kList + at] = entry_of(C.z[i][k], C.row.index(C.load(i), k));
-        ++at;
-      }
+  for (uint32_t i = t; i < n; i += kThreads) put(base + i, own[i]);
 }
 
 struct RowShared {

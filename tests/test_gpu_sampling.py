@@ -191,3 +191,27 @@ def test_many_values_where_the_filter_ends(many):
     z[2, at] = 6.0
     for par in (dict(top_k=many // 3), dict(top_p=0.2), dict(top_k=many // 2, top_p=0.6), dict(top_p=0.4, min_p=0.5), dict(top_k=many - 1)):
         _check(z, u, **par)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_long_rows_with_masked_and_not_finite_logits(dtype):
+    V, n = 40000, 10
+    z, u = _rows(n, V, torch.float32, 8)
+    z = z.to(dtype)
+    ints = z.view(torch.int16 if dtype == torch.bfloat16 else torch.int32)
+    quiet, signalling = (0x7FC0, 0x7F81) if dtype == torch.bfloat16 else (0x7FC00000, 0x7F800001)
+    z[0, ::2] = math.nan
+    ints[1, ::3] = signalling  # as bits: copies keep them
+    ints[2, 5::7] = quiet - (1 << (16 if dtype == torch.bfloat16 else 32)) | (1 << 15 if dtype == torch.bfloat16 else 1 << 31)  # negative
+    z[3, 100] = math.inf
+    z[4, 7::5] = math.inf
+    z[5] = -math.inf
+    z[5, 31234] = 1.5
+    z[6] = math.nan
+    z[7] = -math.inf
+    z[8, :39000] = torch.finfo(dtype).min
+    z[9] = -0.0
+    z[9, 20000:] = 0.0
+    assert torch.isnan(z[1, 0]) and torch.isnan(z[2, 5])
+    for par in FILTERS:
+        _check(z, u, **par)
