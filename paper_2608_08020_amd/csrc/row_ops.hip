@@ -244,9 +244,9 @@ __global__ __launch_bounds__(256) void quantize_kernel(RowArgs A, uint32_t group
   for (int i = 0; i < kUnroll; ++i) {
     const uint32_t g = g0 + 16 * i, row = g / groups;
     const int d = (g % groups) * kGroup + 8 * l;
-    if constexpr (kGated)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) a[i].v[e] = silu(a[i].v[e]) * b[i].v[e];
+    for (int e = 0; e < 8; ++e)  // (as it is, a signalling NaN would be the result of a maximum)
+      a[i].v[e] = kGated ? silu(a[i].v[e]) * b[i].v[e] : __builtin_canonicalizef(a[i].v[e]);
     float s;
     const uint2 c = codes8(a[i], &s);
     if (g < total && d < A.dim) {

@@ -213,3 +213,20 @@ def test_values_that_are_not_finite():
     kk, _ = s.tokens(0, 0, 0, 16)
     assert torch.isnan(kk[3, 0, [5, 69]]).all()
     assert torch.isfinite(kk[[0, 1, 2] + list(range(5, 16))]).all() and torch.isfinite(s.pool.kv_scale[0]).all()
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("rot", [16, 128])
+def test_signalling_nan_counts_as_nan(fp8, rot):
+    got = []
+    for bits in (0x7F81, 0x7FC0):
+        s = Kept(8, 2, T=1, maxb=4, fp8=fp8, seed=3)
+        s.pool.kv_alloc([0], [40])
+        q, k, v = (t.contiguous() for t in _packed(40, 8, 2, 7))
+        for t in (q, k, v):
+            t[..., ::8] = 3.0  # before it
+            t.view(torch.int16)[5:, :, 1::8] = bits
+        qo = s.pool.kv_write_rotated(0, [0], [0], [40], k, v, _table(60, rot), q=q)
+        got.append([torch.nan_to_num(qo.float(), nan=77.0)] + [torch.nan_to_num(t.float(), nan=77.0) for t in s.tokens(0, 0, 0, 40)] + ([s.pool.kv_scale] if fp8 else []))
+    for a, b in zip(*got):
+        assert torch.equal(a, b)

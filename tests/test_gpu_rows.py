@@ -180,3 +180,19 @@ def test_no_rows():
     assert g.rms_norm(torch.empty(0, 128, device=DEV), w).shape == (0, 128)
     codes, scale = g.quantize(torch.empty(0, 128, device=DEV))
     assert codes.shape == (0, 128) and scale.shape == (1, 0)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_signalling_nan_counts_as_nan(dtype):
+    x = _normal(3, 5, 512, dtype=dtype)
+    bits = x.view(torch.int16 if dtype == BF16 else torch.int32)
+    x[:, ::128] = 100.0  # a group's largest, just before it
+    quiet = x.clone()
+    bits[:, 1::8] = 0x7F81 if dtype == BF16 else 0x7F800001
+    quiet[:, 1::8] = float("nan")
+    assert torch.isnan(x[:, 1::8]).all()
+    (c, s), (cq, sq) = g.quantize(x), g.quantize(quiet)
+    assert torch.equal(s, sq) and torch.equal(c.view(torch.uint8), cq.view(torch.uint8)) and (s == 100 / 448).all()
+    (c, s), (cq, sq) = g.quantize(x, gated=True), g.quantize(quiet, gated=True)
+    assert torch.equal(s, sq) and torch.equal(c.view(torch.uint8), cq.view(torch.uint8))
+    assert torch.isnan(g.rms_norm(x, torch.ones(512, device=DEV))).all()
