@@ -133,7 +133,7 @@ __device__ inline void dma_dword(const void* base, uint32_t at, uint32_t lds) {
 // set once a load; it is restored, as the compiler does not track it here.)
 template <int kLoads>
 __device__ inline void dma_rows(const uint8_t* base, const uint32_t* at, uint32_t lds) {
-  static_assert(kLoads == 2 || kLoads == 4 || kLoads == 8, "");
+  static_assert(kLoads == 4 || kLoads == 8, "");
   uint32_t save;
 #define DMA_NEXT(v) "s_add_u32 m0, m0, 0x400\n\ts_nop 0\n\tglobal_load_lds_dwordx4 " v ", %2\n\t"
   if constexpr (kLoads == 8)
@@ -143,19 +143,12 @@ __device__ inline void dma_rows(const uint8_t* base, const uint32_t* at, uint32_
                  : "=&s"(save)
                  : "s"(lds), "s"(base), "v"(at[0]), "v"(at[1]), "v"(at[2]), "v"(at[3]), "v"(at[4]), "v"(at[5]), "v"(at[6]), "v"(at[7])
                  : "memory", "scc");
-  else if constexpr (kLoads == 4)
+  else
     asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %3, %2\n\t"
                  DMA_NEXT("%4") DMA_NEXT("%5") DMA_NEXT("%6")
                  "s_mov_b32 m0, %0"
                  : "=&s"(save)
                  : "s"(lds), "s"(base), "v"(at[0]), "v"(at[1]), "v"(at[2]), "v"(at[3])
-                 : "memory", "scc");
-  else
-    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %3, %2\n\t"
-                 DMA_NEXT("%4")
-                 "s_mov_b32 m0, %0"
-                 : "=&s"(save)
-                 : "s"(lds), "s"(base), "v"(at[0]), "v"(at[1])
                  : "memory", "scc");
 #undef DMA_NEXT
 }

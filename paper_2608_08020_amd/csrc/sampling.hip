@@ -30,10 +30,10 @@
 // log2(e) / T keeps too few bits) it draws as short rows are, the way of
 // sampling_any.h.
 //
-// Bound by the weights' arithmetic in fp64 (about 36 instructions a value) and the
+// Bound by the weights' arithmetic in fp64 (over 30 instructions a value) and the
 // two reads at many rows, by the launches' chain of dependent reads at few.  512 fp32
-// rows of 151936 values, top_p 0.95: 190 us, chunks 110, border 10, gather 66, rows
-// 20; top_k 50: 130 us; eight bf16 rows with filters of their own 38 us.
+// rows of 151936 values, top_p 0.95: 175 us, chunks 105, border 10, gather 55, rows
+// 20; eight bf16 rows with filters of their own 38 us.
 #include <algorithm>
 
 #include "../../include/gambit.h"
