@@ -262,13 +262,16 @@ void launch_norm(const RowArgs& A, hipStream_t s) {
     const int threads = lanes > 256 ? lanes : 256, per = threads / lanes;
     hipLaunchKernelGGL(kernel, dim3((A.rows + per - 1) / per), dim3(threads), 0, s, A);
   };
-  // the fewest lanes and loads that hold a row
+  // The fewest lanes and loads that hold a row, but for two sizes where more lanes are
+  // sooner (us, 8 / 512 / 8192 rows and a residual: 1024 values, 64 lanes 3.9, 3.9, 22.1, 256
+  // lanes 3.9, 3.9, 21.0 - 640 values 13.7 and 16.0 at 8192 rows -; 8192 values, 256 lanes
+  // 5.5, 10.5, 143, 1024 lanes 4.4, 9.5, 139; 4096 values, 4.0, 6.2, 74.8 and 3.9, 6.2, 78.4).
   if (A.dim <= 128) return go(rms_norm_kernel<16, 1, kX32, kRes>, 16);
   if (A.dim <= 512) return go(rms_norm_kernel<64, 1, kX32, kRes>, 64);
-  if (A.dim <= 1024) return go(rms_norm_kernel<64, 2, kX32, kRes>, 64);
+  if (A.dim <= 768) return go(rms_norm_kernel<64, 2, kX32, kRes>, 64);
   if (A.dim <= 2048) return go(rms_norm_kernel<256, 1, kX32, kRes>, 256);
   if (A.dim <= 4096) return go(rms_norm_kernel<256, 2, kX32, kRes>, 256);
-  if (A.dim <= 8192) return go(rms_norm_kernel<256, 4, kX32, kRes>, 256);
+  if (A.dim <= 8192) return go(rms_norm_kernel<1024, 1, kX32, kRes>, 1024);
   if (A.dim <= 16384) return go(rms_norm_kernel<1024, 2, kX32, kRes>, 1024);
   return go(rms_norm_kernel<1024, 4, kX32, kRes>, 1024);
 }

@@ -196,3 +196,15 @@ def test_signalling_nan_counts_as_nan(dtype):
     (c, s), (cq, sq) = g.quantize(x, gated=True), g.quantize(quiet, gated=True)
     assert torch.equal(s, sq) and torch.equal(c.view(torch.uint8), cq.view(torch.uint8))
     assert torch.isnan(g.rms_norm(x, torch.ones(512, device=DEV))).all()
+
+
+@pytest.mark.parametrize("dim", [640, 768, 776, 1024, 4104, 5120, 6144, 8192])
+def test_norm_at_other_lane_counts(dim):
+    for n in (1, 3, 9):
+        x, w, r = _normal(1, n, dim), _normal(2, dim, dtype=F32), _normal(3, n, dim, dtype=F32)
+        y, h = layer.rms_norm(_np(x), _np(w), 1e-6, _np(r))
+        out = torch.empty_like(r)
+        _check(g.rms_norm(x, w, residual=r, residual_out=out, out_dtype=F32), y)
+        assert np.abs(_np(out) - h).max() <= 2.0 ** -24 * np.abs(h).max()
+        if dim % 16 == 0:
+            _check_codes(*g.rms_norm(x, w, residual=r, residual_out=out, out_dtype=E4M3), y, REL)
